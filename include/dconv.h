@@ -57,6 +57,7 @@ extern "C" {
 #define DCONV_ERANGE (-3)       /* a tensor has more than 2^31-1 elements */
 #define DCONV_EHIP (-4)         /* the HIP runtime reported an error */
 #define DCONV_EUNSUPPORTED (-5) /* the forced variant cannot run this shape */
+#define DCONV_EWORKSPACE (-6)   /* the workspace is smaller than the call needs */
 
 /* Kernel families for the *_variant calls and the plans. */
 #define DCONV_VARIANT_AUTO 0 /* the planner's choice */
@@ -318,6 +319,166 @@ int dconv_plan_single_paper(int Wx, int Wy, int K, int M, const dconv_device_par
  * `stream`; read `out` after synchronising.
  */
 int dconv_probe_latency(const int *chain, int steps, long long *out, void *stream);
+
+/* ==========================================================================
+ * Operators of an attention block over a map's tokens
+ *
+ * A map of C channels read row by row is a sequence of tokens of C values; a
+ * clip adds a time axis.  The calls below are what a block over such tokens
+ * (or over text) needs beside its matrix products.  They take fp32, fp16 or
+ * bf16 tensors, compute in fp32 (sums, statistics and angles included) and
+ * round each output once.  As for the convolutions: device pointers owned by
+ * the caller, arguments validated before any HIP call, work enqueued on
+ * `stream`, nothing allocated (a workspace is the caller's), bitwise equal
+ * results for equal calls on a device.  Strides count elements; the last
+ * dimension of every tensor is contiguous.  Tensors start on a multiple of
+ * their element's size; whole 16-byte rows are faster.
+ * ======================================================================== */
+
+/* Element types. */
+#define DCONV_F32 0
+#define DCONV_F16 1
+#define DCONV_BF16 2
+
+/*
+ * dconv_rotate -- rotary positions with several axes.
+ *
+ * Pair r < R of every head is turned by the angle positions[axis[r]][b][t] *
+ * freq[r]:  (u, w) -> (u cos - w sin, u sin + w cos), with u, w the elements
+ * 2r, 2r+1 of the head (adjacent = 1) or r, r+R (adjacent = 0).  inverse = 1
+ * turns by the negative angle, which is the gradient: dx = inverse(dy).
+ * Elements from 2R on are copied.  The angle is reduced without loss, so it
+ * is as accurate at position 10^6 as at 1.
+ *
+ *   x, out : [B][T][H][D], strides for batch, token, head; out may be x
+ *   positions : fp32 [axes][B][T] with strides for axis, batch, token (0 to
+ *               share the positions of one sequence)
+ *   freq : fp32 [R], radians per unit of position;  axis : int32 [R] (a pair
+ *               whose axis is not in 0 .. axes-1 is left as it is)
+ * B = 0 or T = 0 is a call without work.
+ */
+typedef struct dconv_rotate_shape {
+  int B, T, H, D;
+  int R, axes;
+  int adjacent, inverse;
+  int dtype;
+  long long x_stride[3], out_stride[3];
+  long long pos_stride[3];
+} dconv_rotate_shape;
+
+int dconv_rotate(const dconv_rotate_shape *shape, const void *x, const float *positions,
+                 const float *freq, const int *axis, void *out, void *stream);
+
+/*
+ * dconv_join -- from a block's output to the next block's input:
+ *
+ *   p = N(branch) * post_weight   (post = 1)   or   branch   (post = 0)
+ *   h = residual_scale * x + branch_scale * gate * p
+ *   y = N(h) * pre_weight + pre_bias
+ *   N(z) = (z - m) / sqrt(mean((z - m)^2) + eps),  m = mean(z) (DCONV_NORM_LAYER)
+ *          or 0 (DCONV_NORM_RMS), over the last dimension
+ *
+ *   branch, x : [B][T][D] with strides for batch and token
+ *   h, y : [B][T][D] contiguous, written
+ *   post_weight, gate, pre_weight, pre_bias : vectors of vector_dtype (the
+ *     tensors' type or fp32), [D], or [B][D] where per_sample has the vector's
+ *     bit; NULL stands for ones (zeros for pre_bias)
+ *   stats : NULL, or fp32 [B*T][4], written: mean and 1 / sqrt(..) of branch
+ *     (0, 1 without post), then of h; what dconv_join_backward reads
+ * branch = NULL is the norm before the first block (h = residual_scale * x,
+ * post and gate unused; h may be NULL); y = NULL leaves out the second norm
+ * (after the last block).  1 <= D <= 16384.
+ */
+#define DCONV_NORM_RMS 0
+#define DCONV_NORM_LAYER 1
+#define DCONV_JOIN_POST_WEIGHT 1 /* bits of per_sample */
+#define DCONV_JOIN_GATE 2
+#define DCONV_JOIN_PRE_WEIGHT 4
+#define DCONV_JOIN_PRE_BIAS 8
+
+typedef struct dconv_join_shape {
+  int B, T, D;
+  int dtype, vector_dtype;
+  int norm, post;
+  int per_sample;
+  float residual_scale, branch_scale, eps;
+  long long branch_stride[2], x_stride[2];
+  long long dh_stride[2], dy_stride[2]; /* of the backward call's inputs */
+} dconv_join_shape;
+
+int dconv_join(const dconv_join_shape *shape, const void *branch, const void *x,
+               const void *post_weight, const void *gate, const void *pre_weight,
+               const void *pre_bias, void *h, void *y, float *stats, void *stream);
+
+/*
+ * dconv_join_backward -- the gradients of dconv_join for the gradients dh, dy
+ * of its outputs (either may be NULL: zeros; dy must be NULL where the forward
+ * call had no y).  branch, x, the vectors and stats are the forward call's.
+ * Written: dbranch, dx [B][T][D] contiguous, and d* of each vector in the
+ * vector's layout and type, summed over what the vector was broadcast over.
+ * A vector's gradient may be NULL (not wanted); for the vectors that the
+ * forward call had as NULL it must be.  dbranch is NULL if branch is.
+ * `workspace`: dconv_join_workspace bytes of device memory, 16-byte aligned.
+ */
+int dconv_join_workspace(const dconv_join_shape *shape, long long *bytes);
+
+int dconv_join_backward(const dconv_join_shape *shape, const void *dh, const void *dy,
+                        const void *branch, const void *x, const void *post_weight,
+                        const void *gate, const void *pre_weight, const float *stats,
+                        void *dbranch, void *dx, void *dpost_weight, void *dgate,
+                        void *dpre_weight, void *dpre_bias, void *workspace,
+                        long long workspace_bytes, void *stream);
+
+/*
+ * dconv_attend -- softmax attention with a sliding window and a few first keys
+ * that stay visible.
+ *
+ * Sequence b has lengths[b] keys, and its query t stands at position
+ * i = starts[b] + t.  Key j is visible to it if
+ *     j < lengths[b],  i >= 0,  j <= i + right,  and  (j >= i - left or j < sinks).
+ * right = 0 is causal attention; left or right = -1 is without that limit.
+ * Head h reads the keys and values of head h / (Hq / Hkv).
+ *     out = sum_j softmax_j(scale * q.k_j) v_j  over the visible keys;
+ *     lse = log sum_j exp(scale * q.k_j)
+ * A query that sees no key has out = 0 and lse = -infinity.  Keys and values
+ * that a query does not see do not reach its result, whatever they hold.
+ *
+ *   q, out : [B][Tq][Hq][D]   k, v : [B][Tk][Hkv][D]   strides for batch,
+ *     token, head;  out must not overlap the inputs
+ *   lse : NULL or fp32 [B][Hq][Tq], written
+ *   lengths : int32 [B], taken as 0 .. Tk, or NULL: Tk each
+ *   starts : int32 [B] or NULL: lengths[b] - Tq (the queries are the last ones)
+ *   workspace : dconv_attend_workspace bytes (0 for many calls: then NULL will
+ *     do), 16-byte aligned
+ * 1 <= D <= 256.  B = 0, Tq = 0 is a call without work; Tk = 0 writes zeros.
+ */
+typedef struct dconv_attend_shape {
+  int B, Tq, Tk, Hq, Hkv, D;
+  int dtype;
+  int left, right, sinks;
+  float scale;
+  long long q_stride[3], k_stride[3], v_stride[3], out_stride[3];
+  long long dout_stride[3]; /* of the backward call's input */
+} dconv_attend_shape;
+
+int dconv_attend_workspace(const dconv_attend_shape *shape, long long *bytes);
+
+int dconv_attend(const dconv_attend_shape *shape, const void *q, const void *k, const void *v,
+                 const int *lengths, const int *starts, void *out, float *lse, void *workspace,
+                 long long workspace_bytes, void *stream);
+
+/*
+ * dconv_attend_backward -- the gradients dq, dk, dv of dconv_attend for the
+ * gradient dout of its output; out and lse are what it wrote.  dq [B][Tq][Hq][D]
+ * and dk, dv [B][Tk][Hkv][D] are contiguous and written whole (zeros where
+ * nothing reaches), the latter summed over the heads that share a key head.
+ */
+int dconv_attend_backward_workspace(const dconv_attend_shape *shape, long long *bytes);
+
+int dconv_attend_backward(const dconv_attend_shape *shape, const void *dout, const void *q,
+                          const void *k, const void *v, const void *out, const float *lse,
+                          const int *lengths, const int *starts, void *dq, void *dk, void *dv,
+                          void *workspace, long long workspace_bytes, void *stream);
 
 #ifdef __cplusplus
 }

@@ -1,0 +1,134 @@
+// Attention with a sliding window and first keys that stay visible
+// (dconv_attend, dconv_attend_backward): validation and launch.
+#include <climits>
+#include <cmath>
+
+#include "attend.h"
+
+#define DCONV_EXPORT extern "C" __attribute__((visibility("default")))
+
+namespace dconv {
+namespace {
+
+// One wave per row, four rows per workgroup.
+template <class T, int KIND>
+__global__ __launch_bounds__(256) void attend_rows(const dconv_attend_shape sh, const AttendPtrs p,
+                                                   const int64_t n, const int heads, const int T_) {
+  const int64_t i = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (i >= n) return;
+  const int t = (int)(i % T_), h = (int)(i / T_ % heads), b = (int)(i / T_ / heads);
+  if constexpr (KIND == 0) attend_row<T>(sh, p, b, h, t);
+  if constexpr (KIND == 1) attend_row_dq<T>(sh, p, b, h, t);
+  if constexpr (KIND == 2) attend_row_dkv<T>(sh, p, b, h, t);
+}
+
+template <class T, int KIND>
+void rows(const dconv_attend_shape &sh, const AttendPtrs &p, hipStream_t s) {
+  const int heads = KIND == 2 ? sh.Hkv : sh.Hq, len = KIND == 2 ? sh.Tk : sh.Tq;
+  const int64_t n = (int64_t)sh.B * heads * len;
+  if (n > 0)
+    hipLaunchKernelGGL((attend_rows<T, KIND>), dim3((unsigned)((n + 3) / 4)), dim3(256), 0, s, sh, p,
+                       n, heads, len);
+}
+
+template <class F>
+void by_type(int dtype, F f) {
+  if (dtype == DCONV_F32) return f((float *)nullptr);
+  if (dtype == DCONV_F16) return f((f16_t *)nullptr);
+  return f((bf16_t *)nullptr);
+}
+
+int validate(const dconv_attend_shape &sh) {
+  if (sh.B < 0 || sh.Tq < 0 || sh.Tk < 0 || sh.Hq < 1 || sh.Hkv < 1 || sh.Hq % sh.Hkv || sh.D < 1 ||
+      sh.left < -1 || sh.right < -1 || sh.sinks < 0 || !element_size(sh.dtype) ||
+      !std::isfinite(sh.scale))
+    return DCONV_EINVAL;
+  if (sh.D > kAttendMaxD) return DCONV_EUNSUPPORTED;
+  // rows of queries and of keys are counted in 32 bits
+  if ((int64_t)sh.B * sh.Hq > INT_MAX / ((int64_t)(sh.Tq > sh.Tk ? sh.Tq : sh.Tk) + 1))
+    return DCONV_ERANGE;
+  return DCONV_OK;
+}
+
+int64_t forward_workspace(const dconv_attend_shape &) { return 0; }
+int64_t backward_workspace(const dconv_attend_shape &) { return 0; }
+
+}  // namespace
+}  // namespace dconv
+
+DCONV_EXPORT int dconv_attend_workspace(const dconv_attend_shape *shape, long long *bytes) {
+  if (!shape || !bytes) return DCONV_ENULL;
+  const int rc = dconv::validate(*shape);
+  if (rc == DCONV_OK) *bytes = dconv::forward_workspace(*shape);
+  return rc;
+}
+
+DCONV_EXPORT int dconv_attend_backward_workspace(const dconv_attend_shape *shape, long long *bytes) {
+  if (!shape || !bytes) return DCONV_ENULL;
+  const int rc = dconv::validate(*shape);
+  if (rc == DCONV_OK) *bytes = dconv::backward_workspace(*shape);
+  return rc;
+}
+
+DCONV_EXPORT int dconv_attend(const dconv_attend_shape *shape, const void *q, const void *k,
+                              const void *v, const int *lengths, const int *starts, void *out,
+                              float *lse, void *workspace, long long workspace_bytes, void *stream) {
+  using namespace dconv;
+  if (!shape) return DCONV_ENULL;
+  const int rc = validate(*shape);
+  if (rc != DCONV_OK) return rc;
+  if (shape->B == 0 || shape->Tq == 0) return DCONV_OK;
+  if (!q || !out || (shape->Tk > 0 && (!k || !v))) return DCONV_ENULL;
+  const int64_t need = forward_workspace(*shape);
+  if (need > 0 && !workspace) return DCONV_ENULL;
+  if (workspace_bytes < need) return DCONV_EWORKSPACE;
+  AttendPtrs p = {};
+  p.q = q;
+  p.k = k;
+  p.v = v;
+  p.lengths = lengths;
+  p.starts = starts;
+  p.o = out;
+  p.lse_out = lse;
+  (void)hipGetLastError();  // report this launch only
+  by_type(shape->dtype, [&](auto *t) {
+    rows<std::remove_pointer_t<decltype(t)>, 0>(*shape, p, (hipStream_t)stream);
+  });
+  return hipGetLastError() == hipSuccess ? DCONV_OK : DCONV_EHIP;
+}
+
+DCONV_EXPORT int dconv_attend_backward(const dconv_attend_shape *shape, const void *dout,
+                                       const void *q, const void *k, const void *v, const void *out,
+                                       const float *lse, const int *lengths, const int *starts,
+                                       void *dq, void *dk, void *dv, void *workspace,
+                                       long long workspace_bytes, void *stream) {
+  using namespace dconv;
+  if (!shape) return DCONV_ENULL;
+  const int rc = validate(*shape);
+  if (rc != DCONV_OK) return rc;
+  if (shape->B == 0) return DCONV_OK;
+  if (shape->Tq > 0 && (!dout || !q || !out || !lse || !dq)) return DCONV_ENULL;
+  if (shape->Tk > 0 && (!k || !v || !dk || !dv)) return DCONV_ENULL;
+  const int64_t need = backward_workspace(*shape);
+  if (need > 0 && !workspace) return DCONV_ENULL;
+  if (workspace_bytes < need) return DCONV_EWORKSPACE;
+  AttendPtrs p = {};
+  p.q = q;
+  p.k = k;
+  p.v = v;
+  p.out = out;
+  p.dout = dout;
+  p.lse = lse;
+  p.lengths = lengths;
+  p.starts = starts;
+  p.dq = dq;
+  p.dk = dk;
+  p.dv = dv;
+  (void)hipGetLastError();  // report this launch only
+  by_type(shape->dtype, [&](auto *t) {
+    using T = std::remove_pointer_t<decltype(t)>;
+    rows<T, 1>(*shape, p, (hipStream_t)stream);
+    rows<T, 2>(*shape, p, (hipStream_t)stream);
+  });
+  return hipGetLastError() == hipSuccess ? DCONV_OK : DCONV_EHIP;
+}

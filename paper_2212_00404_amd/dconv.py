@@ -25,6 +25,7 @@ EINVAL = -2
 ERANGE = -3
 EHIP = -4
 EUNSUPPORTED = -5
+EWORKSPACE = -6
 
 VARIANT_AUTO = 0
 VARIANT_VALU = 1
@@ -36,7 +37,10 @@ EXPORTED = ("dconv_single", "dconv_single_variant", "dconv_multi", "dconv_multi_
             "dconv_plan_single_candidates", "dconv_single_with_plan", "dconv_plan_multi",
             "dconv_plan_multi_candidates", "dconv_multi_with_plan", "dconv_model_latency",
             "dconv_model_single", "dconv_model_multi", "dconv_plan_multi_paper",
-            "dconv_plan_single_paper", "dconv_probe_latency")
+            "dconv_plan_single_paper", "dconv_probe_latency", "dconv_rotate", "dconv_join",
+            "dconv_join_workspace", "dconv_join_backward", "dconv_attend",
+            "dconv_attend_workspace", "dconv_attend_backward",
+            "dconv_attend_backward_workspace")
 
 
 class Plan(ctypes.Structure):
@@ -161,6 +165,18 @@ def load(path: str | None = None):
     lib.dconv_plan_single_paper.restype = i
     lib.dconv_probe_latency.argtypes = [vp, i, vp, vp]
     lib.dconv_probe_latency.restype = i
+    ll, size = ctypes.c_longlong, ctypes.POINTER(ctypes.c_longlong)
+    lib.dconv_rotate.argtypes = [vp] * 7
+    lib.dconv_join.argtypes = [vp] * 11
+    lib.dconv_join_workspace.argtypes = [vp, size]
+    lib.dconv_join_backward.argtypes = [vp] * 16 + [ll, vp]
+    lib.dconv_attend.argtypes = [vp] * 9 + [ll, vp]
+    lib.dconv_attend_workspace.argtypes = [vp, size]
+    lib.dconv_attend_backward.argtypes = [vp] * 13 + [ll, vp]
+    lib.dconv_attend_backward_workspace.argtypes = [vp, size]
+    for name in ("rotate", "join", "join_workspace", "join_backward", "attend", "attend_workspace",
+                 "attend_backward", "attend_backward_workspace"):
+        getattr(lib, "dconv_" + name).restype = i
     if path is None:
         _lib = lib
     return lib

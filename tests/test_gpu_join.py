@@ -1,0 +1,259 @@
+"""GPU: the norms before and after a block with its gate, scales and residual
+sum, and their gradients, against the formula in 64 bits."""
+import math
+
+import pytest
+import torch
+
+import paper_2212_00404_amd as dc
+import token_ref as ref
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+PAIRS = [(torch.float32, torch.float32), (torch.float16, torch.float16), (torch.bfloat16, torch.bfloat16),
+         (torch.float16, torch.float32), (torch.bfloat16, torch.float32)]
+PAIR_IDS = ["f32", "f16", "bf16", "f16-f32", "bf16-f32"]
+VECTORS = ("post_weight", "gate", "pre_weight", "pre_bias")
+
+
+def make(seed, dt, vt, B, T, D, norm, post, per, vectors=VECTORS):
+    g = torch.Generator().manual_seed(seed)
+    def normal(*s, mean=0.0, std=1.0, to=dt):
+        return (torch.randn(s, generator=g) * std + mean).to(to).to(DEV)
+    st = dict(branch=normal(B, T, D, std=0.7), x=normal(B, T, D, mean=0.1, std=1.5))
+    for n in VECTORS:
+        lead = (B,) if per and n != "post_weight" else ()
+        v = normal(*lead, D, mean=0.0 if n == "pre_bias" else 0.8, std=0.3, to=vt)
+        st[n] = v if n in vectors and (post or n != "post_weight") else None
+    how = dict(norm=norm, post=post, residual_scale=0.9, branch_scale=0.5, eps=1e-5)
+    return st, normal(B, T, D), normal(B, T, D), how
+
+
+def reference(st, dh, dy, how, pre=True):
+    """Outputs, gradients and their bounds.
+
+    fp32 sums of D terms lose at most D units of the sum of magnitudes; means and
+    square roots carry that on relative to the row's size, so what a row's values
+    are multiples of is its root mean square; the tensors' rounding comes on top.
+    The gradients' rows are bounded by the largest magnitude likewise, of the row
+    and of what a norm's gradient is the difference of (dn / deviation: with one
+    value in a row it cancels but for eps); the vectors' sums over N rows by N
+    units of the sum of magnitudes of their terms and the error of those."""
+    d = {n: t.cpu().double().requires_grad_() for n, t in st.items() if t is not None}
+    kw = dict(how)
+    h, y = ref.join(d.get("branch"), d["x"], norm_kind=kw.pop("norm"), pre=pre,
+                    **{n: d.get(n) for n in VECTORS}, **kw)
+    outs, seeds = [], []
+    for o, s in ((h, dh), (y, dy)):
+        if o is not None and s is not None:
+            outs.append(o)
+            seeds.append(s.cpu().double())
+    grads = dict(zip(d, torch.autograd.grad(outs, list(d.values()), seeds, allow_unused=True)))
+    grads = {n: torch.zeros_like(d[n]) if t is None else t for n, t in grads.items()}
+    return h.detach(), None if y is None else y.detach(), grads
+
+
+def before_cancelling(st, dy, how, wh, wg):
+    """The largest magnitude in a row of what the two norms' gradients are
+    differences of, for dx and dbranch."""
+    per = (lambda v: 1.0 if v is None else v.cpu().double()[:, None] if v.dim() == 2 else v.cpu().double())
+    def deviation(z):
+        if how["norm"] == "layer":
+            z = z - z.mean(-1, keepdim=True)
+        return torch.sqrt((z * z).mean(-1, keepdim=True) + how["eps"])
+    top = (lambda t: t.abs().amax(-1, keepdim=True))
+    big_x = torch.zeros(())
+    if dy is not None:
+        big_x = top(dy.cpu().double() * per(st["pre_weight"])) / deviation(wh)
+    if st["branch"] is None:
+        return big_x, None
+    gain = how["branch_scale"] * per(st["gate"]) * per(st["post_weight"]) + torch.zeros_like(wh)
+    big_b = top(gain) * (top(wg["x"]) / how["residual_scale"] + big_x)
+    if how["post"]:
+        big_b = big_b / deviation(st["branch"].cpu().double())
+    return big_x, big_b
+
+
+def row_tol(want, dt, D, extra=0.0):
+    big = want.abs().amax(-1, keepdim=True) + extra
+    return 2 * ref.UNIT[dt] * want.abs() + (math.sqrt(D) + 16) * 2.0 ** -23 * big + ref.TINY[dt]
+
+
+def compare(st, dh, dy, how, pre=True):
+    dt = st["x"].dtype
+    D = st["x"].shape[-1]
+    how_f = dict(how, **{n: st[n] for n in VECTORS})
+    h, y, stats = dc.join(st["branch"], st["x"], pre=pre, return_stats=True, **how_f)
+    grads = dc.join_backward(dh, dy if pre else None, st["branch"], st["x"], stats, **how_f)
+    wh, wy, wg = reference(st, dh, dy if pre else None, how, pre)
+    if st["branch"] is not None:
+        ref.check(h, wh, row_tol(wh, dt, D), "h")
+    else:
+        assert h is None
+    if pre:
+        ref.check(y, wy, row_tol(wy, dt, D), "y")
+    assert set(grads) == {n for n in st if st[n] is not None}
+    big_x, big_b = before_cancelling(st, dy if pre else None, how, wh, wg)
+    for n, big in (("branch", big_b), ("x", big_x)):
+        if n in grads:
+            ref.check(grads[n], wg[n], row_tol(wg[n], dt, D, big), "d" + n)
+    # sums over rows: every term is bounded by its row's largest values
+    N = st["x"].shape[0] * st["x"].shape[1]
+    for n in VECTORS:
+        if n not in grads:
+            continue
+        gt = wg[n]
+        size = max(1.0, gt.abs().max().item())
+        rows = N if st[n].dim() == 1 else st["x"].shape[1]
+        tol = 2 * ref.UNIT[st[n].dtype] * gt.abs() + \
+            (math.sqrt(D) + 16 + math.sqrt(rows)) * 2.0 ** -23 * math.sqrt(rows) * 8 * size
+        ref.check(grads[n], gt, tol, "d" + n)
+    return h, y, grads
+
+
+# (B, T, D): one value to rows longer than a workgroup, odd and even
+SIZES = [(1, 1, 1), (2, 3, 7), (1, 5, 64), (3, 17, 65), (2, 40, 192), (2, 33, 512), (1, 9, 1000),
+         (1, 130, 96), (1, 4, 4096), (2, 3, 5001), (1, 2, 16384), (1, 2, 16383), (1, 700, 256)]
+
+
+@pytest.mark.parametrize("types", PAIRS, ids=PAIR_IDS)
+@pytest.mark.parametrize("size", SIZES, ids=[str(s) for s in SIZES])
+@pytest.mark.parametrize("norm, post, per", [("rms", True, False), ("layer", True, True), ("rms", False, True),
+                                             ("layer", False, False)])
+def test_join(size, types, norm, post, per):
+    if norm == "layer" and size[2] == 1:
+        pytest.skip("one value less its mean is 0")
+    compare(*make(1, *types, *size, norm, post, per))
+
+
+@pytest.mark.parametrize("vectors", [(), ("gate",), ("post_weight", "pre_weight"), ("pre_bias",)])
+def test_vectors_left_out(vectors):
+    compare(*make(2, torch.float32, torch.float32, 2, 9, 200, "layer", True, False, vectors))
+    compare(*make(2, torch.bfloat16, torch.float32, 2, 9, 200, "rms", True, True, vectors))
+
+
+@pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+def test_first_and_last(dt):
+    """The norm before the first block (no branch) and after the last one (no
+    second norm); gradients that arrive at one output only."""
+    st, dh, dy, how = make(3, dt, dt, 2, 21, 320, "rms", True, False)
+    first = dict(st, branch=None, gate=None, post_weight=None)
+    compare(first, dh, dy, dict(how, post=False))
+    compare(first, None, dy, dict(how, post=False))
+    last = dict(st, pre_weight=None, pre_bias=None)
+    compare(last, dh, dy, how, pre=False)
+    compare(st, None, dy, how)
+    compare(st, dh, None, how)
+
+
+def test_strides_and_alignment():
+    """Rows of a longer sequence (a first token left out) and rows off 16-byte
+    boundaries: the values of the contiguous call."""
+    for dt in (torch.float32, torch.bfloat16):
+        for D, lead, width in ((256, 0, 256), (256, 1, 259), (256, 8, 272)):
+            st, dh, dy, how = make(4, dt, dt, 2, 10, D, "layer", True, True)
+            def inside(t):
+                big = torch.full((2, 12, width), float("nan"), dtype=dt, device=DEV)
+                big[:, 1:11, lead:lead + D] = t
+                return big[:, 1:11, lead:lead + D]
+            moved = dict(st, branch=inside(st["branch"]), x=inside(st["x"]))
+            compare(moved, inside(dh), inside(dy), how)
+
+
+def test_rows_of_zeros_and_constants():
+    """A row of zeros is divided by sqrt(eps) only; a constant row has no variance;
+    neither gives NaN, forward or backward."""
+    st, dh, dy, how = make(5, torch.float32, torch.float32, 1, 4, 300, "layer", True, False)
+    st["branch"][0, 0] = 0
+    st["x"][0, 0] = 0
+    st["branch"][0, 1] = 2.5
+    h, y, grads = compare(st, dh, dy, how)
+    st, dh, dy, how = make(5, torch.bfloat16, torch.bfloat16, 1, 4, 300, "rms", True, False)
+    st["branch"][0, 0] = 0
+    st["x"][0, 0] = 0
+    compare(st, dh, dy, how)
+
+
+def test_large_mean_and_special_values():
+    """A mean of a thousand times the deviation does not cancel (the variance is
+    taken about the mean); NaN and infinities stay in their row."""
+    st, dh, dy, how = make(6, torch.float32, torch.float32, 1, 6, 512, "layer", False, False)
+    st["x"] = st["x"] * 0.01 + 10.0
+    st["branch"] = st["branch"] * 0.01
+    how_f = dict(how, **{n: st[n] for n in VECTORS})
+    _, y = dc.join(st["branch"], st["x"], **how_f)
+    _, wy, _ = reference(st, dh, dy, how)
+    ref.check(y, wy, 2e-4 * wy.abs().amax(-1, keepdim=True), "y")   # 1000 * 2^-23 of the row's size, once
+    clean = dc.join(st["branch"], st["x"], **how_f)
+    bad = st["x"].clone()
+    bad[0, 2, 5], bad[0, 4, 7] = math.nan, math.inf
+    got = dc.join(st["branch"], bad, **how_f)
+    for a, b in zip(clean, got):
+        for t in (0, 1, 3, 5):
+            assert torch.equal(a[0, t], b[0, t])
+        assert b[0, 2].isnan().any()
+
+
+def test_no_rows():
+    st, dh, dy, how = make(7, torch.float32, torch.float32, 2, 3, 16, "rms", True, False)
+    empty = {n: (t[:0] if n in ("branch", "x") else t) for n, t in st.items()}
+    how_f = dict(how, **{n: st[n] for n in VECTORS})
+    h, y, stats = dc.join(empty["branch"], empty["x"], return_stats=True, **how_f)
+    grads = dc.join_backward(dh[:0], dy[:0], empty["branch"], empty["x"], stats, **how_f)
+    assert h.shape == (0, 3, 16) and all((grads[n] == 0).all() for n in VECTORS)
+
+
+def test_many_rows():
+    """More rows than workgroups, both for whole-batch and for per-sequence
+    vectors."""
+    compare(*make(8, torch.bfloat16, torch.float32, 3, 2011, 128, "rms", True, True))
+    compare(*make(8, torch.float32, torch.float32, 2, 3001, 72, "layer", True, False))
+
+
+def test_equal_calls_streams_and_graph():
+    st, dh, dy, how = make(9, torch.bfloat16, torch.float32, 2, 600, 512, "rms", True, True)
+    how_f = dict(how, **{n: st[n] for n in VECTORS})
+
+    def both():
+        h, y, stats = dc.join(st["branch"], st["x"], return_stats=True, **how_f)
+        g = dc.join_backward(dh, dy, st["branch"], st["x"], stats, **how_f)
+        return [h, y, stats] + [g[n] for n in sorted(g)]
+    want = both()
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        got = both()
+    torch.cuda.synchronize()
+    for a, b in zip(want, got):
+        assert torch.equal(a, b)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        captured = both()
+    for i in range(3):
+        st["x"].copy_(torch.randn_like(st["x"]))
+        dy.copy_(torch.randn_like(dy))
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(both(), captured):
+            assert torch.equal(a, b)
+
+
+def test_gradients_against_differences():
+    st, dh, dy, how = make(10, torch.float32, torch.float32, 2, 5, 40, "layer", True, True)
+    how_f = dict(how, **{n: st[n] for n in VECTORS})
+    _, _, stats = dc.join(st["branch"], st["x"], return_stats=True, **how_f)
+    grads = dc.join_backward(dh, dy, st["branch"], st["x"], stats, **how_f)
+    base = {n: t.cpu().double() for n, t in st.items()}
+    g = torch.Generator().manual_seed(11)
+    for n in base:
+        d = torch.randn(base[n].shape, generator=g, dtype=torch.float64)
+
+        def f(sign):
+            v = dict(base)
+            v[n] = v[n] + sign * 1e-4 * d
+            kw = dict(how)
+            h, y = ref.join(v["branch"], v["x"], norm_kind=kw.pop("norm"), **{m: v[m] for m in VECTORS}, **kw)
+            return (h * dh.cpu().double()).sum() + (y * dy.cpu().double()).sum()
+        want = (f(1) - f(-1)) / 2e-4
+        terms = grads[n].cpu().double() * d
+        assert abs(terms.sum() - want) <= 1e-5 * terms.abs().sum() + 1e-6, n
