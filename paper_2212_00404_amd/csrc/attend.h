@@ -182,4 +182,20 @@ __device__ void attend_row_dkv(const dconv_attend_shape &sh, const AttendPtrs &p
     }
 }
 
+// How a forward call runs: `few` rows with the keys divided over waves and
+// `splits` workgroups (attend_split), else 128 rows per workgroup
+// (attend_tiles).
+struct ForwardPlan {
+  bool few, direct;
+  int dp;              // head size the kernels are built for
+  int tiles, splits;   // tiles of rows per key head, parts of the keys
+  int64_t workspace;   // bytes
+};
+constexpr int attend_part_floats(int dp) { return 32 * (2 + dp); }
+
+// Instantiated in attend_f32.hip, attend_f16.hip and attend_bf16.hip.
+template <class T>
+void launch_attend(const dconv_attend_shape &sh, const AttendPtrs &p, const ForwardPlan &plan, float *workspace,
+                   hipStream_t s);
+
 }  // namespace dconv

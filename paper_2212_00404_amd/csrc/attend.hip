@@ -17,7 +17,6 @@ __global__ __launch_bounds__(256) void attend_rows(const dconv_attend_shape sh, 
   const int64_t i = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
   if (i >= n) return;
   const int t = (int)(i % T_), h = (int)(i / T_ % heads), b = (int)(i / T_ / heads);
-  if constexpr (KIND == 0) attend_row<T>(sh, p, b, h, t);
   if constexpr (KIND == 1) attend_row_dq<T>(sh, p, b, h, t);
   if constexpr (KIND == 2) attend_row_dkv<T>(sh, p, b, h, t);
 }
@@ -50,7 +49,47 @@ int validate(const dconv_attend_shape &sh) {
   return DCONV_OK;
 }
 
-int64_t forward_workspace(const dconv_attend_shape &) { return 0; }
+// Rows in memory as whole 16-byte pieces on 4-byte boundaries (what the copies
+// into LDS need).
+bool whole_pieces(const void *p, const long long *stride, const dconv_attend_shape &sh) {
+  const int es = element_size(sh.dtype), unit = 4 / es;
+  return sh.D * es % 16 == 0 && (uintptr_t)p % 4 == 0 && stride[0] % unit == 0 && stride[1] % unit == 0 &&
+         stride[2] % unit == 0;
+}
+
+int padded_head(int D) { return D <= 32 ? 32 : D <= 64 ? 64 : D <= 96 ? 96 : D <= 128 ? 128 : 256; }
+
+// The most keys that a tile of `queries` queries sees (lengths are on the device).
+int64_t most_keys(const dconv_attend_shape &sh, int queries) {
+  int64_t n = sh.Tk;
+  if (sh.left >= 0 && sh.right >= 0) {
+    const int64_t window = (int64_t)sh.left + sh.right + queries + sh.sinks;
+    if (window < n) n = window;
+  }
+  return n;
+}
+
+ForwardPlan plan_forward(const dconv_attend_shape &sh) {
+  ForwardPlan f = {};
+  f.dp = padded_head(sh.D);
+  const int64_t rows = (int64_t)sh.Tq * (sh.Hq / sh.Hkv), heads = (int64_t)sh.B * sh.Hkv;
+  f.few = heads * ((rows + 127) / 128) < 128;
+  f.tiles = (int)(f.few ? (rows + 31) / 32 : (rows + 127) / 128);
+  f.splits = 1;
+  if (f.few) {
+    const int waves = f.dp * element_size(sh.dtype) <= 256 ? 4 : f.dp * element_size(sh.dtype) <= 512 ? 2 : 1;
+    const int64_t groups = heads * f.tiles, room = (256 + groups - 1) / groups;
+    const int64_t tiles = (most_keys(sh, 32) + 32 * waves - 1) / (32 * waves);
+    f.splits = (int)(room < tiles ? room : tiles);
+    if (f.splits < 1) f.splits = 1;
+    if (f.splits > 1) f.workspace = groups * f.splits * attend_part_floats(f.dp) * 4;
+  }
+  return f;
+}
+
+int64_t forward_workspace(const dconv_attend_shape &sh) {
+  return sh.B == 0 || sh.Tq == 0 ? 0 : plan_forward(sh).workspace;
+}
 int64_t backward_workspace(const dconv_attend_shape &) { return 0; }
 
 }  // namespace
@@ -90,9 +129,12 @@ DCONV_EXPORT int dconv_attend(const dconv_attend_shape *shape, const void *q, co
   p.starts = starts;
   p.o = out;
   p.lse_out = lse;
+  ForwardPlan plan = plan_forward(*shape);
+  plan.direct = whole_pieces(q, shape->q_stride, *shape) && whole_pieces(k, shape->k_stride, *shape) &&
+                whole_pieces(v, shape->v_stride, *shape) && whole_pieces(out, shape->out_stride, *shape);
   (void)hipGetLastError();  // report this launch only
   by_type(shape->dtype, [&](auto *t) {
-    rows<std::remove_pointer_t<decltype(t)>, 0>(*shape, p, (hipStream_t)stream);
+    launch_attend<std::remove_pointer_t<decltype(t)>>(*shape, p, plan, (float *)workspace, (hipStream_t)stream);
   });
   return hipGetLastError() == hipSuccess ? DCONV_OK : DCONV_EHIP;
 }

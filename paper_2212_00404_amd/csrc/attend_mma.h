@@ -1,0 +1,598 @@
+// Windowed attention on the matrix cores: fragments, tiles in LDS and the two
+// forward kernels.  Instantiated per type in attend_*.hip.
+//
+// All products are 32 x 32 tiles.  Scores are computed transposed, keys along
+// the rows of the tile and queries along its columns: a lane then holds half
+// of one query's scores (the other half is 32 lanes away), so the maximum, the
+// sum and the rescaling of the softmax are register arithmetic, and the
+// probabilities already stand where the next product, values transposed times
+// probabilities, takes its second operand from (see Mma).
+#pragma once
+
+#include "attend.h"
+
+namespace dconv {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef __attribute__((address_space(3))) void *lds_ptr;
+
+// 32 x 32 += (32 x 16) (16 x 32).  Operands: lane l holds row (column) l % 32
+// and eight of the 16 inner indices, group l / 32.  Result: register i of lane
+// l is column l % 32, row acc_row(i, l / 32) = 8 (i / 4) + 4 (l / 32) + i % 4.
+// The inner index has no order of its own: eight result registers 8 s .. 8 s + 7
+// serve as a second operand whose inner indices are the rows
+// 16 s + 8 (e / 4) + 4 (l / 32) + e % 4, if the first operand is read by the
+// same rows (Tile::column).
+// fp32 takes eight 32 x 32 x 2 instructions, one per element of the fragment.
+template <class T>
+struct Mma;
+template <>
+struct Mma<bf16_t> {
+  typedef bf16_t Frag __attribute__((ext_vector_type(8)));
+  static __device__ __forceinline__ f32x16 mac(Frag a, Frag b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+  }
+};
+template <>
+struct Mma<f16_t> {
+  typedef f16_t Frag __attribute__((ext_vector_type(8)));
+  static __device__ __forceinline__ f32x16 mac(Frag a, Frag b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+  }
+};
+template <>
+struct Mma<float> {
+  typedef float Frag __attribute__((ext_vector_type(8)));
+  static __device__ __forceinline__ f32x16 mac(Frag a, Frag b, f32x16 c) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[e], b[e], c, 0, 0, 0);
+    return c;
+  }
+};
+
+__device__ __forceinline__ constexpr int acc_row(int i, int half) { return 8 * (i / 4) + 4 * half + i % 4; }
+
+// Registers 8 s .. 8 s + 7 of a result as an operand.
+template <class T>
+__device__ __forceinline__ typename Mma<T>::Frag as_operand(const f32x16 &c, int s) {
+  typename Mma<T>::Frag f;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) f[e] = from_f32<T>(c[8 * s + e]);
+  return f;
+}
+
+// Rows of DP elements in LDS, in chunks of eight elements that are permuted
+// within a row by an exclusive or, so that eight consecutive rows of one chunk
+// (a row operand), and four rows of two neighbouring chunks (a column operand),
+// lie on different banks.
+template <class T, int DP>
+struct Tile {
+  typedef typename Mma<T>::Frag Frag;
+  static constexpr int kChunks = DP / 8;
+  static __device__ __forceinline__ int swizzle(int row) {
+    if constexpr (sizeof(T) == 4) return DP % 64 == 0 ? row & 7 : row & 3;
+    // rows of a multiple of 128 bytes: all three low bits; rows that alternate
+    // between the halves of 128 bytes: two bits
+    return DP % 64 == 0 ? ((row & 3) << 1) | ((row >> 2) & 1) : (row & 2) | ((row >> 2) & 1);
+  }
+  static __device__ __forceinline__ int at(int row, int chunk) { return row * DP + (chunk ^ swizzle(row)) * 8; }
+
+  // Elements 16 s + 8 (l / 32) .. + 7 of row r0 + l % 32.
+  static __device__ __forceinline__ Frag row(const T *t, int r0, int s, int lane) {
+    return *reinterpret_cast<const Frag *>(t + at(r0 + (lane & 31), 2 * s + (lane >> 5)));
+  }
+  // Column 32 c + l % 32 of the rows r0 + 8 (e / 4) + 4 (l / 32) + e % 4
+  // (r0 a multiple of 16).
+  static __device__ __forceinline__ Frag column(const T *t, int r0, int c, int lane) {
+    Frag f;
+    if constexpr (sizeof(T) == 2) {
+      // a 16-lane group reads four rows of 16 elements, a lane four of a row,
+      // and gets four rows of one column
+      typedef short s16x4 __attribute__((ext_vector_type(4)));
+      typedef __attribute__((address_space(3))) s16x4 *lds_s16x4;
+      const int r = r0 + 4 * (lane >> 5) + ((lane & 15) >> 2);
+      const int chunk = 4 * c + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+      s16x4 v[2];
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+        v[j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+            (lds_s16x4)(t + at(r + 8 * j, chunk) + 4 * (lane & 1)));
+      __builtin_memcpy(&f, v, 16);
+    } else {
+      const int d = 32 * c + (lane & 31);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) f[e] = t[at(r0 + 8 * (e / 4) + 4 * (lane >> 5) + e % 4, d >> 3) + (d & 7)];
+    }
+    return f;
+  }
+
+  // NR rows of D elements from row_start(r) into LDS by the NT threads of a
+  // workgroup or wave (`me`: the thread's number).  direct: the rows are whole
+  // 16-byte pieces on 4-byte boundaries, copied without a register; a piece past
+  // D repeats the row's first (its products meet zeros).  Otherwise element by
+  // element, zeros past D.
+  template <int NR, int NT, class F>
+  static __device__ __forceinline__ void stage(T *lds, int D, bool direct, int me, F row_start) {
+    constexpr int kPer = 16 / sizeof(T), kPieces = DP / kPer;
+    if (direct) {
+      static_assert(NR * kPieces % NT == 0, "whole copies");
+#pragma unroll
+      for (int i = 0; i < NR * kPieces / NT; ++i) {
+        const int slot = i * NT + me, r = slot / kPieces, piece = slot % kPieces;
+        int e = ((piece * kPer / 8) ^ swizzle(r)) * 8 + piece * kPer % 8;
+        e = e < D ? e : 0;
+        // the wave's part of LDS is contiguous: lane l lands 16 l bytes on
+        __builtin_amdgcn_global_load_lds(row_start(r) + e, (lds_ptr)(lds + (i * NT + (me & ~63)) * kPer), 16,
+                                         0, 0);
+      }
+    } else {
+      for (int x = me; x < NR * DP; x += NT) {
+        const int r = x / DP, d = x % DP;
+        lds[at(r, d >> 3) + (d & 7)] = d < D ? row_start(r)[d] : from_f32<T>(0.0f);
+      }
+    }
+  }
+};
+
+// Eight elements of a row in memory from d on, times `sign`; zeros past D.
+template <class T>
+__device__ __forceinline__ typename Mma<T>::Frag load_frag(const T *row, int d, int D, bool direct, float sign) {
+  typename Mma<T>::Frag f;
+  if (direct && d + 8 <= D) {
+    __builtin_memcpy(&f, __builtin_assume_aligned(row + d, 4), sizeof(f));
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f[e] = d + e < D ? row[d + e] : from_f32<T>(0.0f);
+  }
+  if (sign != 1.0f) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f[e] = from_f32<T>(to_f32(f[e]) * sign);
+  }
+  return f;
+}
+
+// The other half of a query's lanes, 32 away.
+__device__ __forceinline__ float half_max(float x) { return fmaxf(x, __shfl_xor(x, 32)); }
+__device__ __forceinline__ float half_sum(float x) { return x + __shfl_xor(x, 32); }
+
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
+// What the host hands to the tile kernels beside the shape.
+struct AttendTile {
+  float scale2;   // |scale| / ln 2: the softmax is taken in powers of two
+  float sign;     // of the scale, taken into the queries; 0: every score is 0
+  bool direct;    // rows can be copied in 16-byte pieces
+  int tiles;      // tiles of rows per key head
+  int splits;     // parts of the keys (attend_split)
+  float *partial; // their sums
+};
+
+// Rows of a group: row r of key head hk is query r / G of head hk * G + r % G, so
+// that the heads that share keys share the tiles of them.  The keys that any row
+// of a tile sees are numbered v = 0 .. n - 1: the first keys, then the window.
+struct Keys {
+  int n, first, off;
+  __device__ __forceinline__ int key(int v) const { return v < first ? v : v + off; }
+};
+__device__ __forceinline__ Keys keys_of(const dconv_attend_shape &sh, const Seq &s, int t0, int t1) {
+  Keys k = {0, 0, 0};
+  if (s.start + t1 < 0) return k;
+  const Span a = span_of(sh, s, max((int64_t)0, s.start + t0)), b = span_of(sh, s, s.start + t1);
+  k.first = a.first;
+  k.off = a.lo - a.first;
+  k.n = b.hi - k.off;
+  return k;
+}
+// Row at position i sees v < hi with v >= lo or v < sinks.
+struct RowKeys {
+  int lo, hi;
+  bool none;
+};
+__device__ __forceinline__ RowKeys row_keys(const dconv_attend_shape &sh, const Seq &s, const Keys &k, int64_t i) {
+  const Span a = span_of(sh, s, i);
+  RowKeys r;
+  r.none = a.hi - a.lo + a.first == 0;
+  r.lo = a.lo - k.off;
+  r.hi = r.none ? 0 : a.hi - k.off;
+  return r;
+}
+
+// The running softmax of 32 rows by one wave: each lane half of a row.
+template <class T, int DP>
+struct Softmax {
+  static constexpr int KS = DP / 16, DT = DP / 32;
+  typedef typename Mma<T>::Frag Frag;
+  f32x16 o[DT];   // o[c][i]: column 32 c + acc_row(i, half) of the row
+  float m, l;     // base of the exponentials (in powers of two), this lane's sum
+
+  __device__ __forceinline__ void clear() {
+    for (int c = 0; c < DT; ++c) o[c] = f32x16{};
+    m = -INFINITY;
+    l = 0.0f;
+  }
+
+  // Adds 32 * HB keys v0 .. of the tiles ks, vs.
+  template <int HB>
+  __device__ __forceinline__ void add(const T *ks, const T *vs, const Frag (&q)[KS], int v0, const RowKeys &see,
+                                      int sinks, float scale2, bool masked, int lane) {
+    f32x16 s[HB];
+#pragma unroll
+    for (int hb = 0; hb < HB; ++hb) {
+      s[hb] = f32x16{};
+#pragma unroll
+      for (int k = 0; k < KS; ++k) s[hb] = Mma<T>::mac(Tile<T, DP>::row(ks, 32 * hb, k, lane), q[k], s[hb]);
+    }
+    if (masked) {
+#pragma unroll
+      for (int hb = 0; hb < HB; ++hb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int v = v0 + 32 * hb + acc_row(i, lane >> 5);
+          const bool on = v < see.hi && (v >= see.lo || v < sinks);
+          s[hb][i] = on ? s[hb][i] : -INFINITY;
+        }
+    }
+    float top = s[0][0];
+#pragma unroll
+    for (int hb = 0; hb < HB; ++hb)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) top = fmaxf(top, s[hb][i]);
+    top = half_max(top) * scale2;
+    // The base follows the maximum only when it is left behind by more than
+    // 2^8: sums and probabilities stay below 2^8 times their true size, and the
+    // rescaling of the result is rare.
+    if (__any(top - m > 8.0f)) {
+      const float to = fmaxf(m, top);
+      const float keep = to == -INFINITY ? 1.0f : exp2f(m - to);
+#pragma unroll
+      for (int c = 0; c < DT; ++c) o[c] *= keep;
+      l *= keep;
+      m = to;
+    }
+    const float base = m == -INFINITY ? 0.0f : m;
+#pragma unroll
+    for (int hb = 0; hb < HB; ++hb)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        s[hb][i] = __builtin_amdgcn_exp2f(fmaf(s[hb][i], scale2, -base));
+        l += s[hb][i];
+      }
+#pragma unroll
+    for (int hb = 0; hb < HB; ++hb)
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const Frag w = as_operand<T>(s[hb], k);
+#pragma unroll
+        for (int c = 0; c < DT; ++c)
+          o[c] = Mma<T>::mac(Tile<T, DP>::column(vs, 32 * hb + 16 * k, c, lane), w, o[c]);
+      }
+  }
+};
+
+// log(2) (m + log2(l))
+__device__ __forceinline__ float log_sum(float m, float l) { return 0.69314718055994531f * (m + log2f(l)); }
+
+template <class T>
+constexpr int forward_keys(int dp) { return dp * (int)sizeof(T) <= 256 ? 64 : 32; }
+constexpr int kForwardRows = 128;
+
+// 128 rows per workgroup, 32 per wave; tiles of BN keys and values in two LDS
+// buffers, the next one copied while the current one is used.
+template <class T, int DP>
+__global__ __launch_bounds__(256) void attend_tiles(const dconv_attend_shape sh, const AttendPtrs p,
+                                                    const AttendTile at) {
+  constexpr int BN = forward_keys<T>(DP), KS = DP / 16, DT = DP / 32;
+  __shared__ __align__(16) T buf0[2 * BN * DP];
+  __shared__ __align__(16) T buf1[2 * BN * DP];
+  DCONV_POISON(poison_lds(buf0, 2 * BN * DP); poison_lds(buf1, 2 * BN * DP));
+  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
+  const int id = xcd_remap(blockIdx.x, gridDim.x);
+  const int bh = id / at.tiles, b = bh / sh.Hkv, hk = bh % sh.Hkv, G = sh.Hq / sh.Hkv;
+  const int r0 = (id % at.tiles) * kForwardRows, rows = sh.Tq * G;
+  const Seq seq = seq_of(sh, p, b);
+  const Keys keys = keys_of(sh, seq, r0 / G, (min(r0 + kForwardRows, rows) - 1) / G);
+  const int n = uniform(keys.n);
+
+  const int r = r0 + 32 * wave + (lane & 31), rr = min(r, rows - 1);
+  const int t = rr / G, h = hk * G + rr % G;
+  const RowKeys see = row_keys(sh, seq, keys, seq.start + t);
+  // the wave's keys: none outside [from, to) but for the first ones, all visible
+  // to all rows inside [all_from, all_to)
+  int from = see.lo, to = see.hi, all_from = see.lo, all_to = see.hi;
+#pragma unroll
+  for (int x = 16; x > 0; x >>= 1) {
+    from = min(from, __shfl_xor(from, x));
+    to = max(to, __shfl_xor(to, x));
+    all_from = max(all_from, __shfl_xor(all_from, x));
+    all_to = min(all_to, __shfl_xor(all_to, x));
+  }
+  from = uniform(from), to = uniform(to), all_from = uniform(all_from), all_to = uniform(all_to);
+
+  typename Mma<T>::Frag q[KS];
+  const T *qrow = row_of<T>(p.q, sh.q_stride, b, t, h);
+#pragma unroll
+  for (int k = 0; k < KS; ++k) q[k] = load_frag(qrow, 16 * k + 8 * (lane >> 5), sh.D, at.direct, at.sign);
+
+  const T *kh = row_of<T>(p.k, sh.k_stride, b, 0, hk), *vh = row_of<T>(p.v, sh.v_stride, b, 0, hk);
+  auto stage = [&](T *buf, int v0) {
+    auto from_row = [&](const T *base, long long stride) {
+      return [=](int x) { return base + (int64_t)keys.key(min(v0 + x, n - 1)) * stride; };
+    };
+    Tile<T, DP>::template stage<BN, 256>(buf, sh.D, at.direct, threadIdx.x, from_row(kh, sh.k_stride[1]));
+    Tile<T, DP>::template stage<BN, 256>(buf + BN * DP, sh.D, at.direct, threadIdx.x,
+                                         from_row(vh, sh.v_stride[1]));
+  };
+  Softmax<T, DP> soft;
+  soft.clear();
+  auto step = [&](const T *buf, int v0) {
+    if (v0 >= to || (v0 + BN <= from && v0 >= sh.sinks)) return;
+    const bool masked = !(v0 + BN <= all_to && (v0 >= all_from || v0 + BN <= sh.sinks));
+    soft.template add<BN / 32>(buf, buf + BN * DP, q, v0, see, sh.sinks, at.scale2, masked, lane);
+  };
+  auto arrived = [&]() {
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    __syncthreads();
+  };
+  if (n > 0) stage(buf0, 0);
+  for (int v0 = 0; v0 < n; v0 += 2 * BN) {
+    arrived();
+    if (v0 + BN < n) stage(buf1, v0 + BN);
+    step(buf0, v0);
+    if (v0 + BN >= n) break;
+    arrived();
+    if (v0 + 2 * BN < n) stage(buf0, v0 + 2 * BN);
+    step(buf1, v0 + BN);
+  }
+
+  const float l = half_sum(soft.l), inv = see.none ? 0.0f : 1.0f / l;
+  bool bad = false;
+#pragma unroll
+  for (int c = 0; c < DT; ++c)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      soft.o[c][i] = see.none ? 0.0f : soft.o[c][i] * inv;
+      bad |= 32 * c + acc_row(i, lane >> 5) < sh.D && !(fabsf(soft.o[c][i]) < INFINITY);
+    }
+  const unsigned long long any = __ballot(bad && r < rows);
+  const unsigned redo = kSumAgain ? (unsigned)(any | (any >> 32)) : 0u;
+  if (r < rows && !(redo >> (lane & 31) & 1)) {
+    T *o = (T *)p.o + b * sh.out_stride[0] + t * sh.out_stride[1] + h * sh.out_stride[2];
+#pragma unroll
+    for (int c = 0; c < DT; ++c)
+#pragma unroll
+      for (int i = 0; i < 16; i += 4) {
+        const int d = 32 * c + acc_row(i, lane >> 5);
+        T x[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = from_f32<T>(soft.o[c][i + e]);
+        if (at.direct && d + 4 <= sh.D) {
+          __builtin_memcpy(__builtin_assume_aligned(o + d, 4), x, sizeof(x));
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (d + e < sh.D) o[d + e] = x[e];
+        }
+      }
+    if (p.lse_out && lane < 32)
+      p.lse_out[((int64_t)b * sh.Hq + h) * sh.Tq + t] = see.none ? -INFINITY : log_sum(soft.m, l);
+  }
+  // A row with a result that is not finite is taken again by the plain form,
+  // which reads visible keys and values only: a zero probability times an
+  // infinity or NaN that the row does not see has made a NaN here.
+  for (unsigned again = redo; again; again &= again - 1) {
+    const int x = r0 + 32 * wave + __ffs(again) - 1;
+    attend_row<T>(sh, p, b, hk * G + x % G, x / G);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Few rows: the keys divided over waves and workgroups
+// ---------------------------------------------------------------------------
+template <class T>
+constexpr int split_waves(int dp) { return dp * (int)sizeof(T) <= 256 ? 4 : dp * (int)sizeof(T) <= 512 ? 2 : 1; }
+
+// One row's parts joined: lane l gets elements l, l + 64, ... of the result.
+// part(i): {base, sum, row of unscaled results}.
+template <class T, class F>
+__device__ __forceinline__ void join_parts(const dconv_attend_shape &sh, const AttendPtrs &p, int b, int h, int t,
+                                           bool none, int parts, F part) {
+  const int lane = threadIdx.x & 63;
+  float m = -INFINITY, l = 0.0f, acc[kRowParts] = {};
+  for (int i = 0; i < parts; ++i) m = fmaxf(m, part(i).m);
+  const float base = m == -INFINITY ? 0.0f : m;
+  for (int i = 0; i < parts; ++i) {
+    const auto x = part(i);
+    const float w = exp2f(x.m - base);
+    l += w * x.l;
+#pragma unroll
+    for (int k = 0; k < kRowParts; ++k)
+      if (lane + 64 * k < sh.D) acc[k] = fmaf(w, x.o[lane + 64 * k], acc[k]);
+  }
+  bool bad = false;
+#pragma unroll
+  for (int k = 0; k < kRowParts; ++k) {
+    acc[k] = none ? 0.0f : acc[k] / l;
+    bad |= lane + 64 * k < sh.D && !(fabsf(acc[k]) < INFINITY);
+  }
+  if (kSumAgain && __any(bad)) {
+    attend_row<T>(sh, p, b, h, t);
+    return;
+  }
+  T *o = (T *)p.o + b * sh.out_stride[0] + t * sh.out_stride[1] + h * sh.out_stride[2];
+#pragma unroll
+  for (int k = 0; k < kRowParts; ++k)
+    if (lane + 64 * k < sh.D) o[lane + 64 * k] = from_f32<T>(acc[k]);
+  if (p.lse_out && lane == 0)
+    p.lse_out[((int64_t)b * sh.Hq + h) * sh.Tq + t] = none ? -INFINITY : log_sum(m, l);
+}
+
+struct Part {
+  float m, l;
+  const float *o;
+};
+
+// Floats of one part of 32 rows in the workspace: bases, sums, rows.
+template <int DP>
+constexpr int part_floats() { return attend_part_floats(DP); }
+
+// 32 rows per workgroup; wave w of part s takes tiles of 32 keys by itself, with
+// two LDS buffers of its own and no barrier.
+template <class T, int DP>
+__global__ __launch_bounds__(64 * split_waves<T>(DP)) void attend_split(const dconv_attend_shape sh,
+                                                                        const AttendPtrs p, const AttendTile at) {
+  constexpr int KS = DP / 16, DT = DP / 32, kTile = 32 * DP, W = split_waves<T>(DP);
+  __shared__ __align__(16) T buf0[W * 2 * kTile];
+  __shared__ __align__(16) T buf1[W * 2 * kTile];
+  DCONV_POISON(poison_lds(buf0, W * 2 * kTile); poison_lds(buf1, W * 2 * kTile));
+  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
+  const int part = blockIdx.x % at.splits, id = blockIdx.x / at.splits;
+  const int bh = id / at.tiles, b = bh / sh.Hkv, hk = bh % sh.Hkv, G = sh.Hq / sh.Hkv;
+  const int r0 = (id % at.tiles) * 32, rows = sh.Tq * G;
+  const Seq seq = seq_of(sh, p, b);
+  const Keys keys = keys_of(sh, seq, r0 / G, (min(r0 + 32, rows) - 1) / G);
+  const int n = uniform(keys.n);
+  const int rr = min(r0 + (lane & 31), rows - 1), t = rr / G, h = hk * G + rr % G;
+  const RowKeys see = row_keys(sh, seq, keys, seq.start + t);
+
+  typename Mma<T>::Frag q[KS];
+  const T *qrow = row_of<T>(p.q, sh.q_stride, b, t, h);
+#pragma unroll
+  for (int k = 0; k < KS; ++k) q[k] = load_frag(qrow, 16 * k + 8 * (lane >> 5), sh.D, at.direct, at.sign);
+
+  const T *kh = row_of<T>(p.k, sh.k_stride, b, 0, hk), *vh = row_of<T>(p.v, sh.v_stride, b, 0, hk);
+  auto stage = [&](T *buf, int v0) {
+    auto from_row = [&](const T *base, long long stride) {
+      return [=](int x) { return base + (int64_t)keys.key(min(v0 + x, n - 1)) * stride; };
+    };
+    T *mine = buf + wave * 2 * kTile;
+    Tile<T, DP>::template stage<32, 64>(mine, sh.D, at.direct, lane, from_row(kh, sh.k_stride[1]));
+    Tile<T, DP>::template stage<32, 64>(mine + kTile, sh.D, at.direct, lane, from_row(vh, sh.v_stride[1]));
+  };
+  Softmax<T, DP> soft;
+  soft.clear();
+  auto step = [&](const T *buf, int v0) {
+    const T *mine = buf + wave * 2 * kTile;
+    soft.template add<1>(mine, mine + kTile, q, v0, see, sh.sinks, at.scale2, true, lane);
+  };
+  auto arrived = [&]() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory"); };
+  // tiles part * W + wave, then every (splits * W)-th
+  const int stride = 32 * at.splits * W;
+  int v0 = 32 * (part * W + wave);
+  if (v0 < n) stage(buf0, v0);
+  for (; v0 < n; v0 += 2 * stride) {
+    arrived();
+    if (v0 + stride < n) stage(buf1, v0 + stride);
+    step(buf0, v0);
+    if (v0 + stride >= n) break;
+    arrived();
+    if (v0 + 2 * stride < n) stage(buf0, v0 + 2 * stride);
+    step(buf1, v0 + stride);
+  }
+  const float l = half_sum(soft.l);
+  const int half = lane >> 5;
+  // each wave's sums as rows, in LDS (its own buffers, all read)
+  constexpr int kFloats = part_floats<DP>();
+  __shared__ float ml[W][64];
+  __syncthreads();
+  // row r of wave w: DP floats; the first 16 rows in buf0, the others in buf1
+  auto lds_row = [&](int w, int r) {
+    return reinterpret_cast<float *>(r < 16 ? buf0 : buf1) + (w * 16 + (r & 15)) * DP;
+  };
+  static_assert(16 * DP * sizeof(float) <= 2 * kTile * sizeof(T), "half the rows fit a buffer");
+#pragma unroll
+  for (int c = 0; c < DT; ++c)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) lds_row(wave, lane & 31)[32 * c + acc_row(i, half)] = soft.o[c][i];
+  if (half == 0) {
+    ml[wave][lane] = soft.m;
+    ml[wave][32 + lane] = l;
+  }
+  __syncthreads();
+  for (int x = wave; x < 32 && r0 + x < rows; x += W) {
+    const int tx = (r0 + x) / G, hx = hk * G + (r0 + x) % G;
+    if (at.splits == 1) {
+      const bool none = row_keys(sh, seq, keys, seq.start + tx).none;
+      join_parts<T>(sh, p, b, hx, tx, none, W,
+                    [&](int w) { return Part{ml[w][x], ml[w][32 + x], lds_row(w, x)}; });
+      continue;
+    }
+    // the workgroup's part: the waves joined, not divided yet
+    float m = -INFINITY, sum = 0.0f;
+    for (int w = 0; w < W; ++w) m = fmaxf(m, ml[w][x]);
+    const float base = m == -INFINITY ? 0.0f : m;
+    float *out = at.partial + (int64_t)blockIdx.x * kFloats;
+    float f[W];
+    for (int w = 0; w < W; ++w) {
+      f[w] = exp2f(ml[w][x] - base);
+      sum += f[w] * ml[w][32 + x];
+    }
+    for (int d = lane; d < DP; d += 64) {
+      float o = 0.0f;
+      for (int w = 0; w < W; ++w) o = fmaf(f[w], lds_row(w, x)[d], o);
+      out[64 + x * DP + d] = o;
+    }
+    if (lane == 0) {
+      out[x] = m;
+      out[32 + x] = sum;
+    }
+  }
+}
+
+// A wave per row joins the parts that workgroups left.
+template <class T, int DP>
+__global__ __launch_bounds__(64) void attend_join(const dconv_attend_shape sh, const AttendPtrs p,
+                                                  const AttendTile at) {
+  const int G = sh.Hq / sh.Hkv, rows = sh.Tq * G;
+  const int r = blockIdx.x % rows, bh = blockIdx.x / rows, b = bh / sh.Hkv, hk = bh % sh.Hkv;
+  const Seq seq = seq_of(sh, p, b);
+  const Span see = span_of(sh, seq, seq.start + r / G);
+  const float *base = at.partial + ((int64_t)bh * at.tiles + r / 32) * at.splits * part_floats<DP>();
+  join_parts<T>(sh, p, b, hk * G + r % G, r / G, see.hi - see.lo + see.first == 0, at.splits, [&](int i) {
+    const float *x = base + (int64_t)i * part_floats<DP>();
+    return Part{x[r & 31], x[32 + (r & 31)], x + 64 + (r & 31) * DP};
+  });
+}
+
+// ---------------------------------------------------------------------------
+// Launch
+// ---------------------------------------------------------------------------
+template <class F>
+void by_width(int dp, F f) {
+  if (dp == 32) return f(std::integral_constant<int, 32>());
+  if (dp == 64) return f(std::integral_constant<int, 64>());
+  if (dp == 96) return f(std::integral_constant<int, 96>());
+  if (dp == 128) return f(std::integral_constant<int, 128>());
+  return f(std::integral_constant<int, 256>());
+}
+
+inline AttendTile attend_tile(const dconv_attend_shape &sh, bool direct) {
+  AttendTile at = {};
+  at.scale2 = sh.scale == 0.0f ? 1.0f : fabsf(sh.scale) * 1.4426950408889634f;
+  at.sign = sh.scale > 0.0f ? 1.0f : sh.scale < 0.0f ? -1.0f : 0.0f;
+  at.direct = direct;
+  return at;
+}
+
+template <class T>
+void launch_attend(const dconv_attend_shape &sh, const AttendPtrs &p, const ForwardPlan &plan, float *workspace,
+                   hipStream_t s) {
+  AttendTile at = attend_tile(sh, plan.direct);
+  at.tiles = plan.tiles;
+  at.splits = plan.splits;
+  at.partial = workspace;
+  by_width(plan.dp, [&](auto dp) {
+    constexpr int DP = decltype(dp)::value;
+    const unsigned groups = (unsigned)(sh.B * sh.Hkv * plan.tiles);
+    if (!plan.few) {
+      hipLaunchKernelGGL((attend_tiles<T, DP>), dim3(groups), dim3(256), 0, s, sh, p, at);
+      return;
+    }
+    hipLaunchKernelGGL((attend_split<T, DP>), dim3(groups * plan.splits), dim3(64 * split_waves<T>(DP)), 0, s,
+                       sh, p, at);
+    if (plan.splits > 1)
+      hipLaunchKernelGGL((attend_join<T, DP>), dim3((unsigned)((int64_t)sh.B * sh.Hq * sh.Tq)), dim3(64), 0, s,
+                         sh, p, at);
+  });
+}
+
+}  // namespace dconv
