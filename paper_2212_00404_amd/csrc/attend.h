@@ -198,4 +198,20 @@ template <class T>
 void launch_attend(const dconv_attend_shape &sh, const AttendPtrs &p, const ForwardPlan &plan, float *workspace,
                    hipStream_t s);
 
+// How a backward call runs (head sizes up to 128): dq by tiles of 128 rows; dk
+// and dv of the keys [0, first) by tiles of 32 with the rows divided
+// (attend_dkv_split), of the others by tiles of 128 (attend_dkv).
+constexpr int kGradMaxD = 128;
+struct BackwardPlan {
+  bool direct;
+  int dp;
+  int row_tiles, key_tiles;
+  int first, first_tiles, parts;
+  int64_t stats_bytes, workspace;
+};
+// Instantiated in attend_grad_f32.hip, attend_grad_f16.hip and attend_grad_bf16.hip.
+template <class T>
+void launch_attend_grad(const dconv_attend_shape &sh, const AttendPtrs &p, const BackwardPlan &plan, void *workspace,
+                        hipStream_t s);
+
 }  // namespace dconv

@@ -90,7 +90,33 @@ ForwardPlan plan_forward(const dconv_attend_shape &sh) {
 int64_t forward_workspace(const dconv_attend_shape &sh) {
   return sh.B == 0 || sh.Tq == 0 ? 0 : plan_forward(sh).workspace;
 }
-int64_t backward_workspace(const dconv_attend_shape &) { return 0; }
+BackwardPlan plan_backward(const dconv_attend_shape &sh) {
+  BackwardPlan f = {};
+  f.dp = padded_head(sh.D);
+  const int G = sh.Hq / sh.Hkv;
+  const int64_t rows = (int64_t)sh.Tq * G, heads = (int64_t)sh.B * sh.Hkv;
+  f.row_tiles = (int)((rows + 127) / 128);
+  f.key_tiles = (sh.Tk + 127) / 128;
+  // the keys that every row sees, where the others are seen by a window of rows;
+  // all keys where 128 of them per workgroup would leave half the chip idle
+  f.first = sh.left < 0 ? 0 : sh.sinks < sh.Tk ? sh.sinks : sh.Tk;
+  if (heads * f.key_tiles < 128) f.first = sh.Tk;
+  f.first_tiles = (f.first + 31) / 32;
+  f.parts = 1;
+  if (f.first > 0) {
+    const int64_t groups = heads * f.first_tiles, room = (256 + groups - 1) / groups;
+    const int64_t tiles = (rows + 127) / 128;   // 32 rows for each of four waves
+    f.parts = (int)(room < tiles ? room : tiles);
+    if (f.parts < 1) f.parts = 1;
+  }
+  f.stats_bytes = (heads * rows * 8 + 15) / 16 * 16;
+  f.workspace = f.stats_bytes + (f.first > 0 ? heads * f.first_tiles * f.parts * 64 * f.dp * 4 : 0);
+  return f;
+}
+
+int64_t backward_workspace(const dconv_attend_shape &sh) {
+  return sh.B == 0 || sh.D > kGradMaxD ? 0 : plan_backward(sh).workspace;
+}
 
 }  // namespace
 }  // namespace dconv
@@ -166,9 +192,22 @@ DCONV_EXPORT int dconv_attend_backward(const dconv_attend_shape *shape, const vo
   p.dq = dq;
   p.dk = dk;
   p.dv = dv;
+  BackwardPlan plan = plan_backward(*shape);
+  const int64_t flat = (int64_t)shape->D;
+  const long long dense[3] = {flat, flat, flat};
+  plan.direct = whole_pieces(q, shape->q_stride, *shape) && whole_pieces(k, shape->k_stride, *shape) &&
+                whole_pieces(v, shape->v_stride, *shape) && whole_pieces(out, shape->out_stride, *shape) &&
+                whole_pieces(dout, shape->dout_stride, *shape) && whole_pieces(dq, dense, *shape) &&
+                whole_pieces(dk, dense, *shape) && whole_pieces(dv, dense, *shape);
   (void)hipGetLastError();  // report this launch only
   by_type(shape->dtype, [&](auto *t) {
     using T = std::remove_pointer_t<decltype(t)>;
+    if (shape->D <= kGradMaxD) {
+      launch_attend_grad<T>(*shape, p, plan, workspace, (hipStream_t)stream);
+      return;
+    }
+    // larger heads: keys, values and both gradients of a tile do not fit the
+    // registers of a wave
     rows<T, 1>(*shape, p, (hipStream_t)stream);
     rows<T, 2>(*shape, p, (hipStream_t)stream);
   });

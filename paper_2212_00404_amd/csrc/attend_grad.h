@@ -1,0 +1,523 @@
+// The gradients of windowed attention on the matrix cores.  Probabilities are
+// computed again from the scores and the forward call's sums; with
+//   ds = p (dout . v - delta),  delta = dout . out
+// the two kernels below need three and four products per tile of scores.
+// attend_dq walks the keys for each tile of rows as the forward kernel does, and
+// leaves each row's sum and delta for the others; attend_dkv and attend_dkv_split
+// walk the rows for each tile of keys.  Nothing is added by atomics: the order
+// of every sum is fixed.
+#pragma once
+
+#include "attend_mma.h"
+
+namespace dconv {
+
+// A row's sum (in powers of two) and its delta, as the workspace holds them.
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+struct GradTile {
+  AttendTile a;
+  f32x2 *stats;      // [B * Hkv][rows]
+  int first;         // keys [0, first) belong to attend_dkv_split, the others to attend_dkv
+  int parts;         // parts of the rows (attend_dkv_split)
+};
+
+template <class T>
+__device__ __forceinline__ float frag_dot(typename Mma<T>::Frag a, typename Mma<T>::Frag b) {
+  float s = 0.0f;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) s = fmaf(to_f32(a[e]), to_f32(b[e]), s);
+  return s;
+}
+
+// Stores four consecutive elements from column d on.
+template <class T>
+__device__ __forceinline__ void store4(T *row, int d, int D, bool whole, float a, float b, float c, float e) {
+  T x[4] = {from_f32<T>(a), from_f32<T>(b), from_f32<T>(c), from_f32<T>(e)};
+  if (whole && d + 4 <= D) {
+    __builtin_memcpy(__builtin_assume_aligned(row + d, 4), x, sizeof(x));
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (d + i < D) row[d + i] = x[i];
+  }
+}
+
+// ---------------------------------------------------------------------------
+// dq
+// ---------------------------------------------------------------------------
+template <class T, int DP>
+__global__ __launch_bounds__(256) void attend_dq(const dconv_attend_shape sh, const AttendPtrs p, const GradTile gt) {
+  constexpr int BN = forward_keys<T>(DP), KS = DP / 16, DT = DP / 32;
+  typedef typename Mma<T>::Frag Frag;
+  __shared__ __align__(16) T buf0[2 * BN * DP];
+  __shared__ __align__(16) T buf1[2 * BN * DP];
+  DCONV_POISON(poison_lds(buf0, 2 * BN * DP); poison_lds(buf1, 2 * BN * DP));
+  const AttendTile &at = gt.a;
+  const int lane = threadIdx.x & 63, half = lane >> 5, wave = uniform(threadIdx.x >> 6);
+  const int id = xcd_remap(blockIdx.x, gridDim.x);
+  const int bh = id / at.tiles, b = bh / sh.Hkv, hk = bh % sh.Hkv, G = sh.Hq / sh.Hkv;
+  const int r0 = (id % at.tiles) * kForwardRows, rows = sh.Tq * G;
+  const Seq seq = seq_of(sh, p, b);
+  const Keys keys = keys_of(sh, seq, r0 / G, (min(r0 + kForwardRows, rows) - 1) / G);
+  const int n = uniform(keys.n);
+  const int r = r0 + 32 * wave + (lane & 31), rr = min(r, rows - 1);
+  const int t = rr / G, h = hk * G + rr % G;
+  const RowKeys see = row_keys(sh, seq, keys, seq.start + t);
+  int from = see.lo, to = see.hi, all_from = see.lo, all_to = see.hi;
+#pragma unroll
+  for (int x = 16; x > 0; x >>= 1) {
+    from = min(from, __shfl_xor(from, x));
+    to = max(to, __shfl_xor(to, x));
+    all_from = max(all_from, __shfl_xor(all_from, x));
+    all_to = min(all_to, __shfl_xor(all_to, x));
+  }
+  from = uniform(from), to = uniform(to), all_from = uniform(all_from), all_to = uniform(all_to);
+
+  const T *kh = row_of<T>(p.k, sh.k_stride, b, 0, hk), *vh = row_of<T>(p.v, sh.v_stride, b, 0, hk);
+  auto stage = [&](T *buf, int v0) {
+    auto from_row = [&](const T *base, long long stride) {
+      return [=](int x) { return base + (int64_t)keys.key(min(v0 + x, n - 1)) * stride; };
+    };
+    Tile<T, DP>::template stage<BN, 256>(buf, sh.D, at.direct, threadIdx.x, from_row(kh, sh.k_stride[1]));
+    Tile<T, DP>::template stage<BN, 256>(buf + BN * DP, sh.D, at.direct, threadIdx.x,
+                                         from_row(vh, sh.v_stride[1]));
+  };
+  if (n > 0) stage(buf0, 0);
+
+  Frag q[KS], g[KS];
+  const T *qrow = row_of<T>(p.q, sh.q_stride, b, t, h), *grow = row_of<T>(p.dout, sh.dout_stride, b, t, h);
+  const T *orow = row_of<T>(p.out, sh.out_stride, b, t, h);
+  float delta = 0.0f;
+#pragma unroll
+  for (int k = 0; k < KS; ++k) {
+    const int d = 16 * k + 8 * half;
+    q[k] = load_frag(qrow, d, sh.D, at.direct, at.sign);
+    g[k] = load_frag(grow, d, sh.D, at.direct, 1.0f);
+    delta += frag_dot<T>(g[k], load_frag(orow, d, sh.D, at.direct, 1.0f));
+  }
+  delta = half_sum(delta);
+  const float lse2 = see.none ? 0.0f : 1.4426950408889634f * p.lse[((int64_t)b * sh.Hq + h) * sh.Tq + t];
+
+  // out, rounded to the tensors' type, gives delta to within that rounding of
+  // |dout| |out|.  Where a row's weight is on a few keys, dp - delta cancels and
+  // that error is much of what is left.  The sum of p (dp - delta) over the keys
+  // is how far off it is: it corrects delta for the other kernels and, times the
+  // mean key (sum of p k: a fourth product, on operands already loaded), dq.
+  f32x16 acc[DT], mean[DT];
+  float miss = 0.0f;
+#pragma unroll
+  for (int c = 0; c < DT; ++c) acc[c] = mean[c] = f32x16{};
+  auto step = [&](const T *buf, int v0) {
+    if (v0 >= to || (v0 + BN <= from && v0 >= sh.sinks)) return;
+    const bool masked = !(v0 + BN <= all_to && (v0 >= all_from || v0 + BN <= sh.sinks));
+    const T *ks = buf, *vs = buf + BN * DP;
+#pragma unroll
+    for (int hb = 0; hb < BN / 32; ++hb) {
+      f32x16 s = {}, dp = {};
+#pragma unroll
+      for (int k = 0; k < KS; ++k) s = Mma<T>::mac(Tile<T, DP>::row(ks, 32 * hb, k, lane), q[k], s);
+#pragma unroll
+      for (int k = 0; k < KS; ++k) dp = Mma<T>::mac(Tile<T, DP>::row(vs, 32 * hb, k, lane), g[k], dp);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        s[i] = power2<T>(fmaf(s[i], at.scale2, -lse2));
+        dp[i] = s[i] * (dp[i] - delta);
+      }
+      if (masked) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int v = v0 + 32 * hb + acc_row(i, half);
+          const bool on = v < see.hi && (v >= see.lo || v < sh.sinks);
+          s[i] = on ? s[i] : 0.0f;
+          dp[i] = on ? dp[i] : 0.0f;
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < 16; ++i) miss += dp[i];
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const Frag w = as_operand<T>(s, k), u = as_operand<T>(dp, k);
+#pragma unroll
+        for (int c = 0; c < DT; ++c) {
+          const Frag x = Tile<T, DP>::column(ks, 32 * hb + 16 * k, c, lane);
+          acc[c] = Mma<T>::mac(x, u, acc[c]);
+          mean[c] = Mma<T>::mac(x, w, mean[c]);
+        }
+      }
+    }
+  };
+  auto arrived = [&]() {
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    __syncthreads();
+  };
+  for (int v0 = 0; v0 < n; v0 += 2 * BN) {
+    arrived();
+    if (v0 + BN < n) stage(buf1, v0 + BN);
+    step(buf0, v0);
+    if (v0 + BN >= n) break;
+    arrived();
+    if (v0 + 2 * BN < n) stage(buf0, v0 + 2 * BN);
+    step(buf1, v0 + BN);
+  }
+
+  miss = half_sum(miss);
+  if (half == 0 && r < rows) gt.stats[(int64_t)bh * rows + r] = f32x2{lse2, delta + miss};
+  bool bad = false;
+#pragma unroll
+  for (int c = 0; c < DT; ++c)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      acc[c][i] = sh.scale * fmaf(-miss, mean[c][i], acc[c][i]);
+      bad |= 32 * c + acc_row(i, half) < sh.D && !(fabsf(acc[c][i]) < INFINITY);
+    }
+  const unsigned long long any = __ballot(bad && r < rows);
+  const unsigned redo = kSumAgain ? (unsigned)(any | (any >> 32)) : 0u;
+  if (r < rows && !(redo >> (lane & 31) & 1)) {
+    T *o = (T *)p.dq + (((int64_t)b * sh.Tq + t) * sh.Hq + h) * sh.D;
+#pragma unroll
+    for (int c = 0; c < DT; ++c)
+#pragma unroll
+      for (int i = 0; i < 16; i += 4)
+        store4(o, 32 * c + acc_row(i, half), sh.D, at.direct, acc[c][i], acc[c][i + 1], acc[c][i + 2],
+               acc[c][i + 3]);
+  }
+  for (unsigned again = redo; again; again &= again - 1) {
+    const int x = r0 + 32 * wave + __ffs(again) - 1;
+    attend_row_dq<T>(sh, p, b, hk * G + x % G, x / G);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// dk, dv
+// ---------------------------------------------------------------------------
+// 32 keys of one wave, a key per column (lane % 32).
+template <class T, int DP>
+struct KeyGrad {
+  static constexpr int KS = DP / 16, DT = DP / 32;
+  typedef typename Mma<T>::Frag Frag;
+  Frag k[KS], v[KS];
+  f32x16 dk[DT], dv[DT];   // dk[c][i]: element 32 c + acc_row(i, half) of the key
+
+  __device__ __forceinline__ void load(const dconv_attend_shape &sh, const AttendTile &at, const T *krow,
+                                       const T *vrow, int half) {
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      k[s] = load_frag(krow, 16 * s + 8 * half, sh.D, at.direct, at.sign);
+      v[s] = load_frag(vrow, 16 * s + 8 * half, sh.D, at.direct, 1.0f);
+    }
+#pragma unroll
+    for (int c = 0; c < DT; ++c) dk[c] = dv[c] = f32x16{};
+  }
+
+  // 32 rows r .. of the tiles qs (queries) and gs (dout), their statistics in st;
+  // the key is seen by rows [lo, hi).
+  __device__ __forceinline__ void add(const T *qs, const T *gs, const f32x2 *st, int r, int lo, int hi, bool masked,
+                                      float scale2, int lane) {
+    const int half = lane >> 5;
+    f32x16 s = {}, dp = {};
+#pragma unroll
+    for (int x = 0; x < KS; ++x) s = Mma<T>::mac(Tile<T, DP>::row(qs, 0, x, lane), k[x], s);
+#pragma unroll
+    for (int x = 0; x < KS; ++x) dp = Mma<T>::mac(Tile<T, DP>::row(gs, 0, x, lane), v[x], dp);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const f32x2 x = st[acc_row(i, half)];
+      s[i] = power2<T>(fmaf(s[i], scale2, -x[0]));
+      dp[i] = s[i] * (dp[i] - x[1]);
+    }
+    if (masked) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int x = r + acc_row(i, half);
+        const bool on = x >= lo && x < hi;
+        s[i] = on ? s[i] : 0.0f;
+        dp[i] = on ? dp[i] : 0.0f;
+      }
+    }
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      const Frag w = as_operand<T>(s, x), u = as_operand<T>(dp, x);
+#pragma unroll
+      for (int c = 0; c < DT; ++c) {
+        dv[c] = Mma<T>::mac(Tile<T, DP>::column(gs, 16 * x, c, lane), w, dv[c]);
+        dk[c] = Mma<T>::mac(Tile<T, DP>::column(qs, 16 * x, c, lane), u, dk[c]);
+      }
+    }
+  }
+};
+
+// Rows [lo, hi) that see key j (of those this kernel counts).
+struct KeyRows {
+  int lo, hi;
+};
+__device__ __forceinline__ KeyRows key_rows(const dconv_attend_shape &sh, const Seq &s, int j, int from, int end) {
+  KeyRows r = {0, 0};
+  if (j < from || j >= min(end, s.len)) return r;
+  const QuerySpan q = queries_of(sh, s, j);
+  const int G = sh.Hq / sh.Hkv;
+  r.lo = q.lo * G;
+  r.hi = q.hi * G;
+  return r;
+}
+
+// The rows of a wave's 32 keys: all of them, and those that see every key.
+struct TileRows {
+  int from, to, all_from, all_to;
+};
+__device__ __forceinline__ TileRows tile_rows(const KeyRows &k) {
+  TileRows t = {k.lo < k.hi ? k.lo : 0x7fffffff, k.hi, k.lo, k.hi};
+#pragma unroll
+  for (int x = 16; x > 0; x >>= 1) {
+    t.from = min(t.from, __shfl_xor(t.from, x));
+    t.to = max(t.to, __shfl_xor(t.to, x));
+    t.all_from = max(t.all_from, __shfl_xor(t.all_from, x));
+    t.all_to = min(t.all_to, __shfl_xor(t.all_to, x));
+  }
+  t.from = uniform(t.from), t.to = uniform(t.to), t.all_from = uniform(t.all_from), t.all_to = uniform(t.all_to);
+  return t;
+}
+
+// The statistics of 32 rows r .. into LDS, by one wave (past `to` the last row's).
+__device__ __forceinline__ void stage_stats(f32x2 *lds, const f32x2 *stats, int r, int to, int lane) {
+  const float *from = reinterpret_cast<const float *>(stats + min(r + (lane >> 1), to - 1)) + (lane & 1);
+  __builtin_amdgcn_global_load_lds(from, (lds_ptr)lds, 4, 0, 0);
+}
+
+constexpr int kGradKeys = 128;
+
+// 128 keys per workgroup, 32 per wave; tiles of 32 rows of queries and dout in two
+// LDS buffers, the next one copied while the current one is used.
+template <class T, int DP>
+__global__ __launch_bounds__(256) void attend_dkv(const dconv_attend_shape sh, const AttendPtrs p, const GradTile gt) {
+  constexpr int DT = DP / 32, kTile = 32 * DP;
+  __shared__ __align__(16) T buf0[2 * kTile];
+  __shared__ __align__(16) T buf1[2 * kTile];
+  __shared__ __align__(16) f32x2 stats0[32];
+  __shared__ __align__(16) f32x2 stats1[32];
+  __shared__ int span[2][4];
+  DCONV_POISON(poison_lds(buf0, 2 * kTile); poison_lds(buf1, 2 * kTile); poison_lds(stats0, 32);
+               poison_lds(stats1, 32));
+  const AttendTile &at = gt.a;
+  const int lane = threadIdx.x & 63, half = lane >> 5, wave = uniform(threadIdx.x >> 6);
+  const int id = xcd_remap(blockIdx.x, gridDim.x);
+  const int bh = id / at.tiles, b = bh / sh.Hkv, hk = bh % sh.Hkv, G = sh.Hq / sh.Hkv;
+  const int j = (id % at.tiles) * kGradKeys + 32 * wave + (lane & 31), jj = min(j, sh.Tk - 1);
+  const Seq seq = seq_of(sh, p, b);
+  const KeyRows see = key_rows(sh, seq, j, gt.first, sh.Tk);
+  const TileRows mine = tile_rows(see);
+  if (lane == 0) {
+    span[0][wave] = mine.from;
+    span[1][wave] = mine.to;
+  }
+  __syncthreads();
+  const int from = uniform(min(min(span[0][0], span[0][1]), min(span[0][2], span[0][3])));
+  const int to = uniform(max(max(span[1][0], span[1][1]), max(span[1][2], span[1][3])));
+
+  auto stage = [&](T *buf, f32x2 *st, int r) {
+    auto from_row = [&](const void *base, const long long *stride) {
+      return [=](int x) {
+        const int y = min(r + x, to - 1);
+        return row_of<T>(base, stride, b, y / G, hk * G + y % G);
+      };
+    };
+    Tile<T, DP>::template stage<32, 256>(buf, sh.D, at.direct, threadIdx.x, from_row(p.q, sh.q_stride));
+    Tile<T, DP>::template stage<32, 256>(buf + kTile, sh.D, at.direct, threadIdx.x,
+                                         from_row(p.dout, sh.dout_stride));
+    if (wave == 0) stage_stats(st, gt.stats + (int64_t)bh * sh.Tq * G, r, to, lane);
+  };
+  if (from < to) stage(buf0, stats0, from);
+  KeyGrad<T, DP> acc;
+  acc.load(sh, at, row_of<T>(p.k, sh.k_stride, b, jj, hk), row_of<T>(p.v, sh.v_stride, b, jj, hk), half);
+  auto step = [&](const T *buf, const f32x2 *st, int r) {
+    if (r >= mine.to || r + 32 <= mine.from) return;
+    acc.add(buf, buf + kTile, st, r, see.lo, see.hi, !(r >= mine.all_from && r + 32 <= mine.all_to), at.scale2,
+            lane);
+  };
+  auto arrived = [&]() {
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    __syncthreads();
+  };
+  for (int r = from; r < to; r += 64) {
+    arrived();
+    if (r + 32 < to) stage(buf1, stats1, r + 32);
+    step(buf0, stats0, r);
+    if (r + 32 >= to) break;
+    arrived();
+    if (r + 64 < to) stage(buf0, stats0, r + 64);
+    step(buf1, stats1, r + 32);
+  }
+
+  bool bad = false;
+#pragma unroll
+  for (int c = 0; c < DT; ++c)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      acc.dk[c][i] *= sh.scale;
+      bad |= 32 * c + acc_row(i, half) < sh.D &&
+             !(fabsf(acc.dk[c][i]) < INFINITY && fabsf(acc.dv[c][i]) < INFINITY);
+    }
+  const bool own = j >= gt.first && j < sh.Tk;
+  const unsigned long long any = __ballot(bad && own);
+  const unsigned redo = kSumAgain ? (unsigned)(any | (any >> 32)) : 0u;
+  if (own && !(redo >> (lane & 31) & 1)) {
+    const int64_t o = (((int64_t)b * sh.Tk + j) * sh.Hkv + hk) * sh.D;
+#pragma unroll
+    for (int c = 0; c < DT; ++c)
+#pragma unroll
+      for (int i = 0; i < 16; i += 4) {
+        const int d = 32 * c + acc_row(i, half);
+        store4((T *)p.dk + o, d, sh.D, at.direct, acc.dk[c][i], acc.dk[c][i + 1], acc.dk[c][i + 2], acc.dk[c][i + 3]);
+        store4((T *)p.dv + o, d, sh.D, at.direct, acc.dv[c][i], acc.dv[c][i + 1], acc.dv[c][i + 2], acc.dv[c][i + 3]);
+      }
+  }
+  for (unsigned again = redo; again; again &= again - 1)
+    attend_row_dkv<T>(sh, p, b, hk, (id % at.tiles) * kGradKeys + 32 * wave + __ffs(again) - 1);
+}
+
+// Keys [0, gt.first) in tiles of 32: the first keys, which every row sees, or all
+// keys of a small call.  The rows are divided over the waves, each with two LDS
+// buffers of its own, and over gt.parts workgroups, which leave their sums in the
+// workspace.
+template <class T, int DP>
+__global__ __launch_bounds__(64 * split_waves<T>(DP)) void attend_dkv_split(const dconv_attend_shape sh,
+                                                                            const AttendPtrs p, const GradTile gt) {
+  constexpr int DT = DP / 32, kTile = 32 * DP, W = split_waves<T>(DP);
+  __shared__ __align__(16) T buf0[W * 2 * kTile];
+  __shared__ __align__(16) T buf1[W * 2 * kTile];
+  __shared__ __align__(16) f32x2 stats0[W * 32];
+  __shared__ __align__(16) f32x2 stats1[W * 32];
+  DCONV_POISON(poison_lds(buf0, W * 2 * kTile); poison_lds(buf1, W * 2 * kTile); poison_lds(stats0, W * 32);
+               poison_lds(stats1, W * 32));
+  const AttendTile &at = gt.a;
+  const int lane = threadIdx.x & 63, half = lane >> 5, wave = uniform(threadIdx.x >> 6);
+  const int part = blockIdx.x % gt.parts, id = blockIdx.x / gt.parts;
+  const int bh = id / at.tiles, b = bh / sh.Hkv, hk = bh % sh.Hkv, G = sh.Hq / sh.Hkv;
+  const int j0 = (id % at.tiles) * 32, j = j0 + (lane & 31), jj = min(j, sh.Tk - 1);
+  const Seq seq = seq_of(sh, p, b);
+  const KeyRows see = key_rows(sh, seq, j, 0, gt.first);
+  const TileRows mine = tile_rows(see);
+
+  auto stage = [&](T *buf, f32x2 *st, int r) {
+    auto from_row = [&](const void *base, const long long *stride) {
+      return [=](int x) {
+        const int y = min(r + x, mine.to - 1);
+        return row_of<T>(base, stride, b, y / G, hk * G + y % G);
+      };
+    };
+    T *to = buf + wave * 2 * kTile;
+    Tile<T, DP>::template stage<32, 64>(to, sh.D, at.direct, lane, from_row(p.q, sh.q_stride));
+    Tile<T, DP>::template stage<32, 64>(to + kTile, sh.D, at.direct, lane, from_row(p.dout, sh.dout_stride));
+    stage_stats(st + wave * 32, gt.stats + (int64_t)bh * sh.Tq * G, r, mine.to, lane);
+  };
+  KeyGrad<T, DP> acc;
+  acc.load(sh, at, row_of<T>(p.k, sh.k_stride, b, jj, hk), row_of<T>(p.v, sh.v_stride, b, jj, hk), half);
+  auto step = [&](const T *buf, const f32x2 *st, int r) {
+    const T *from = buf + wave * 2 * kTile;
+    acc.add(from, from + kTile, st + wave * 32, r, see.lo, see.hi, true, at.scale2, lane);
+  };
+  auto arrived = [&]() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory"); };
+  const int stride = 32 * gt.parts * W;
+  if (mine.from < mine.to) {
+    int r = mine.from + 32 * (part * W + wave);
+    if (r < mine.to) stage(buf0, stats0, r);
+    for (; r < mine.to; r += 2 * stride) {
+      arrived();
+      if (r + stride < mine.to) stage(buf1, stats1, r + stride);
+      step(buf0, stats0, r);
+      if (r + stride >= mine.to) break;
+      arrived();
+      if (r + 2 * stride < mine.to) stage(buf0, stats0, r + 2 * stride);
+      step(buf1, stats1, r + stride);
+    }
+  }
+  // the waves' sums as rows in LDS: first dk, then dv
+  auto lds_row = [&](int w, int x) {
+    return reinterpret_cast<float *>(x < 16 ? buf0 : buf1) + (w * 16 + (x & 15)) * DP;
+  };
+  for (int which = 0; which < 2; ++which) {
+    __syncthreads();
+#pragma unroll
+    for (int c = 0; c < DT; ++c)
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        lds_row(wave, lane & 31)[32 * c + acc_row(i, half)] = which ? acc.dv[c][i] : acc.dk[c][i];
+    __syncthreads();
+    float *out = at.partial + ((int64_t)blockIdx.x * 2 + which) * kTile;
+    for (int x = threadIdx.x; x < kTile; x += 64 * W) {
+      float s = 0.0f;
+      for (int w = 0; w < W; ++w) s += lds_row(w, x / DP)[x % DP];
+      out[x] = s;
+    }
+  }
+}
+
+// A wave per key adds the parts.
+template <class T, int DP>
+__global__ __launch_bounds__(64) void attend_dkv_join(const dconv_attend_shape sh, const AttendPtrs p,
+                                                      const GradTile gt) {
+  const int lane = threadIdx.x, j = blockIdx.x % gt.first, bh = blockIdx.x / gt.first;
+  const int b = bh / sh.Hkv, hk = bh % sh.Hkv;
+  const float *part = gt.a.partial + ((int64_t)bh * gt.a.tiles + j / 32) * gt.parts * 64 * DP + j % 32 * DP;
+  float dk[DP / 64 + 1], dv[DP / 64 + 1];
+  bool bad = false;
+#pragma unroll
+  for (int i = 0; i <= DP / 64; ++i) {
+    const int d = lane + 64 * i;
+    dk[i] = dv[i] = 0.0f;
+    if (d >= sh.D) continue;
+    for (int x = 0; x < gt.parts; ++x) {
+      dk[i] += part[(int64_t)x * 64 * DP + d];
+      dv[i] += part[(int64_t)x * 64 * DP + 32 * DP + d];
+    }
+    dk[i] *= sh.scale;
+    bad |= !(fabsf(dk[i]) < INFINITY && fabsf(dv[i]) < INFINITY);
+  }
+  if (kSumAgain && __any(bad)) {
+    attend_row_dkv<T>(sh, p, b, hk, j);
+    return;
+  }
+  const int64_t o = (((int64_t)b * sh.Tk + j) * sh.Hkv + hk) * sh.D;
+#pragma unroll
+  for (int i = 0; i <= DP / 64; ++i)
+    if (lane + 64 * i < sh.D) {
+      ((T *)p.dk)[o + lane + 64 * i] = from_f32<T>(dk[i]);
+      ((T *)p.dv)[o + lane + 64 * i] = from_f32<T>(dv[i]);
+    }
+}
+
+template <class T>
+void launch_attend_grad(const dconv_attend_shape &sh, const AttendPtrs &p, const BackwardPlan &plan, void *workspace,
+                        hipStream_t s) {
+  GradTile gt = {};
+  gt.a = attend_tile(sh, plan.direct);
+  gt.stats = (f32x2 *)workspace;
+  gt.a.partial = (float *)((char *)workspace + plan.stats_bytes);
+  gt.first = plan.first;
+  gt.parts = plan.parts;
+  auto launch = [&](auto dp) {
+    constexpr int DP = decltype(dp)::value;
+    const unsigned heads = (unsigned)(sh.B * sh.Hkv);
+    if (plan.row_tiles > 0) {
+      gt.a.tiles = plan.row_tiles;
+      hipLaunchKernelGGL((attend_dq<T, DP>), dim3(heads * plan.row_tiles), dim3(256), 0, s, sh, p, gt);
+    }
+    if (plan.first < sh.Tk) {
+      gt.a.tiles = plan.key_tiles;
+      hipLaunchKernelGGL((attend_dkv<T, DP>), dim3(heads * plan.key_tiles), dim3(256), 0, s, sh, p, gt);
+    }
+    if (plan.first > 0) {
+      gt.a.tiles = plan.first_tiles;
+      hipLaunchKernelGGL((attend_dkv_split<T, DP>), dim3(heads * plan.first_tiles * plan.parts),
+                         dim3(64 * split_waves<T>(DP)), 0, s, sh, p, gt);
+      hipLaunchKernelGGL((attend_dkv_join<T, DP>), dim3(heads * plan.first), dim3(64), 0, s, sh, p, gt);
+    }
+  };
+  if (plan.dp == 32) launch(std::integral_constant<int, 32>());
+  if (plan.dp == 64) launch(std::integral_constant<int, 64>());
+  if (plan.dp == 96) launch(std::integral_constant<int, 96>());
+  if (plan.dp == 128) launch(std::integral_constant<int, 128>());
+}
+
+}  // namespace dconv

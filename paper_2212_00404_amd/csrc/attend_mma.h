@@ -115,9 +115,10 @@ struct Tile {
   static __device__ __forceinline__ void stage(T *lds, int D, bool direct, int me, F row_start) {
     constexpr int kPer = 16 / sizeof(T), kPieces = DP / kPer;
     if (direct) {
-      static_assert(NR * kPieces % NT == 0, "whole copies");
+      static_assert(NR * kPieces % 64 == 0, "whole waves");
 #pragma unroll
-      for (int i = 0; i < NR * kPieces / NT; ++i) {
+      for (int i = 0; i < (NR * kPieces + NT - 1) / NT; ++i) {
+        if (NR * kPieces % NT != 0 && i * NT + (me & ~63) >= NR * kPieces) break;
         const int slot = i * NT + me, r = slot / kPieces, piece = slot % kPieces;
         int e = ((piece * kPer / 8) ^ swizzle(r)) * 8 + piece * kPer % 8;
         e = e < D ? e : 0;
@@ -149,6 +150,13 @@ __device__ __forceinline__ typename Mma<T>::Frag load_frag(const T *row, int d, 
     for (int e = 0; e < 8; ++e) f[e] = from_f32<T>(to_f32(f[e]) * sign);
   }
   return f;
+}
+
+// 2^x.  The instruction gives 0 below 2^-126; fp32 tensors keep such values, for
+// 16-bit ones they are far below what a probability is rounded to.
+template <class T>
+__device__ __forceinline__ float power2(float x) {
+  return sizeof(T) == 4 ? exp2f(x) : __builtin_amdgcn_exp2f(x);
 }
 
 // The other half of a query's lanes, 32 away.
@@ -254,7 +262,7 @@ struct Softmax {
     for (int hb = 0; hb < HB; ++hb)
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        s[hb][i] = __builtin_amdgcn_exp2f(fmaf(s[hb][i], scale2, -base));
+        s[hb][i] = power2<T>(fmaf(s[hb][i], scale2, -base));
         l += s[hb][i];
       }
 #pragma unroll
