@@ -384,7 +384,8 @@ int dconv_rotate(const dconv_rotate_shape *shape, const void *x, const float *po
  *     tensors' type or fp32), [D], or [B][D] where per_sample has the vector's
  *     bit; NULL stands for ones (zeros for pre_bias)
  *   stats : NULL, or fp32 [B*T][4], written: mean and 1 / sqrt(..) of branch
- *     (0, 1 without post), then of h; what dconv_join_backward reads
+ *     (0, 1 without post), then of h; what dconv_join_backward reads;
+     16-byte aligned
  * branch = NULL is the norm before the first block (h = residual_scale * x,
  * post and gate unused; h may be NULL); y = NULL leaves out the second norm
  * (after the last block).  1 <= D <= 16384.

@@ -1,0 +1,6 @@
+// The kernels of dconv_join for one type.
+#include "join_kernels.h"
+
+namespace dconv {
+template void launch_join<float, float>(const dconv_join_shape &, const JoinPtrs &, const JoinPlan &, float *, bool, hipStream_t);
+}  // namespace dconv
