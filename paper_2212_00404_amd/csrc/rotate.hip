@@ -9,6 +9,8 @@
 namespace dconv {
 namespace {
 
+constexpr int64_t kThreads = 256 * 2048;   // what the chip holds at once
+
 // sin and cos of position * freq.  The angle is taken in turns: freq / 2pi as
 // the sum of two fp32 values, the product with its rounding error (one fma),
 // and the whole turns dropped exactly before anything is rounded, so the
@@ -26,47 +28,124 @@ __device__ __forceinline__ void turn_sincos(float position, float freq, float *s
   sincospif(2.0f * ((p - rintf(p)) + e), s, c);
 }
 
-// One thread per pair, or per element of the unrotated rest.
-template <class T>
-__global__ __launch_bounds__(256) void rotate_pairs(const dconv_rotate_shape sh, const T *x,
-                                                    const float *__restrict__ positions,
-                                                    const float *__restrict__ freq,
-                                                    const int *__restrict__ axis, T *out) {
-  const int per_head = sh.D - sh.R;
-  const int64_t n = (int64_t)sh.B * sh.T * sh.H * per_head;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
-    const int r = (int)(i % per_head);
-    int64_t k = i / per_head;
-    const int h = (int)(k % sh.H);
-    k /= sh.H;
-    const int t = (int)(k % sh.T);
-    const int b = (int)(k / sh.T);
-    const T *xr = x + b * sh.x_stride[0] + t * sh.x_stride[1] + h * sh.x_stride[2];
-    T *yr = out + b * sh.out_stride[0] + t * sh.out_stride[1] + h * sh.out_stride[2];
-    if (r >= sh.R) {
-      yr[r + sh.R] = xr[r + sh.R];
-      continue;
+// Bound by memory: every element is read and written once.  A thread takes one
+// piece of a token (P pairs, or V elements past the pairs), computes its sines and
+// cosines once (some 60 instructions a pair) and turns that piece in every
+// `split`-th head; neighbouring threads take neighbouring pieces, then heads.
+struct Work {
+  int pieces, pairs;   // pieces per token, those that hold pairs
+  int split;           // threads that share a token's heads
+  int64_t threads;
+};
+
+// V elements per access (16 bytes, or one).
+template <class T, int V, bool ADJACENT>
+__global__ __launch_bounds__(256) void rotate_pieces(const dconv_rotate_shape sh, const Work wk, const T *x,
+                                                     const float *__restrict__ positions,
+                                                     const float *__restrict__ freq, const int *__restrict__ axis,
+                                                     T *out) {
+  constexpr int P = ADJACENT ? (V > 1 ? V / 2 : 1) : V;   // pairs per piece
+  constexpr bool kTwo = !ADJACENT || V == 1;               // a piece's pairs are in two places
+  struct alignas(V * sizeof(T)) Pack {
+    T v[V];
+  };
+  const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (id >= wk.threads) return;
+  const int piece = (int)(id % wk.pieces);
+  const int64_t rest = id / wk.pieces;
+  const int h0 = (int)(rest % wk.split);
+  const int64_t token = rest / wk.split;
+  const int t = (int)(token % sh.T);
+  const int64_t b = token / sh.T;
+  const T *xr = x + b * sh.x_stride[0] + t * sh.x_stride[1];
+  T *yr = out + b * sh.out_stride[0] + t * sh.out_stride[1];
+
+  if (piece >= wk.pairs) {   // past the pairs: copied
+    const int e = (ADJACENT ? wk.pairs * (V > 1 ? V : 2) : 2 * sh.R) + (piece - wk.pairs) * V;
+#pragma unroll 4
+    for (int h = h0; h < sh.H; h += wk.split)
+      *reinterpret_cast<Pack *>(yr + h * sh.out_stride[2] + e) =
+          *reinterpret_cast<const Pack *>(xr + h * sh.x_stride[2] + e);
+    return;
+  }
+  const int r0 = piece * P;
+  float s[P], c[P];
+  bool turned[P];
+#pragma unroll
+  for (int k = 0; k < P; ++k) {
+    const int r = r0 + k;
+    const int a = r < sh.R ? axis[r] : -1;
+    s[k] = 0.0f;
+    c[k] = 1.0f;
+    turned[k] = a >= 0 && a < sh.axes;
+    if (turned[k])
+      turn_sincos(positions[a * sh.pos_stride[0] + b * sh.pos_stride[1] + t * sh.pos_stride[2]], freq[r], &s[k],
+                  &c[k]);
+    if (sh.inverse) s[k] = -s[k];
+  }
+  // (a pair that is not turned is copied: 0 times an infinity is not 0)
+  auto turn = [&](int k, T &u, T &w) {
+    const float fu = to_f32(u), fw = to_f32(w);
+    if (turned[k]) {
+      // (which product is fused is written out: the same bits in every variant)
+      u = from_f32<T>(fmaf(fu, c[k], -(fw * s[k])));
+      w = from_f32<T>(fmaf(fu, s[k], fw * c[k]));
     }
-    const int a = axis[r];
-    float s = 0.0f, c = 1.0f;
-    if (a >= 0 && a < sh.axes)
-      turn_sincos(positions[a * sh.pos_stride[0] + b * sh.pos_stride[1] + t * sh.pos_stride[2]],
-                  freq[r], &s, &c);
-    if (sh.inverse) s = -s;
-    const int iu = sh.adjacent ? 2 * r : r, iw = sh.adjacent ? 2 * r + 1 : r + sh.R;
-    const float u = to_f32(xr[iu]), w = to_f32(xr[iw]);
-    yr[iu] = from_f32<T>(u * c - w * s);
-    yr[iw] = from_f32<T>(u * s + w * c);
+  };
+  const int eu = ADJACENT ? (V > 1 ? piece * V : 2 * r0) : r0;
+  const int ew = ADJACENT ? eu + 1 : r0 + sh.R;
+#pragma unroll 4
+  for (int h = h0; h < sh.H; h += wk.split) {
+    const T *xh = xr + h * sh.x_stride[2];
+    T *yh = yr + h * sh.out_stride[2];
+    Pack u = *reinterpret_cast<const Pack *>(xh + eu);
+    if constexpr (kTwo) {
+      Pack w = *reinterpret_cast<const Pack *>(xh + ew);
+#pragma unroll
+      for (int k = 0; k < P; ++k) turn(k, u.v[k], w.v[k]);
+      *reinterpret_cast<Pack *>(yh + ew) = w;
+    } else {
+#pragma unroll
+      for (int k = 0; k < P; ++k) turn(k, u.v[2 * k], u.v[2 * k + 1]);
+    }
+    *reinterpret_cast<Pack *>(yh + eu) = u;
   }
 }
 
+template <class T, int V, bool ADJACENT>
+void launch_pieces(const dconv_rotate_shape &sh, const void *x, const float *positions, const float *freq,
+                   const int *axis, void *out, hipStream_t s) {
+  Work wk;
+  if (ADJACENT) {
+    const int per = V > 1 ? V : 2;
+    wk.pairs = (2 * sh.R + per - 1) / per;
+    wk.pieces = wk.pairs + (sh.D - (wk.pairs * per < sh.D ? wk.pairs * per : sh.D)) / V;
+  } else {
+    wk.pairs = sh.R / V;
+    wk.pieces = wk.pairs + (sh.D - 2 * sh.R) / V;
+  }
+  // Each thread takes as many heads as leave threads enough to fill the chip.
+  const int64_t per_head = (int64_t)sh.B * sh.T * wk.pieces;
+  int64_t split = (kThreads + per_head - 1) / per_head;
+  wk.split = (int)(split < sh.H ? split : sh.H);
+  wk.threads = per_head * wk.split;
+  hipLaunchKernelGGL((rotate_pieces<T, V, ADJACENT>), dim3((unsigned)((wk.threads + 255) / 256)), dim3(256), 0, s,
+                     sh, wk, (const T *)x, positions, freq, axis, (T *)out);
+}
+
 template <class T>
-hipError_t launch(const dconv_rotate_shape &sh, const void *x, const float *positions,
-                  const float *freq, const int *axis, void *out, hipStream_t s) {
-  const int64_t n = (int64_t)sh.B * sh.T * sh.H * (sh.D - sh.R);
-  const int64_t blocks = (n + 255) / 256;
-  hipLaunchKernelGGL(rotate_pairs<T>, dim3((unsigned)(blocks < (1 << 20) ? blocks : (1 << 20))),
-                     dim3(256), 0, s, sh, (const T *)x, positions, freq, axis, (T *)out);
+hipError_t launch(const dconv_rotate_shape &sh, const void *x, const float *positions, const float *freq,
+                  const int *axis, void *out, hipStream_t s) {
+  constexpr int V = 16 / sizeof(T);
+  bool whole = sh.D % V == 0 && (uintptr_t)x % 16 == 0 && (uintptr_t)out % 16 == 0 &&
+               (sh.adjacent || sh.R % V == 0);
+  for (int i = 0; i < 3; ++i) whole = whole && sh.x_stride[i] % V == 0 && sh.out_stride[i] % V == 0;
+  if (whole)
+    sh.adjacent ? launch_pieces<T, V, true>(sh, x, positions, freq, axis, out, s)
+                : launch_pieces<T, V, false>(sh, x, positions, freq, axis, out, s);
+  else
+    sh.adjacent ? launch_pieces<T, 1, true>(sh, x, positions, freq, axis, out, s)
+                : launch_pieces<T, 1, false>(sh, x, positions, freq, axis, out, s);
   return hipGetLastError();
 }
 
@@ -81,7 +160,8 @@ DCONV_EXPORT int dconv_rotate(const dconv_rotate_shape *shape, const void *x,
   if (sh.B < 0 || sh.T < 0 || sh.H < 1 || sh.D < 1 || sh.R < 0 || sh.R > sh.D / 2 ||
       sh.axes < 1 || (sh.adjacent & ~1) || (sh.inverse & ~1) || !dconv::element_size(sh.dtype))
     return DCONV_EINVAL;
-  if (sh.H > INT_MAX / sh.D || (int64_t)sh.B * sh.T > INT64_MAX / sh.H / sh.D / 8)
+  // threads are counted by 2^31 workgroups of 256, a piece of an element each at most
+  if (sh.H > INT_MAX / sh.D || (int64_t)sh.B * sh.T > ((int64_t)INT_MAX * 256) / ((int64_t)sh.H * sh.D))
     return DCONV_ERANGE;
   if (sh.B == 0 || sh.T == 0) return DCONV_OK;
   if (!x || !out || (sh.R > 0 && (!positions || !freq || !axis))) return DCONV_ENULL;
