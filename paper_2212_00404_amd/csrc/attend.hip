@@ -73,7 +73,7 @@ ForwardPlan plan_forward(const dconv_attend_shape &sh) {
   ForwardPlan f = {};
   f.dp = padded_head(sh.D);
   const int64_t rows = (int64_t)sh.Tq * (sh.Hq / sh.Hkv), heads = (int64_t)sh.B * sh.Hkv;
-  f.few = heads * ((rows + 127) / 128) < 128;
+  f.few = rows <= 32 || heads * ((rows + 127) / 128) < 128;
   f.tiles = (int)(f.few ? (rows + 31) / 32 : (rows + 127) / 128);
   f.splits = 1;
   if (f.few) {

@@ -48,7 +48,7 @@ __device__ __forceinline__ void store4(T *row, int d, int D, bool whole, float a
 // dq
 // ---------------------------------------------------------------------------
 template <class T, int DP>
-__global__ __launch_bounds__(256) void attend_dq(const dconv_attend_shape sh, const AttendPtrs p, const GradTile gt) {
+__global__ __launch_bounds__(256, 2) void attend_dq(const dconv_attend_shape sh, const AttendPtrs p, const GradTile gt) {
   constexpr int BN = forward_keys<T>(DP), KS = DP / 16, DT = DP / 32;
   typedef typename Mma<T>::Frag Frag;
   __shared__ __align__(16) T buf0[2 * BN * DP];
@@ -126,6 +126,7 @@ __global__ __launch_bounds__(256) void attend_dq(const dconv_attend_shape sh, co
         dp[i] = s[i] * (dp[i] - delta);
       }
       if (masked) {
+        no_speculation();
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
           const int v = v0 + 32 * hb + acc_row(i, half);
@@ -228,6 +229,7 @@ struct KeyGrad {
       dp[i] = s[i] * (dp[i] - x[1]);
     }
     if (masked) {
+      no_speculation();
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         const int x = r + acc_row(i, half);
@@ -290,7 +292,7 @@ constexpr int kGradKeys = 128;
 // 128 keys per workgroup, 32 per wave; tiles of 32 rows of queries and dout in two
 // LDS buffers, the next one copied while the current one is used.
 template <class T, int DP>
-__global__ __launch_bounds__(256) void attend_dkv(const dconv_attend_shape sh, const AttendPtrs p, const GradTile gt) {
+__global__ __launch_bounds__(256, 2) void attend_dkv(const dconv_attend_shape sh, const AttendPtrs p, const GradTile gt) {
   constexpr int DT = DP / 32, kTile = 32 * DP;
   __shared__ __align__(16) T buf0[2 * kTile];
   __shared__ __align__(16) T buf1[2 * kTile];

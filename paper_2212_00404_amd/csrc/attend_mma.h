@@ -169,6 +169,10 @@ __device__ __forceinline__ float half_sum(float x) {
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
+// Keeps a branch a branch: the compiler would otherwise run a rare block's
+// arithmetic every time and select.
+__device__ __forceinline__ void no_speculation() { asm volatile(""); }
+
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
 // What the host hands to the tile kernels beside the shape.
@@ -237,6 +241,7 @@ struct Softmax {
       for (int k = 0; k < KS; ++k) s[hb] = Mma<T>::mac(Tile<T, DP>::row(ks, 32 * hb, k, lane), q[k], s[hb]);
     }
     if (masked) {
+      no_speculation();
 #pragma unroll
       for (int hb = 0; hb < HB; ++hb)
 #pragma unroll
@@ -256,6 +261,7 @@ struct Softmax {
     // 2^8: sums and probabilities stay below 2^8 times their true size, and the
     // rescaling of the result is rare.
     if (__any(top - m > 8.0f)) {
+      no_speculation();
       const float to = fmaxf(m, top);
       const float keep = to == -INFINITY ? 1.0f : exp2f(m - to);
 #pragma unroll
@@ -293,7 +299,7 @@ constexpr int kForwardRows = 128;
 // 128 rows per workgroup, 32 per wave; tiles of BN keys and values in two LDS
 // buffers, the next one copied while the current one is used.
 template <class T, int DP>
-__global__ __launch_bounds__(256) void attend_tiles(const dconv_attend_shape sh, const AttendPtrs p,
+__global__ __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1) void attend_tiles(const dconv_attend_shape sh, const AttendPtrs p,
                                                     const AttendTile at) {
   constexpr int BN = forward_keys<T>(DP), KS = DP / 16, DT = DP / 32;
   __shared__ __align__(16) T buf0[2 * BN * DP];
