@@ -186,7 +186,7 @@ __device__ void attend_row_dkv(const dconv_attend_shape &sh, const AttendPtrs &p
 // `splits` workgroups (attend_split), else 128 rows per workgroup
 // (attend_tiles).
 struct ForwardPlan {
-  bool few, direct;
+  bool few, direct, near;
   int dp;              // head size the kernels are built for
   int tiles, splits;   // tiles of rows per key head, parts of the keys
   int64_t workspace;   // bytes
@@ -203,7 +203,7 @@ void launch_attend(const dconv_attend_shape &sh, const AttendPtrs &p, const Forw
 // (attend_dkv_split), of the others by tiles of 128 (attend_dkv).
 constexpr int kGradMaxD = 128;
 struct BackwardPlan {
-  bool direct;
+  bool direct, near;
   int dp;
   int row_tiles, key_tiles;
   int first, first_tiles, parts;

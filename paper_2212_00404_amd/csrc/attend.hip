@@ -57,6 +57,13 @@ bool whole_pieces(const void *p, const long long *stride, const dconv_attend_sha
          stride[2] % unit == 0;
 }
 
+// Whether 64 consecutive rows, of a head or of a group of heads, span less than
+// 2^31 bytes.
+bool close_rows(const long long *stride, const dconv_attend_shape &sh) {
+  const long long most = (1ll << 31) / element_size(sh.dtype) / 64 / (sh.Hq / sh.Hkv) - sh.D;
+  return stride[1] >= 0 && stride[2] >= 0 && stride[1] < most && stride[2] < most;
+}
+
 int padded_head(int D) { return D <= 32 ? 32 : D <= 64 ? 64 : D <= 96 ? 96 : D <= 128 ? 128 : 256; }
 
 // The most keys that a tile of `queries` queries sees (lengths are on the device).
@@ -158,6 +165,7 @@ DCONV_EXPORT int dconv_attend(const dconv_attend_shape *shape, const void *q, co
   ForwardPlan plan = plan_forward(*shape);
   plan.direct = whole_pieces(q, shape->q_stride, *shape) && whole_pieces(k, shape->k_stride, *shape) &&
                 whole_pieces(v, shape->v_stride, *shape) && whole_pieces(out, shape->out_stride, *shape);
+  plan.near = plan.direct && close_rows(shape->k_stride, *shape) && close_rows(shape->v_stride, *shape);
   (void)hipGetLastError();  // report this launch only
   by_type(shape->dtype, [&](auto *t) {
     launch_attend<std::remove_pointer_t<decltype(t)>>(*shape, p, plan, (float *)workspace, (hipStream_t)stream);
@@ -199,6 +207,8 @@ DCONV_EXPORT int dconv_attend_backward(const dconv_attend_shape *shape, const vo
                 whole_pieces(v, shape->v_stride, *shape) && whole_pieces(out, shape->out_stride, *shape) &&
                 whole_pieces(dout, shape->dout_stride, *shape) && whole_pieces(dq, dense, *shape) &&
                 whole_pieces(dk, dense, *shape) && whole_pieces(dv, dense, *shape);
+  plan.near = plan.direct && close_rows(shape->q_stride, *shape) && close_rows(shape->k_stride, *shape) &&
+              close_rows(shape->v_stride, *shape) && close_rows(shape->dout_stride, *shape);
   (void)hipGetLastError();  // report this launch only
   by_type(shape->dtype, [&](auto *t) {
     using T = std::remove_pointer_t<decltype(t)>;

@@ -75,15 +75,8 @@ __global__ __launch_bounds__(256, 2) void attend_dq(const dconv_attend_shape sh,
   }
   from = uniform(from), to = uniform(to), all_from = uniform(all_from), all_to = uniform(all_to);
 
-  const T *kh = row_of<T>(p.k, sh.k_stride, b, 0, hk), *vh = row_of<T>(p.v, sh.v_stride, b, 0, hk);
-  auto stage = [&](T *buf, int v0) {
-    auto from_row = [&](const T *base, long long stride) {
-      return [=](int x) { return base + (int64_t)keys.key(min(v0 + x, n - 1)) * stride; };
-    };
-    Tile<T, DP>::template stage<BN, 256>(buf, sh.D, at.direct, threadIdx.x, from_row(kh, sh.k_stride[1]));
-    Tile<T, DP>::template stage<BN, 256>(buf + BN * DP, sh.D, at.direct, threadIdx.x,
-                                         from_row(vh, sh.v_stride[1]));
-  };
+  const KeyTiles<T, DP, BN, 4> tiles(sh, p, b, hk, wave, lane);
+  auto stage = [&](T *buf, int v0) { tiles.stage(buf, at, keys, n, v0, sh.D, wave, lane); };
   if (n > 0) stage(buf0, 0);
 
   Frag q[KS], g[KS];
@@ -287,6 +280,60 @@ __device__ __forceinline__ void stage_stats(f32x2 *lds, const f32x2 *stats, int 
   __builtin_amdgcn_global_load_lds(from, (lds_ptr)lds, 4, 0, 0);
 }
 
+// Tiles of 32 rows of queries and dout, in this order, and the rows' statistics.
+template <class T, int DP, int NW>
+struct RowTiles {
+  typedef Copy<T, DP, 32, NW> C;
+  C cq, cg;
+  const T *q, *g;
+  const f32x2 *stats;
+  int G;
+  bool near;
+
+  __device__ __forceinline__ RowTiles(const dconv_attend_shape &sh, const AttendPtrs &p, const GradTile &gt, int b,
+                                      int hk, int wave, int lane)
+      : q(row_of<T>(p.q, sh.q_stride, b, 0, (int64_t)hk * (sh.Hq / sh.Hkv))),
+        g(row_of<T>(p.dout, sh.dout_stride, b, 0, (int64_t)hk * (sh.Hq / sh.Hkv))),
+        stats(gt.stats + ((int64_t)b * sh.Hkv + hk) * sh.Tq * (sh.Hq / sh.Hkv)), G(sh.Hq / sh.Hkv) {
+    // a tile begins with the first head of a group: with a power of two of them
+    // every tile's rows lie alike
+    near = gt.a.near && (C::kStep ? C::kStep : 32) % G == 0;
+    auto offset = [&](const long long *stride) {
+      const uint32_t t = (uint32_t)stride[1], h = (uint32_t)stride[2];
+      return [=](int r) { return ((uint32_t)(r / G) * t + (uint32_t)(r % G) * h) * (uint32_t)sizeof(T); };
+    };
+    if (near) {
+      cq.init(sh.D, wave, lane, offset(sh.q_stride));
+      cg.init(sh.D, wave, lane, offset(sh.dout_stride));
+    }
+  }
+  // Rows r .. (the first of a head group if `near`); past `to` the last one.
+  __device__ __forceinline__ void stage(T *lds, f32x2 *st, const dconv_attend_shape &sh, bool direct, int r, int to,
+                                        int wave, int lane) const {
+    if (wave == 0) stage_stats(st, stats, r, to, lane);
+    if (near && r + 32 <= to) {
+      const int64_t t = r / G;
+      cq.tile(lds, q + t * sh.q_stride[1], C::kStep / G * sh.q_stride[1] * (int64_t)sizeof(T), wave);
+      cg.tile(lds + 32 * DP, g + t * sh.dout_stride[1], C::kStep / G * sh.dout_stride[1] * (int64_t)sizeof(T), wave);
+      return;
+    }
+    auto from = [&](const T *base, const long long *stride) {
+      const int64_t by_t = stride[1], by_h = stride[2];
+      return [=](int x) {
+        const int y = min(r + x, to - 1);
+        return base + y / G * by_t + y % G * by_h;
+      };
+    };
+    if (direct) {
+      C::rows(lds, sh.D, wave, lane, from(q, sh.q_stride));
+      C::rows(lds + 32 * DP, sh.D, wave, lane, from(g, sh.dout_stride));
+    } else {
+      C::elements(lds, sh.D, wave, lane, from(q, sh.q_stride));
+      C::elements(lds + 32 * DP, sh.D, wave, lane, from(g, sh.dout_stride));
+    }
+  }
+};
+
 constexpr int kGradKeys = 128;
 
 // 128 keys per workgroup, 32 per wave; tiles of 32 rows of queries and dout in two
@@ -304,7 +351,7 @@ __global__ __launch_bounds__(256, 2) void attend_dkv(const dconv_attend_shape sh
   const AttendTile &at = gt.a;
   const int lane = threadIdx.x & 63, half = lane >> 5, wave = uniform(threadIdx.x >> 6);
   const int id = xcd_remap(blockIdx.x, gridDim.x);
-  const int bh = id / at.tiles, b = bh / sh.Hkv, hk = bh % sh.Hkv, G = sh.Hq / sh.Hkv;
+  const int bh = id / at.tiles, b = bh / sh.Hkv, hk = bh % sh.Hkv;
   const int j = (id % at.tiles) * kGradKeys + 32 * wave + (lane & 31), jj = min(j, sh.Tk - 1);
   const Seq seq = seq_of(sh, p, b);
   const KeyRows see = key_rows(sh, seq, j, gt.first, sh.Tk);
@@ -317,18 +364,8 @@ __global__ __launch_bounds__(256, 2) void attend_dkv(const dconv_attend_shape sh
   const int from = uniform(min(min(span[0][0], span[0][1]), min(span[0][2], span[0][3])));
   const int to = uniform(max(max(span[1][0], span[1][1]), max(span[1][2], span[1][3])));
 
-  auto stage = [&](T *buf, f32x2 *st, int r) {
-    auto from_row = [&](const void *base, const long long *stride) {
-      return [=](int x) {
-        const int y = min(r + x, to - 1);
-        return row_of<T>(base, stride, b, y / G, hk * G + y % G);
-      };
-    };
-    Tile<T, DP>::template stage<32, 256>(buf, sh.D, at.direct, threadIdx.x, from_row(p.q, sh.q_stride));
-    Tile<T, DP>::template stage<32, 256>(buf + kTile, sh.D, at.direct, threadIdx.x,
-                                         from_row(p.dout, sh.dout_stride));
-    if (wave == 0) stage_stats(st, gt.stats + (int64_t)bh * sh.Tq * G, r, to, lane);
-  };
+  const RowTiles<T, DP, 4> tiles(sh, p, gt, b, hk, wave, lane);
+  auto stage = [&](T *buf, f32x2 *st, int r) { tiles.stage(buf, st, sh, at.direct, r, to, wave, lane); };
   if (from < to) stage(buf0, stats0, from);
   KeyGrad<T, DP> acc;
   acc.load(sh, at, row_of<T>(p.k, sh.k_stride, b, jj, hk), row_of<T>(p.v, sh.v_stride, b, jj, hk), half);
@@ -395,23 +432,15 @@ __global__ __launch_bounds__(64 * split_waves<T>(DP)) void attend_dkv_split(cons
   const AttendTile &at = gt.a;
   const int lane = threadIdx.x & 63, half = lane >> 5, wave = uniform(threadIdx.x >> 6);
   const int part = blockIdx.x % gt.parts, id = blockIdx.x / gt.parts;
-  const int bh = id / at.tiles, b = bh / sh.Hkv, hk = bh % sh.Hkv, G = sh.Hq / sh.Hkv;
+  const int bh = id / at.tiles, b = bh / sh.Hkv, hk = bh % sh.Hkv;
   const int j0 = (id % at.tiles) * 32, j = j0 + (lane & 31), jj = min(j, sh.Tk - 1);
   const Seq seq = seq_of(sh, p, b);
   const KeyRows see = key_rows(sh, seq, j, 0, gt.first);
   const TileRows mine = tile_rows(see);
 
+  const RowTiles<T, DP, 1> tiles(sh, p, gt, b, hk, 0, lane);
   auto stage = [&](T *buf, f32x2 *st, int r) {
-    auto from_row = [&](const void *base, const long long *stride) {
-      return [=](int x) {
-        const int y = min(r + x, mine.to - 1);
-        return row_of<T>(base, stride, b, y / G, hk * G + y % G);
-      };
-    };
-    T *to = buf + wave * 2 * kTile;
-    Tile<T, DP>::template stage<32, 64>(to, sh.D, at.direct, lane, from_row(p.q, sh.q_stride));
-    Tile<T, DP>::template stage<32, 64>(to + kTile, sh.D, at.direct, lane, from_row(p.dout, sh.dout_stride));
-    stage_stats(st + wave * 32, gt.stats + (int64_t)bh * sh.Tq * G, r, mine.to, lane);
+    tiles.stage(buf + wave * 2 * kTile, st + wave * 32, sh, at.direct, r, mine.to, 0, lane);
   };
   KeyGrad<T, DP> acc;
   acc.load(sh, at, row_of<T>(p.k, sh.k_stride, b, jj, hk), row_of<T>(p.v, sh.v_stride, b, jj, hk), half);
@@ -493,7 +522,7 @@ template <class T>
 void launch_attend_grad(const dconv_attend_shape &sh, const AttendPtrs &p, const BackwardPlan &plan, void *workspace,
                         hipStream_t s) {
   GradTile gt = {};
-  gt.a = attend_tile(sh, plan.direct);
+  gt.a = attend_tile(sh, plan.direct, plan.near);
   gt.stats = (f32x2 *)workspace;
   gt.a.partial = (float *)((char *)workspace + plan.stats_bytes);
   gt.first = plan.first;

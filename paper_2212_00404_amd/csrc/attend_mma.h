@@ -106,31 +106,68 @@ struct Tile {
     return f;
   }
 
-  // NR rows of D elements from row_start(r) into LDS by the NT threads of a
-  // workgroup or wave (`me`: the thread's number).  direct: the rows are whole
-  // 16-byte pieces on 4-byte boundaries, copied without a register; a piece past
-  // D repeats the row's first (its products meet zeros).  Otherwise element by
-  // element, zeros past D.
-  template <int NR, int NT, class F>
-  static __device__ __forceinline__ void stage(T *lds, int D, bool direct, int me, F row_start) {
-    constexpr int kPer = 16 / sizeof(T), kPieces = DP / kPer;
-    if (direct) {
-      static_assert(NR * kPieces % 64 == 0, "whole waves");
+};
+
+// Copies of NR rows of D elements into a Tile by NW waves.
+template <class T, int DP, int NR, int NW>
+struct Copy {
+  static constexpr int kPer = 16 / sizeof(T), kPieces = DP / kPer, kThreads = 64 * NW;
+  static constexpr int kCopies = (NR * kPieces + kThreads - 1) / kThreads;   // per wave
+  static_assert(NR * kPieces % 64 == 0, "whole waves");
+  // Rows between a lane's copies, where they are in the same place of a row.
+  static constexpr int kStep = kThreads % (8 * kPieces) == 0 ? kThreads / kPieces : 0;
+  uint32_t offset[kStep ? 1 : kCopies];   // of the lane's pieces from the tile's first row, in bytes
+
+  // Row and element of the lane's piece in copy i.  A piece past D repeats the
+  // row's first (its products meet zeros).
+  static __device__ __forceinline__ int row(int i, int wave, int lane) { return (i * kThreads + 64 * wave + lane) / kPieces; }
+  static __device__ __forceinline__ int element(int i, int wave, int lane, int D) {
+    const int piece = (i * kThreads + 64 * wave + lane) % kPieces;
+    const int e = ((piece * kPer / 8) ^ Tile<T, DP>::swizzle(row(i, wave, lane))) * 8 + piece * kPer % 8;
+    return e < D ? e : 0;
+  }
+  static __device__ __forceinline__ bool has(int i, int wave) {
+    return NR * kPieces % kThreads == 0 || i * kThreads + 64 * wave < NR * kPieces;
+  }
+  static __device__ __forceinline__ T *to(T *lds, int i, int wave) {   // lane l lands 16 l bytes on
+    return lds + (i * kThreads + 64 * wave) * kPer;
+  }
+
+  // byte_offset(r): of row r from the tile's first, in 32 bits.
+  template <class F>
+  __device__ __forceinline__ void init(int D, int wave, int lane, F byte_offset) {
 #pragma unroll
-      for (int i = 0; i < (NR * kPieces + NT - 1) / NT; ++i) {
-        if (NR * kPieces % NT != 0 && i * NT + (me & ~63) >= NR * kPieces) break;
-        const int slot = i * NT + me, r = slot / kPieces, piece = slot % kPieces;
-        int e = ((piece * kPer / 8) ^ swizzle(r)) * 8 + piece * kPer % 8;
-        e = e < D ? e : 0;
-        // the wave's part of LDS is contiguous: lane l lands 16 l bytes on
-        __builtin_amdgcn_global_load_lds(row_start(r) + e, (lds_ptr)(lds + (i * NT + (me & ~63)) * kPer), 16,
-                                         0, 0);
-      }
-    } else {
-      for (int x = me; x < NR * DP; x += NT) {
-        const int r = x / DP, d = x % DP;
-        lds[at(r, d >> 3) + (d & 7)] = d < D ? row_start(r)[d] : from_f32<T>(0.0f);
-      }
+    for (int i = 0; i < (kStep ? 1 : kCopies); ++i)
+      offset[i] = byte_offset(row(i, wave, lane)) + element(i, wave, lane, D) * (uint32_t)sizeof(T);
+  }
+  // The rows as init has described them, from `first`; row r + kStep is `step`
+  // bytes after row r.  One instruction per copy: a scalar base and a 32-bit offset.
+  __device__ __forceinline__ void tile(T *lds, const T *first, int64_t step, int wave) const {
+#pragma unroll
+    for (int i = 0; i < kCopies; ++i) {
+      if (!has(i, wave)) break;
+      uint32_t o = offset[kStep ? 0 : i];
+      asm volatile("" : "+v"(o));
+      const char *base = reinterpret_cast<const char *>(first) + (kStep ? i * step : 0);
+      __builtin_amdgcn_global_load_lds(base + o, (lds_ptr)to(lds, i, wave), 16, 0, 0);
+    }
+  }
+  // Any rows: row_start(r) is where row r begins.
+  template <class F>
+  static __device__ __forceinline__ void rows(T *lds, int D, int wave, int lane, F row_start) {
+#pragma unroll
+    for (int i = 0; i < kCopies; ++i) {
+      if (!has(i, wave)) break;
+      __builtin_amdgcn_global_load_lds(row_start(row(i, wave, lane)) + element(i, wave, lane, D),
+                                       (lds_ptr)to(lds, i, wave), 16, 0, 0);
+    }
+  }
+  // Rows that are not whole 16-byte pieces: element by element, zeros past D.
+  template <class F>
+  static __device__ __forceinline__ void elements(T *lds, int D, int wave, int lane, F row_start) {
+    for (int x = 64 * wave + lane; x < NR * DP; x += kThreads) {
+      const int r = x / DP, d = x % DP;
+      lds[Tile<T, DP>::at(r, d >> 3) + (d & 7)] = d < D ? row_start(r)[d] : from_f32<T>(0.0f);
     }
   }
 };
@@ -180,6 +217,7 @@ struct AttendTile {
   float scale2;   // |scale| / ln 2: the softmax is taken in powers of two
   float sign;     // of the scale, taken into the queries; 0: every score is 0
   bool direct;    // rows can be copied in 16-byte pieces
+  bool near;      // and 64 of them span less than 2^31 bytes
   int tiles;      // tiles of rows per key head
   int splits;     // parts of the keys (attend_split)
   float *partial; // their sums
@@ -196,11 +234,48 @@ __device__ __forceinline__ Keys keys_of(const dconv_attend_shape &sh, const Seq 
   Keys k = {0, 0, 0};
   if (s.start + t1 < 0) return k;
   const Span a = span_of(sh, s, max((int64_t)0, s.start + t0)), b = span_of(sh, s, s.start + t1);
-  k.first = a.first;
-  k.off = a.lo - a.first;
-  k.n = b.hi - k.off;
+  k.first = uniform(a.first);
+  k.off = uniform(a.lo - a.first);
+  k.n = uniform(b.hi - k.off);
   return k;
 }
+// Tiles of keys and values, in this order, of one key head.
+template <class T, int DP, int BN, int NW>
+struct KeyTiles {
+  Copy<T, DP, BN, NW> ck, cv;
+  const T *k, *v;
+  int64_t k_stride, v_stride;
+
+  __device__ __forceinline__ KeyTiles(const dconv_attend_shape &sh, const AttendPtrs &p, int b, int hk, int wave,
+                                      int lane)
+      : k(row_of<T>(p.k, sh.k_stride, b, 0, hk)), v(row_of<T>(p.v, sh.v_stride, b, 0, hk)),
+        k_stride(sh.k_stride[1]), v_stride(sh.v_stride[1]) {
+    ck.init(sh.D, wave, lane, [&](int r) { return (uint32_t)r * (uint32_t)k_stride * (uint32_t)sizeof(T); });
+    cv.init(sh.D, wave, lane, [&](int r) { return (uint32_t)r * (uint32_t)v_stride * (uint32_t)sizeof(T); });
+  }
+  // Keys v0 .. of the n of `keys`; past the last one it is repeated.
+  __device__ __forceinline__ void stage(T *lds, const AttendTile &at, const Keys &keys, int n, int v0, int D, int wave,
+                                        int lane) const {
+    typedef Copy<T, DP, BN, NW> C;
+    if (at.near && v0 + BN <= n && (v0 >= keys.first || keys.off == 0)) {
+      const int64_t j = v0 + keys.off;
+      ck.tile(lds, k + j * k_stride, C::kStep * k_stride * (int64_t)sizeof(T), wave);
+      cv.tile(lds + BN * DP, v + j * v_stride, C::kStep * v_stride * (int64_t)sizeof(T), wave);
+      return;
+    }
+    auto from = [&](const T *base, int64_t stride) {
+      return [=](int r) { return base + (int64_t)keys.key(min(v0 + r, n - 1)) * stride; };
+    };
+    if (at.direct) {
+      C::rows(lds, D, wave, lane, from(k, k_stride));
+      C::rows(lds + BN * DP, D, wave, lane, from(v, v_stride));
+    } else {
+      C::elements(lds, D, wave, lane, from(k, k_stride));
+      C::elements(lds + BN * DP, D, wave, lane, from(v, v_stride));
+    }
+  }
+};
+
 // Row at position i sees v < hi with v >= lo or v < sinks.
 struct RowKeys {
   int lo, hi;
@@ -333,15 +408,8 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1) void attend_til
 #pragma unroll
   for (int k = 0; k < KS; ++k) q[k] = load_frag(qrow, 16 * k + 8 * (lane >> 5), sh.D, at.direct, at.sign);
 
-  const T *kh = row_of<T>(p.k, sh.k_stride, b, 0, hk), *vh = row_of<T>(p.v, sh.v_stride, b, 0, hk);
-  auto stage = [&](T *buf, int v0) {
-    auto from_row = [&](const T *base, long long stride) {
-      return [=](int x) { return base + (int64_t)keys.key(min(v0 + x, n - 1)) * stride; };
-    };
-    Tile<T, DP>::template stage<BN, 256>(buf, sh.D, at.direct, threadIdx.x, from_row(kh, sh.k_stride[1]));
-    Tile<T, DP>::template stage<BN, 256>(buf + BN * DP, sh.D, at.direct, threadIdx.x,
-                                         from_row(vh, sh.v_stride[1]));
-  };
+  const KeyTiles<T, DP, BN, 4> tiles(sh, p, b, hk, wave, lane);
+  auto stage = [&](T *buf, int v0) { tiles.stage(buf, at, keys, n, v0, sh.D, wave, lane); };
   Softmax<T, DP> soft;
   soft.clear();
   auto step = [&](const T *buf, int v0) {
@@ -479,15 +547,8 @@ __global__ __launch_bounds__(64 * split_waves<T>(DP)) void attend_split(const dc
 #pragma unroll
   for (int k = 0; k < KS; ++k) q[k] = load_frag(qrow, 16 * k + 8 * (lane >> 5), sh.D, at.direct, at.sign);
 
-  const T *kh = row_of<T>(p.k, sh.k_stride, b, 0, hk), *vh = row_of<T>(p.v, sh.v_stride, b, 0, hk);
-  auto stage = [&](T *buf, int v0) {
-    auto from_row = [&](const T *base, long long stride) {
-      return [=](int x) { return base + (int64_t)keys.key(min(v0 + x, n - 1)) * stride; };
-    };
-    T *mine = buf + wave * 2 * kTile;
-    Tile<T, DP>::template stage<32, 64>(mine, sh.D, at.direct, lane, from_row(kh, sh.k_stride[1]));
-    Tile<T, DP>::template stage<32, 64>(mine + kTile, sh.D, at.direct, lane, from_row(vh, sh.v_stride[1]));
-  };
+  const KeyTiles<T, DP, 32, 1> tiles(sh, p, b, hk, 0, lane);
+  auto stage = [&](T *buf, int v0) { tiles.stage(buf + wave * 2 * kTile, at, keys, n, v0, sh.D, 0, lane); };
   Softmax<T, DP> soft;
   soft.clear();
   auto step = [&](const T *buf, int v0) {
@@ -585,18 +646,19 @@ void by_width(int dp, F f) {
   return f(std::integral_constant<int, 256>());
 }
 
-inline AttendTile attend_tile(const dconv_attend_shape &sh, bool direct) {
+inline AttendTile attend_tile(const dconv_attend_shape &sh, bool direct, bool near) {
   AttendTile at = {};
   at.scale2 = sh.scale == 0.0f ? 1.0f : fabsf(sh.scale) * 1.4426950408889634f;
   at.sign = sh.scale > 0.0f ? 1.0f : sh.scale < 0.0f ? -1.0f : 0.0f;
   at.direct = direct;
+  at.near = near;
   return at;
 }
 
 template <class T>
 void launch_attend(const dconv_attend_shape &sh, const AttendPtrs &p, const ForwardPlan &plan, float *workspace,
                    hipStream_t s) {
-  AttendTile at = attend_tile(sh, plan.direct);
+  AttendTile at = attend_tile(sh, plan.direct, plan.near);
   at.tiles = plan.tiles;
   at.splits = plan.splits;
   at.partial = workspace;
