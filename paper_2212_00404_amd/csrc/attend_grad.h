@@ -48,7 +48,7 @@ __device__ __forceinline__ void store4(T *row, int d, int D, bool whole, float a
 // dq
 // ---------------------------------------------------------------------------
 template <class T, int DP>
-__global__ __launch_bounds__(256, 2) void attend_dq(const dconv_attend_shape sh, const AttendPtrs p, const GradTile gt) {
+__global__ __launch_bounds__(256, DP * sizeof(T) <= 128 ? 2 : 1) void attend_dq(const dconv_attend_shape sh, const AttendPtrs p, const GradTile gt) {
   constexpr int BN = forward_keys<T>(DP), KS = DP / 16, DT = DP / 32;
   typedef typename Mma<T>::Frag Frag;
   __shared__ __align__(16) T buf0[2 * BN * DP];
@@ -120,13 +120,10 @@ __global__ __launch_bounds__(256, 2) void attend_dq(const dconv_attend_shape sh,
       }
       if (masked) {
         no_speculation();
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int v = v0 + 32 * hb + acc_row(i, half);
-          const bool on = v < see.hi && (v >= see.lo || v < sh.sinks);
+        seen_keys(v0 + 32 * hb, see, sh.sinks, lane, [&](int i, bool on) {
           s[i] = on ? s[i] : 0.0f;
           dp[i] = on ? dp[i] : 0.0f;
-        }
+        });
       }
 #pragma unroll
       for (int i = 0; i < 16; ++i) miss += dp[i];
@@ -223,13 +220,10 @@ struct KeyGrad {
     }
     if (masked) {
       no_speculation();
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const int x = r + acc_row(i, half);
-        const bool on = x >= lo && x < hi;
+      within(lo - r, hi - r, half, [&](int i, bool on) {
         s[i] = on ? s[i] : 0.0f;
         dp[i] = on ? dp[i] : 0.0f;
-      }
+      });
     }
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
@@ -280,41 +274,49 @@ __device__ __forceinline__ void stage_stats(f32x2 *lds, const f32x2 *stats, int 
   __builtin_amdgcn_global_load_lds(from, (lds_ptr)lds, 4, 0, 0);
 }
 
-// Tiles of 32 rows of queries and dout, in this order, and the rows' statistics.
-template <class T, int DP, int NW>
+// Tiles of NR rows of queries and dout, in this order, and the rows' statistics.
+template <class T, int DP, int NR, int NW>
 struct RowTiles {
-  typedef Copy<T, DP, 32, NW> C;
+  typedef Copy<T, DP, NR, NW> C;
   C cq, cg;
   const T *q, *g;
   const f32x2 *stats;
   int G;
-  bool near;
+  bool near, alike;   // alike: every tile's rows lie as the first one's do
 
   __device__ __forceinline__ RowTiles(const dconv_attend_shape &sh, const AttendPtrs &p, const GradTile &gt, int b,
                                       int hk, int wave, int lane)
       : q(row_of<T>(p.q, sh.q_stride, b, 0, (int64_t)hk * (sh.Hq / sh.Hkv))),
         g(row_of<T>(p.dout, sh.dout_stride, b, 0, (int64_t)hk * (sh.Hq / sh.Hkv))),
         stats(gt.stats + ((int64_t)b * sh.Hkv + hk) * sh.Tq * (sh.Hq / sh.Hkv)), G(sh.Hq / sh.Hkv) {
-    // a tile begins with the first head of a group: with a power of two of them
-    // every tile's rows lie alike
-    near = gt.a.near && (C::kStep ? C::kStep : 32) % G == 0;
-    auto offset = [&](const long long *stride) {
-      const uint32_t t = (uint32_t)stride[1], h = (uint32_t)stride[2];
-      return [=](int r) { return ((uint32_t)(r / G) * t + (uint32_t)(r % G) * h) * (uint32_t)sizeof(T); };
-    };
-    if (near) {
-      cq.init(sh.D, wave, lane, offset(sh.q_stride));
-      cg.init(sh.D, wave, lane, offset(sh.dout_stride));
+    near = gt.a.near && G <= 128;
+    // walks begin with the first head of a group
+    alike = near && NR % G == 0 && (C::kStep ? C::kStep : NR) % G == 0;
+    if (alike) {
+      cq.init(sh.D, wave, lane, [&](int r) { return offset(r, 0, sh.q_stride); });
+      cg.init(sh.D, wave, lane, [&](int r) { return offset(r, 0, sh.dout_stride); });
     }
   }
-  // Rows r .. (the first of a head group if `near`); past `to` the last one.
+  // Of row r of a tile that begins with head g0 of a group, in bytes.  (The
+  // quotient by a product: exact while (r + g0) G < 2^16.)
+  __device__ __forceinline__ uint32_t offset(int r, int g0, const long long *stride) const {
+    const uint32_t v = r + g0, t = v * (65536u / G + 1) >> 16;
+    return (t * (uint32_t)stride[1] + (v - t * G) * (uint32_t)stride[2]) * (uint32_t)sizeof(T);
+  }
+  // Rows r ..; past `to` the last one.
   __device__ __forceinline__ void stage(T *lds, f32x2 *st, const dconv_attend_shape &sh, bool direct, int r, int to,
                                         int wave, int lane) const {
-    if (wave == 0) stage_stats(st, stats, r, to, lane);
-    if (near && r + 32 <= to) {
-      const int64_t t = r / G;
-      cq.tile(lds, q + t * sh.q_stride[1], C::kStep / G * sh.q_stride[1] * (int64_t)sizeof(T), wave);
-      cg.tile(lds + 32 * DP, g + t * sh.dout_stride[1], C::kStep / G * sh.dout_stride[1] * (int64_t)sizeof(T), wave);
+    if (wave < NR / 32) stage_stats(st + 32 * wave, stats, r + 32 * wave, to, lane);
+    if (near && r + NR <= to) {
+      const int t = r / G, g0 = r - t * G;
+      const T *qt = q + t * sh.q_stride[1], *dt = g + t * sh.dout_stride[1];
+      if (alike) {
+        cq.tile(lds, qt, C::kStep / G * sh.q_stride[1] * (int64_t)sizeof(T), wave);
+        cg.tile(lds + NR * DP, dt, C::kStep / G * sh.dout_stride[1] * (int64_t)sizeof(T), wave);
+      } else {
+        C::tile_at(lds, qt, sh.D, wave, lane, [&](int x) { return offset(x, g0, sh.q_stride); });
+        C::tile_at(lds + NR * DP, dt, sh.D, wave, lane, [&](int x) { return offset(x, g0, sh.dout_stride); });
+      }
       return;
     }
     auto from = [&](const T *base, const long long *stride) {
@@ -326,66 +328,99 @@ struct RowTiles {
     };
     if (direct) {
       C::rows(lds, sh.D, wave, lane, from(q, sh.q_stride));
-      C::rows(lds + 32 * DP, sh.D, wave, lane, from(g, sh.dout_stride));
+      C::rows(lds + NR * DP, sh.D, wave, lane, from(g, sh.dout_stride));
     } else {
       C::elements(lds, sh.D, wave, lane, from(q, sh.q_stride));
-      C::elements(lds + 32 * DP, sh.D, wave, lane, from(g, sh.dout_stride));
+      C::elements(lds + NR * DP, sh.D, wave, lane, from(g, sh.dout_stride));
     }
   }
 };
 
 constexpr int kGradKeys = 128;
 
-// 128 keys per workgroup, 32 per wave; tiles of 32 rows of queries and dout in two
-// LDS buffers, the next one copied while the current one is used.
+// 128 keys per workgroup, 32 per wave; tiles of 32 rows of queries and dout for
+// each row group in two LDS buffers, the next ones copied while the current ones
+// are used.  With two row groups of four waves each, a workgroup alone on its
+// compute unit (256 of them at 2 x 4096 keys and four key heads) has two waves per
+// SIMD to fill each other's waits; the second's sums are added to the first's at
+// the end.  Larger heads leave registers for one.
+template <class T>
+constexpr int row_groups(int dp) { return dp * (int)sizeof(T) <= 192 ? 2 : 1; }
+
 template <class T, int DP>
-__global__ __launch_bounds__(256, 2) void attend_dkv(const dconv_attend_shape sh, const AttendPtrs p, const GradTile gt) {
-  constexpr int DT = DP / 32, kTile = 32 * DP;
-  __shared__ __align__(16) T buf0[2 * kTile];
-  __shared__ __align__(16) T buf1[2 * kTile];
-  __shared__ __align__(16) f32x2 stats0[32];
-  __shared__ __align__(16) f32x2 stats1[32];
+__global__ __launch_bounds__(256 * row_groups<T>(DP)) void attend_dkv(const dconv_attend_shape sh, const AttendPtrs p,
+                                                                      const GradTile gt) {
+  constexpr int RG = row_groups<T>(DP), BM = 32 * RG, DT = DP / 32;
+  constexpr int kBuf = RG > 1 && 2 * BM * DP * sizeof(T) < 16384 ? 16384 / (int)sizeof(T) : 2 * BM * DP;
+  __shared__ __align__(16) T buf0[kBuf];
+  __shared__ __align__(16) T buf1[kBuf];
+  __shared__ __align__(16) f32x2 stats0[BM];
+  __shared__ __align__(16) f32x2 stats1[BM];
   __shared__ int span[2][4];
-  DCONV_POISON(poison_lds(buf0, 2 * kTile); poison_lds(buf1, 2 * kTile); poison_lds(stats0, 32);
-               poison_lds(stats1, 32));
+  DCONV_POISON(poison_lds(buf0, kBuf); poison_lds(buf1, kBuf); poison_lds(stats0, BM); poison_lds(stats1, BM));
   const AttendTile &at = gt.a;
   const int lane = threadIdx.x & 63, half = lane >> 5, wave = uniform(threadIdx.x >> 6);
+  const int kg = wave & 3, rg = wave >> 2;   // key group, row group
   const int id = xcd_remap(blockIdx.x, gridDim.x);
   const int bh = id / at.tiles, b = bh / sh.Hkv, hk = bh % sh.Hkv;
-  const int j = (id % at.tiles) * kGradKeys + 32 * wave + (lane & 31), jj = min(j, sh.Tk - 1);
+  const int j = (id % at.tiles) * kGradKeys + 32 * kg + (lane & 31), jj = min(j, sh.Tk - 1);
   const Seq seq = seq_of(sh, p, b);
   const KeyRows see = key_rows(sh, seq, j, gt.first, sh.Tk);
   const TileRows mine = tile_rows(see);
-  if (lane == 0) {
-    span[0][wave] = mine.from;
-    span[1][wave] = mine.to;
+  if (lane == 0 && rg == 0) {
+    span[0][kg] = mine.from;
+    span[1][kg] = mine.to;
   }
   __syncthreads();
   const int from = uniform(min(min(span[0][0], span[0][1]), min(span[0][2], span[0][3])));
   const int to = uniform(max(max(span[1][0], span[1][1]), max(span[1][2], span[1][3])));
 
-  const RowTiles<T, DP, 4> tiles(sh, p, gt, b, hk, wave, lane);
+  const RowTiles<T, DP, BM, 4 * RG> tiles(sh, p, gt, b, hk, wave, lane);
   auto stage = [&](T *buf, f32x2 *st, int r) { tiles.stage(buf, st, sh, at.direct, r, to, wave, lane); };
   if (from < to) stage(buf0, stats0, from);
   KeyGrad<T, DP> acc;
   acc.load(sh, at, row_of<T>(p.k, sh.k_stride, b, jj, hk), row_of<T>(p.v, sh.v_stride, b, jj, hk), half);
   auto step = [&](const T *buf, const f32x2 *st, int r) {
+    buf += 32 * rg * DP, st += 32 * rg, r += 32 * rg;
     if (r >= mine.to || r + 32 <= mine.from) return;
-    acc.add(buf, buf + kTile, st, r, see.lo, see.hi, !(r >= mine.all_from && r + 32 <= mine.all_to), at.scale2,
+    acc.add(buf, buf + BM * DP, st, r, see.lo, see.hi, !(r >= mine.all_from && r + 32 <= mine.all_to), at.scale2,
             lane);
   };
   auto arrived = [&]() {
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
     __syncthreads();
   };
-  for (int r = from; r < to; r += 64) {
+  for (int r = from; r < to; r += 2 * BM) {
     arrived();
-    if (r + 32 < to) stage(buf1, stats1, r + 32);
+    if (r + BM < to) stage(buf1, stats1, r + BM);
     step(buf0, stats0, r);
-    if (r + 32 >= to) break;
+    if (r + BM >= to) break;
     arrived();
-    if (r + 64 < to) stage(buf0, stats0, r + 64);
-    step(buf1, stats1, r + 32);
+    if (r + 2 * BM < to) stage(buf0, stats0, r + 2 * BM);
+    step(buf1, stats1, r + BM);
+  }
+  if constexpr (RG > 1) {
+    float *xk = reinterpret_cast<float *>(buf0) + kg * 1024, *xv = reinterpret_cast<float *>(buf1) + kg * 1024;
+#pragma unroll
+    for (int c = 0; c < DT; ++c) {
+      __syncthreads();   // every wave is done with what the buffers hold
+      if (rg == 1) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          xk[64 * i + lane] = acc.dk[c][i];
+          xv[64 * i + lane] = acc.dv[c][i];
+        }
+      }
+      __syncthreads();
+      if (rg == 0) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          acc.dk[c][i] += xk[64 * i + lane];
+          acc.dv[c][i] += xv[64 * i + lane];
+        }
+      }
+    }
+    if (rg == 1) return;
   }
 
   bool bad = false;
@@ -412,7 +447,7 @@ __global__ __launch_bounds__(256, 2) void attend_dkv(const dconv_attend_shape sh
       }
   }
   for (unsigned again = redo; again; again &= again - 1)
-    attend_row_dkv<T>(sh, p, b, hk, (id % at.tiles) * kGradKeys + 32 * wave + __ffs(again) - 1);
+    attend_row_dkv<T>(sh, p, b, hk, (id % at.tiles) * kGradKeys + 32 * kg + __ffs(again) - 1);
 }
 
 // Keys [0, gt.first) in tiles of 32: the first keys, which every row sees, or all
@@ -438,7 +473,7 @@ __global__ __launch_bounds__(64 * split_waves<T>(DP)) void attend_dkv_split(cons
   const KeyRows see = key_rows(sh, seq, j, 0, gt.first);
   const TileRows mine = tile_rows(see);
 
-  const RowTiles<T, DP, 1> tiles(sh, p, gt, b, hk, 0, lane);
+  const RowTiles<T, DP, 32, 1> tiles(sh, p, gt, b, hk, 0, lane);
   auto stage = [&](T *buf, f32x2 *st, int r) {
     tiles.stage(buf + wave * 2 * kTile, st + wave * 32, sh, at.direct, r, mine.to, 0, lane);
   };
@@ -498,6 +533,7 @@ __global__ __launch_bounds__(64) void attend_dkv_join(const dconv_attend_shape s
     const int d = lane + 64 * i;
     dk[i] = dv[i] = 0.0f;
     if (d >= sh.D) continue;
+#pragma unroll 8
     for (int x = 0; x < gt.parts; ++x) {
       dk[i] += part[(int64_t)x * 64 * DP + d];
       dv[i] += part[(int64_t)x * 64 * DP + 32 * DP + d];
@@ -536,7 +572,8 @@ void launch_attend_grad(const dconv_attend_shape &sh, const AttendPtrs &p, const
     }
     if (plan.first < sh.Tk) {
       gt.a.tiles = plan.key_tiles;
-      hipLaunchKernelGGL((attend_dkv<T, DP>), dim3(heads * plan.key_tiles), dim3(256), 0, s, sh, p, gt);
+      hipLaunchKernelGGL((attend_dkv<T, DP>), dim3(heads * plan.key_tiles),
+                         dim3(256 * row_groups<T>(DP)), 0, s, sh, p, gt);
     }
     if (plan.first > 0) {
       gt.a.tiles = plan.first_tiles;

@@ -62,18 +62,20 @@ __device__ __forceinline__ typename Mma<T>::Frag as_operand(const f32x16 &c, int
 }
 
 // Rows of DP elements in LDS, in chunks of eight elements that are permuted
-// within a row by an exclusive or, so that eight consecutive rows of one chunk
-// (a row operand), and four rows of two neighbouring chunks (a column operand),
-// lie on different banks.
+// within a row by an exclusive or with bits of the row's number.  LDS serves 256
+// bytes, sixteen chunks of 16 bytes, at a time: sixteen consecutive rows of one
+// chunk (a row operand), and four rows of four neighbouring chunks (a column
+// operand), shall lie on different banks.
 template <class T, int DP>
 struct Tile {
   typedef typename Mma<T>::Frag Frag;
   static constexpr int kChunks = DP / 8;
   static __device__ __forceinline__ int swizzle(int row) {
     if constexpr (sizeof(T) == 4) return DP % 64 == 0 ? row & 7 : row & 3;
-    // rows of a multiple of 128 bytes: all three low bits; rows that alternate
-    // between the halves of 128 bytes: two bits
-    return DP % 64 == 0 ? ((row & 3) << 1) | ((row >> 2) & 1) : (row & 2) | ((row >> 2) & 1);
+    // rows of 256 bytes begin on one bank; of 128 on two in turn; of 64 and 192 on four
+    if constexpr (DP % 128 == 0) return (row & 3) << 2 | (row >> 2 & 3);
+    if constexpr (DP % 64 == 0) return (row >> 1 & 1) << 2 | (row >> 2 & 3);
+    return row >> 2 & 3;
   }
   static __device__ __forceinline__ int at(int row, int chunk) { return row * DP + (chunk ^ swizzle(row)) * 8; }
 
@@ -115,7 +117,7 @@ struct Copy {
   static constexpr int kCopies = (NR * kPieces + kThreads - 1) / kThreads;   // per wave
   static_assert(NR * kPieces % 64 == 0, "whole waves");
   // Rows between a lane's copies, where they are in the same place of a row.
-  static constexpr int kStep = kThreads % (8 * kPieces) == 0 ? kThreads / kPieces : 0;
+  static constexpr int kStep = kThreads % (16 * kPieces) == 0 ? kThreads / kPieces : 0;
   uint32_t offset[kStep ? 1 : kCopies];   // of the lane's pieces from the tile's first row, in bytes
 
   // Row and element of the lane's piece in copy i.  A piece past D repeats the
@@ -150,6 +152,17 @@ struct Copy {
       asm volatile("" : "+v"(o));
       const char *base = reinterpret_cast<const char *>(first) + (kStep ? i * step : 0);
       __builtin_amdgcn_global_load_lds(base + o, (lds_ptr)to(lds, i, wave), 16, 0, 0);
+    }
+  }
+  // The same with offsets computed here.
+  template <class F>
+  static __device__ __forceinline__ void tile_at(T *lds, const T *first, int D, int wave, int lane, F byte_offset) {
+#pragma unroll
+    for (int i = 0; i < kCopies; ++i) {
+      if (!has(i, wave)) break;
+      uint32_t o = byte_offset(row(i, wave, lane)) + element(i, wave, lane, D) * (uint32_t)sizeof(T);
+      asm volatile("" : "+v"(o));
+      __builtin_amdgcn_global_load_lds(reinterpret_cast<const char *>(first) + o, (lds_ptr)to(lds, i, wave), 16, 0, 0);
     }
   }
   // Any rows: row_start(r) is where row r begins.
@@ -211,6 +224,15 @@ __device__ __forceinline__ float half_sum(float x) {
 __device__ __forceinline__ void no_speculation() { asm volatile(""); }
 
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
+// f(i, whether acc_row(i, half) lies in [lo, hi)): one subtraction and one
+// comparison each.
+template <class F>
+__device__ __forceinline__ void within(int lo, int hi, int half, F f) {
+  const unsigned from = (unsigned)(lo - 4 * half), span = (unsigned)max(hi - lo, 0);
+#pragma unroll
+  for (int i = 0; i < 16; ++i) f(i, (unsigned)acc_row(i, 0) - from < span);
+}
 
 // What the host hands to the tile kernels beside the shape.
 struct AttendTile {
@@ -290,6 +312,25 @@ __device__ __forceinline__ RowKeys row_keys(const dconv_attend_shape &sh, const 
   return r;
 }
 
+// What reads LDS and what multiplies stays on its side of this line (vector and
+// scalar arithmetic may cross): operands are read well before their products.
+__device__ __forceinline__ void in_order() { __builtin_amdgcn_sched_barrier(0x2 | 0x4 | 0x400); }
+
+// f(i, whether register i's key, of those from v0 on, is seen by the lane's row).
+template <class F>
+__device__ __forceinline__ void seen_keys(int v0, const RowKeys &see, int sinks, int lane, F f) {
+  const int half = lane >> 5;
+  if (v0 >= sinks) {
+    within(see.lo - v0, see.hi - v0, half, f);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const int v = v0 + acc_row(i, half);
+      f(i, v < see.hi && (v >= see.lo || v < sinks));
+    }
+  }
+}
+
 // The running softmax of 32 rows by one wave: each lane half of a row.
 template <class T, int DP>
 struct Softmax {
@@ -304,39 +345,27 @@ struct Softmax {
     l = 0.0f;
   }
 
-  // Adds 32 * HB keys v0 .. of the tiles ks, vs.
-  template <int HB>
-  __device__ __forceinline__ void add(const T *ks, const T *vs, const Frag (&q)[KS], int v0, const RowKeys &see,
-                                      int sinks, float scale2, bool masked, int lane) {
-    f32x16 s[HB];
+  // 32 scores of each row: keys k0 .. of the tile.
+  static __device__ __forceinline__ f32x16 scores(const T *ks, int k0, const Frag (&q)[KS], int lane) {
+    f32x16 s = {};
 #pragma unroll
-    for (int hb = 0; hb < HB; ++hb) {
-      s[hb] = f32x16{};
+    for (int k = 0; k < KS; ++k) s = Mma<T>::mac(Tile<T, DP>::row(ks, k0, k, lane), q[k], s);
+    return s;
+  }
+  static __device__ __forceinline__ void mask(f32x16 &s, int v0, const RowKeys &see, int sinks, int lane) {
+    seen_keys(v0, see, sinks, lane, [&](int i, bool on) { s[i] = on ? s[i] : -INFINITY; });
+  }
+  // The base follows the maximum only when it is left behind by more than 2^8:
+  // sums and probabilities stay below 2^8 times their true size, and the
+  // rescaling of the result is rare.  before(): what has to be added first.
+  template <class F>
+  __device__ __forceinline__ void follow(const f32x16 &s, float scale2, F before) {
+    float top = s[0];
 #pragma unroll
-      for (int k = 0; k < KS; ++k) s[hb] = Mma<T>::mac(Tile<T, DP>::row(ks, 32 * hb, k, lane), q[k], s[hb]);
-    }
-    if (masked) {
-      no_speculation();
-#pragma unroll
-      for (int hb = 0; hb < HB; ++hb)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int v = v0 + 32 * hb + acc_row(i, lane >> 5);
-          const bool on = v < see.hi && (v >= see.lo || v < sinks);
-          s[hb][i] = on ? s[hb][i] : -INFINITY;
-        }
-    }
-    float top = s[0][0];
-#pragma unroll
-    for (int hb = 0; hb < HB; ++hb)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) top = fmaxf(top, s[hb][i]);
+    for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
     top = half_max(top) * scale2;
-    // The base follows the maximum only when it is left behind by more than
-    // 2^8: sums and probabilities stay below 2^8 times their true size, and the
-    // rescaling of the result is rare.
     if (__any(top - m > 8.0f)) {
-      no_speculation();
+      before();
       const float to = fmaxf(m, top);
       const float keep = to == -INFINITY ? 1.0f : exp2f(m - to);
 #pragma unroll
@@ -344,23 +373,90 @@ struct Softmax {
       l *= keep;
       m = to;
     }
+  }
+  // Scores to probabilities (times 2^-m), as operands.
+  __device__ __forceinline__ void probabilities(const f32x16 &s, float scale2, Frag (&w)[2]) {
     const float base = m == -INFINITY ? 0.0f : m;
+    f32x16 x;
 #pragma unroll
-    for (int hb = 0; hb < HB; ++hb)
+    for (int i = 0; i < 16; ++i) {
+      x[i] = power2<T>(fmaf(s[i], scale2, -base));
+      l += x[i];
+    }
+    w[0] = as_operand<T>(x, 0);
+    w[1] = as_operand<T>(x, 1);
+  }
+  // The result plus the values k0 .. of the tile times their probabilities.
+  __device__ __forceinline__ void values(const T *vs, int k0, const Frag (&w)[2], int lane) {
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        s[hb][i] = power2<T>(fmaf(s[hb][i], scale2, -base));
-        l += s[hb][i];
-      }
+    for (int k = 0; k < 2; ++k)
 #pragma unroll
-    for (int hb = 0; hb < HB; ++hb)
+      for (int c = 0; c < DT; ++c) o[c] = Mma<T>::mac(Tile<T, DP>::column(vs, k0 + 16 * k, c, lane), w[k], o[c]);
+  }
+
+  static __device__ __forceinline__ void load_keys(Frag (&f)[KS], const T *ks, int k0, int lane) {
 #pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        const Frag w = as_operand<T>(s[hb], k);
+    for (int k = 0; k < KS; ++k) f[k] = Tile<T, DP>::row(ks, k0, k, lane);
+  }
+  static __device__ __forceinline__ void load_values(Frag (&f)[DT], const T *vs, int k0, int lane) {
 #pragma unroll
-        for (int c = 0; c < DT; ++c)
-          o[c] = Mma<T>::mac(Tile<T, DP>::column(vs, 32 * hb + 16 * k, c, lane), w, o[c]);
-      }
+    for (int c = 0; c < DT; ++c) f[c] = Tile<T, DP>::column(vs, k0, c, lane);
+  }
+  static __device__ __forceinline__ f32x16 products(const Frag (&f)[KS], const Frag (&q)[KS]) {
+    f32x16 s = {};
+#pragma unroll
+    for (int k = 0; k < KS; ++k) s = Mma<T>::mac(f[k], q[k], s);
+    return s;
+  }
+  __device__ __forceinline__ void weigh(const Frag (&f)[DT], Frag w) {
+#pragma unroll
+    for (int c = 0; c < DT; ++c) o[c] = Mma<T>::mac(f[c], w, o[c]);
+  }
+
+  // Adds 32 keys, v0 .., of the tiles ks, vs.
+  __device__ __forceinline__ void add(const T *ks, const T *vs, const Frag (&q)[KS], int v0, const RowKeys &see,
+                                      int sinks, float scale2, int lane) {
+    f32x16 s = scores(ks, 0, q, lane);
+    mask(s, v0, see, sinks, lane);
+    follow(s, scale2, [] {});
+    Frag w[2];
+    probabilities(s, scale2, w);
+    values(vs, 0, w, lane);
+  }
+  // Adds 64 keys.  The second half's scores are computed beside the first half's
+  // probabilities, and the first half's sum beside the second's probabilities: the
+  // matrix and the vector unit work at the same time within a wave.
+  __device__ __forceinline__ void add_two(const T *ks, const T *vs, const Frag (&q)[KS], int v0, const RowKeys &see,
+                                          int sinks, float scale2, bool masked, int lane) {
+    Frag kf[KS], vf[2][DT], w0[2], w1[2];
+    load_keys(kf, ks, 0, lane);
+    in_order();
+    f32x16 s0 = products(kf, q), s1;
+    load_keys(kf, ks, 32, lane);
+    in_order();
+    if (masked) mask(s0, v0, see, sinks, lane);
+    follow(s0, scale2, [] {});
+    s1 = products(kf, q);
+    load_values(vf[0], vs, 0, lane);
+    in_order();
+    probabilities(s0, scale2, w0);
+    asm volatile("" ::"v"(w0[0]), "v"(w0[1]));   // here, not after the next branch
+    if (masked) mask(s1, v0 + 32, see, sinks, lane);
+    follow(s1, scale2, [&] {
+      values(vs, 0, w0, lane);
+      w0[0] = w0[1] = Frag{};
+    });
+    load_values(vf[1], vs, 16, lane);
+    in_order();
+    weigh(vf[0], w0[0]);
+    load_values(vf[0], vs, 32, lane);
+    in_order();
+    weigh(vf[1], w0[1]);
+    load_values(vf[1], vs, 48, lane);
+    in_order();
+    probabilities(s1, scale2, w1);
+    weigh(vf[0], w1[0]);
+    weigh(vf[1], w1[1]);
   }
 };
 
@@ -415,7 +511,10 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1) void attend_til
   auto step = [&](const T *buf, int v0) {
     if (v0 >= to || (v0 + BN <= from && v0 >= sh.sinks)) return;
     const bool masked = !(v0 + BN <= all_to && (v0 >= all_from || v0 + BN <= sh.sinks));
-    soft.template add<BN / 32>(buf, buf + BN * DP, q, v0, see, sh.sinks, at.scale2, masked, lane);
+    if constexpr (BN == 64)
+      soft.add_two(buf, buf + BN * DP, q, v0, see, sh.sinks, at.scale2, masked, lane);
+    else
+      soft.add(buf, buf + BN * DP, q, v0, see, sh.sinks, at.scale2, lane);
   };
   auto arrived = [&]() {
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
@@ -526,7 +625,7 @@ constexpr int part_floats() { return attend_part_floats(DP); }
 // 32 rows per workgroup; wave w of part s takes tiles of 32 keys by itself, with
 // two LDS buffers of its own and no barrier.
 template <class T, int DP>
-__global__ __launch_bounds__(64 * split_waves<T>(DP)) void attend_split(const dconv_attend_shape sh,
+__global__ __launch_bounds__(64 * split_waves<T>(DP), 1) void attend_split(const dconv_attend_shape sh,
                                                                         const AttendPtrs p, const AttendTile at) {
   constexpr int KS = DP / 16, DT = DP / 32, kTile = 32 * DP, W = split_waves<T>(DP);
   __shared__ __align__(16) T buf0[W * 2 * kTile];
@@ -553,7 +652,7 @@ __global__ __launch_bounds__(64 * split_waves<T>(DP)) void attend_split(const dc
   soft.clear();
   auto step = [&](const T *buf, int v0) {
     const T *mine = buf + wave * 2 * kTile;
-    soft.template add<1>(mine, mine + kTile, q, v0, see, sh.sinks, at.scale2, true, lane);
+    soft.add(mine, mine + kTile, q, v0, see, sh.sinks, at.scale2, lane);
   };
   auto arrived = [&]() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory"); };
   // tiles part * W + wave, then every (splits * W)-th
