@@ -16,7 +16,7 @@ struct JoinPtrs {
 };
 
 // How a call runs: `tpr` threads per row with `ept` elements each, 16 bytes at a
-// time (`whole`) or one element; the rows as `segments` of `rows`, each walked in
+// time (`whole`: on 16-byte boundaries, without a remainder); the rows as `segments` of `rows`, each walked in
 // `runs` of `run_rows`.
 struct JoinPlan {
   bool whole;

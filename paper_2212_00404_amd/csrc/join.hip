@@ -64,10 +64,11 @@ JoinPlan plan_join(const dconv_join_shape &sh, bool backward) {
   // Runs end where a vector changes.
   f.segments = sh.per_sample ? sh.B : 1;
   f.rows = (int)(sh.per_sample ? sh.T : (int64_t)sh.B * sh.T);
-  // Threads enough to fill the chip once; the backward pass half of that, as each
-  // run leaves its sums in memory.
-  const int64_t groups = 256 * (backward ? 1024 : 2048) / f.tpr;
-  int64_t runs = (groups + f.segments - 1) / (f.segments > 0 ? f.segments : 1);
+  // Threads enough to fill the chip once.  (The backward kernel's registers leave
+  // room for 768 threads per compute unit, 512 with 16 elements each; one more
+  // workgroup than that and the last ones run alone.)
+  const int64_t groups = 256 * (!backward ? 2048 : f.tpr > 256 ? 1024 : f.ept == 8 ? 768 : 512) / f.tpr;
+  int64_t runs = f.segments > 0 ? groups / f.segments : 1;
   if (runs > f.rows) runs = f.rows;
   if (runs < 1) runs = 1;
   f.run_rows = (int)((f.rows + runs - 1) / runs);
@@ -132,7 +133,6 @@ DCONV_EXPORT int dconv_join(const dconv_join_shape *shape, const void *branch, c
   if (stats && (uintptr_t)stats % 16 != 0) return DCONV_EINVAL;
   JoinPlan plan = plan_join(*shape, false);
   plan.whole = whole_pieces(*shape, p);
-  if (!plan.whole) plan.ept = 16;
   return run(*shape, p, plan, nullptr, false, stream);
 }
 
@@ -180,6 +180,5 @@ DCONV_EXPORT int dconv_join_backward(const dconv_join_shape *shape, const void *
   if (stats && (uintptr_t)stats % 16 != 0) return DCONV_EINVAL;
   JoinPlan plan = plan_join(*shape, true);
   plan.whole = whole_pieces(*shape, p);
-  if (!plan.whole) plan.ept = 16;
   return run(*shape, p, plan, workspace, true, stream);
 }

@@ -15,67 +15,88 @@
 
 namespace dconv {
 
-template <class T, int V>
-struct alignas(V * sizeof(T) < 16 ? V * sizeof(T) : 16) Pack {
+// V elements, 16 bytes of a row; on an element's boundary only (the memory takes
+// such accesses as one) where rows are not whole 16-byte pieces.
+template <class T, int V, bool WHOLE>
+struct alignas(!WHOLE ? sizeof(T) : V * sizeof(T) < 16 ? V * sizeof(T) : 16) Pack {
   T v[V];
 };
 
-// A thread's part of a row: elements V (i TPR + me) .. + V - 1 for i < EPT / V.
-template <class T, int V, int TPR, int EPT>
-struct RowPart {
-  Pack<T, V> p[EPT / V];
-  __device__ __forceinline__ void load(const T *row, int D, int me) {
-#pragma unroll
-    for (int i = 0; i < EPT / V; ++i) {
-      const int e = V * (i * TPR + me);
-      if (e < D) p[i] = *reinterpret_cast<const Pack<T, V> *>(row + e);
-    }
-  }
-  __device__ __forceinline__ float get(int k) const { return to_f32(p[k / V].v[k % V]); }
+// How a row lies over TPR threads: thread `me` holds elements
+// V (i TPR + me) .. + V - 1 for i < EPT / V.
+template <int V_, int TPR_, int EPT_, bool WHOLE_>
+struct Row {
+  static constexpr int V = V_, TPR = TPR_, EPT = EPT_;
+  static constexpr bool WHOLE = WHOLE_;
+  static __device__ __forceinline__ int first(int i, int me) { return V * (i * TPR + me); }
 };
 
-// f(k, e): the thread's k-th element is element e of the row; k past the row's
-// end are left out.
-template <int V, int TPR, int EPT, class F>
+// A thread's part of a row, as it is in memory.
+template <class T, class R>
+struct RowPart {
+  typedef Pack<T, R::V, R::WHOLE> P;
+  P p[R::EPT / R::V];
+  __device__ __forceinline__ void load(const T *row, int D, int me) {
+#pragma unroll
+    for (int i = 0; i < R::EPT / R::V; ++i) {
+      const int e = R::first(i, me);
+      if (R::WHOLE ? e < D : e + R::V <= D) {
+        p[i] = *reinterpret_cast<const P *>(row + e);
+      } else if (!R::WHOLE && e < D) {
+#pragma unroll
+        for (int j = 0; j < R::V; ++j)
+          if (e + j < D) p[i].v[j] = row[e + j];
+      }
+    }
+  }
+  __device__ __forceinline__ void store(T *row, int D, int me) const {
+#pragma unroll
+    for (int i = 0; i < R::EPT / R::V; ++i) {
+      const int e = R::first(i, me);
+      if (R::WHOLE ? e < D : e + R::V <= D) {
+        *reinterpret_cast<P *>(row + e) = p[i];
+      } else if (!R::WHOLE && e < D) {
+#pragma unroll
+        for (int j = 0; j < R::V; ++j)
+          if (e + j < D) row[e + j] = p[i].v[j];
+      }
+    }
+  }
+  __device__ __forceinline__ float get(int k) const { return to_f32(p[k / R::V].v[k % R::V]); }
+  __device__ __forceinline__ void set(int k, float x) { p[k / R::V].v[k % R::V] = from_f32<T>(x); }
+};
+
+// f(k): for each of the thread's elements that the row has.
+template <class R, class F>
 __device__ __forceinline__ void each(int D, int me, F f) {
 #pragma unroll
-  for (int i = 0; i < EPT / V; ++i)
-    if (V * (i * TPR + me) < D) {
+  for (int i = 0; i < R::EPT / R::V; ++i)
+    if (R::first(i, me) < D) {
 #pragma unroll
-      for (int j = 0; j < V; ++j) f(i * V + j, V * (i * TPR + me) + j);
+      for (int j = 0; j < R::V; ++j)
+        if (R::WHOLE || R::first(i, me) + j < D) f(i * R::V + j);
     }
 }
 
-template <class T, int V, int TPR, int EPT>
-__device__ __forceinline__ void store_row(T *row, int D, int me, const float (&x)[EPT]) {
+template <class T, class R>
+__device__ __forceinline__ void store_row(T *row, int D, int me, const float (&x)[R::EPT]) {
+  RowPart<T, R> p;
 #pragma unroll
-  for (int i = 0; i < EPT / V; ++i) {
-    const int e = V * (i * TPR + me);
-    if (e >= D) continue;
-    Pack<T, V> p;
-#pragma unroll
-    for (int j = 0; j < V; ++j) p.v[j] = from_f32<T>(x[i * V + j]);
-    *reinterpret_cast<Pack<T, V> *>(row + e) = p;
-  }
+  for (int k = 0; k < R::EPT; ++k) p.set(k, x[k]);
+  p.store(row, D, me);
 }
 
 // A vector's part (of type W) in fp32; `absent` where there is none or past the
 // row's end.
-template <class W, int V, int TPR, int EPT>
-__device__ __forceinline__ void load_vector(float (&x)[EPT], const void *p, int64_t offset, int D, int me,
+template <class W, class R>
+__device__ __forceinline__ void load_vector(float (&x)[R::EPT], const void *p, int64_t offset, int D, int me,
                                             float absent) {
 #pragma unroll
-  for (int k = 0; k < EPT; ++k) x[k] = absent;
+  for (int k = 0; k < R::EPT; ++k) x[k] = absent;
   if (!p) return;
-  const W *row = (const W *)p + offset;
-#pragma unroll
-  for (int i = 0; i < EPT / V; ++i) {
-    const int e = V * (i * TPR + me);
-    if (e >= D) continue;
-    const Pack<W, V> v = *reinterpret_cast<const Pack<W, V> *>(row + e);
-#pragma unroll
-    for (int j = 0; j < V; ++j) x[i * V + j] = to_f32(v.v[j]);
-  }
+  RowPart<W, R> v;
+  v.load((const W *)p + offset, D, me);
+  each<R>(D, me, [&](int k) { x[k] = v.get(k); });
 }
 
 constexpr int join_block(int TPR) { return TPR > 256 ? TPR : 256; }
@@ -122,10 +143,10 @@ __device__ __forceinline__ int64_t row_at(const long long *stride, int64_t n, in
   return n / T * stride[0] + n % T * stride[1];
 }
 
-template <class T, class W, int V, int TPR, int EPT>
-__global__ __launch_bounds__(join_block(TPR)) void join_forward(const dconv_join_shape sh, const JoinPtrs p,
+template <class T, class W, class R>
+__global__ __launch_bounds__(join_block(R::TPR)) void join_forward(const dconv_join_shape sh, const JoinPtrs p,
                                                                 const JoinRuns runs) {
-  constexpr int kPerBlock = join_block(TPR) / TPR;
+  constexpr int TPR = R::TPR, EPT = R::EPT, kPerBlock = join_block(TPR) / TPR;
   __shared__ float place[2 * (TPR / 64 + 1)];
   DCONV_POISON(poison_lds(place, 2 * (TPR / 64 + 1)));
   const int me = threadIdx.x % TPR, D = sh.D;
@@ -138,15 +159,15 @@ __global__ __launch_bounds__(join_block(TPR)) void join_forward(const dconv_join
   const bool layer = sh.norm == DCONV_NORM_LAYER, post = sh.post && p.branch;
   const int64_t b = run.segment;   // the sequence, if a vector is set for each
   float pw[EPT], g[EPT], w[EPT], bias[EPT];
-  load_vector<W, V, TPR, EPT>(pw, post ? p.post_weight : nullptr, sh.per_sample & DCONV_JOIN_POST_WEIGHT ? b * D : 0,
+  load_vector<W, R>(pw, post ? p.post_weight : nullptr, sh.per_sample & DCONV_JOIN_POST_WEIGHT ? b * D : 0,
                               D, me, 1.0f);
-  load_vector<W, V, TPR, EPT>(g, p.gate, sh.per_sample & DCONV_JOIN_GATE ? b * D : 0, D, me, 1.0f);
-  load_vector<W, V, TPR, EPT>(w, p.pre_weight, sh.per_sample & DCONV_JOIN_PRE_WEIGHT ? b * D : 0, D, me, 1.0f);
-  load_vector<W, V, TPR, EPT>(bias, p.pre_bias, sh.per_sample & DCONV_JOIN_PRE_BIAS ? b * D : 0, D, me, 0.0f);
+  load_vector<W, R>(g, p.gate, sh.per_sample & DCONV_JOIN_GATE ? b * D : 0, D, me, 1.0f);
+  load_vector<W, R>(w, p.pre_weight, sh.per_sample & DCONV_JOIN_PRE_WEIGHT ? b * D : 0, D, me, 1.0f);
+  load_vector<W, R>(bias, p.pre_bias, sh.per_sample & DCONV_JOIN_PRE_BIAS ? b * D : 0, D, me, 0.0f);
 #pragma unroll
   for (int k = 0; k < EPT; ++k) g[k] *= sh.branch_scale;
 
-  RowPart<T, V, TPR, EPT> x, br, x_next, br_next;
+  RowPart<T, R> x, br, x_next, br_next;
   auto load = [&](int64_t n) {
     x_next.load((const T *)p.x + row_at(sh.x_stride, n, sh.T), D, me);
     if (p.branch) br_next.load((const T *)p.branch + row_at(sh.branch_stride, n, sh.T), D, me);
@@ -157,37 +178,37 @@ __global__ __launch_bounds__(join_block(TPR)) void join_forward(const dconv_join
     br = br_next;
     if (n + 1 < run.end) load(n + 1);
     float h[EPT] = {}, mb = 0.0f, rb = 1.0f;
-    auto all = [&](auto f) { each<V, TPR, EPT>(D, me, f); };
+    auto all = [&](auto f) { each<R>(D, me, f); };
     // N(z) of the row in z: the mean first, then the squares about it
     auto norm = [&](float (&z)[EPT], float &m, float &r) {
       m = 0.0f;
       float s = 0.0f;
       if (layer) {
-        all([&](int k, int) { s += z[k]; });
+        all([&](int k) { s += z[k]; });
         m = sum(s) * inv;
         s = 0.0f;
       }
-      all([&](int k, int) {
+      all([&](int k) {
         z[k] -= m;
         s = fmaf(z[k], z[k], s);
       });
       r = 1.0f / sqrtf(fmaf(sum(s), inv, sh.eps));
-      all([&](int k, int) { z[k] *= r; });
+      all([&](int k) { z[k] *= r; });
     };
     if (p.branch) {
-      all([&](int k, int) { h[k] = br.get(k); });
+      all([&](int k) { h[k] = br.get(k); });
       if (post) norm(h, mb, rb);
-      all([&](int k, int) { h[k] = fmaf(sh.residual_scale, x.get(k), g[k] * (h[k] * pw[k])); });
+      all([&](int k) { h[k] = fmaf(sh.residual_scale, x.get(k), g[k] * (h[k] * pw[k])); });
     } else {
-      all([&](int k, int) { h[k] = sh.residual_scale * x.get(k); });
+      all([&](int k) { h[k] = sh.residual_scale * x.get(k); });
     }
-    if (p.h) store_row<T, V, TPR>((T *)p.h + n * D, D, me, h);
+    if (p.h) store_row<T, R>((T *)p.h + n * D, D, me, h);
     if (!p.y && !p.stats) continue;
     float mh, rh;
     norm(h, mh, rh);
     if (p.y) {
-      all([&](int k, int) { h[k] = fmaf(h[k], w[k], bias[k]); });
-      store_row<T, V, TPR>((T *)p.y + n * D, D, me, h);
+      all([&](int k) { h[k] = fmaf(h[k], w[k], bias[k]); });
+      store_row<T, R>((T *)p.y + n * D, D, me, h);
     }
     if (p.stats && me == 0) *reinterpret_cast<float4 *>(p.stats + 4 * n) = make_float4(mb, rb, mh, rh);
   }
@@ -196,10 +217,10 @@ __global__ __launch_bounds__(join_block(TPR)) void join_forward(const dconv_join
 // dx, dbranch, and each run's sums for the vectors: into the vectors' gradients
 // themselves where there is one run to a segment and a segment to a vector, else
 // into the workspace, [vector][run][D].
-template <class T, class W, int V, int TPR, int EPT>
-__global__ __launch_bounds__(join_block(TPR)) void join_backward(const dconv_join_shape sh, const JoinPtrs p,
+template <class T, class W, class R>
+__global__ __launch_bounds__(join_block(R::TPR), R::TPR <= 256 ? (R::EPT == 8 ? 3 : 2) : 1) void join_backward(const dconv_join_shape sh, const JoinPtrs p,
                                                                  const JoinRuns runs, float *partial) {
-  constexpr int kPerBlock = join_block(TPR) / TPR;
+  constexpr int TPR = R::TPR, EPT = R::EPT, kPerBlock = join_block(TPR) / TPR;
   __shared__ float place[2 * (TPR / 64 + 1)];
   DCONV_POISON(poison_lds(place, 2 * (TPR / 64 + 1)));
   const int me = threadIdx.x % TPR, D = sh.D;
@@ -212,15 +233,15 @@ __global__ __launch_bounds__(join_block(TPR)) void join_backward(const dconv_joi
   const bool layer = sh.norm == DCONV_NORM_LAYER, post = sh.post && p.branch;
   const int64_t b = run.segment;   // the sequence, if a vector is set for each
   float pw[EPT], g[EPT], w[EPT];
-  load_vector<W, V, TPR, EPT>(pw, post ? p.post_weight : nullptr, sh.per_sample & DCONV_JOIN_POST_WEIGHT ? b * D : 0,
+  load_vector<W, R>(pw, post ? p.post_weight : nullptr, sh.per_sample & DCONV_JOIN_POST_WEIGHT ? b * D : 0,
                               D, me, 1.0f);
-  load_vector<W, V, TPR, EPT>(g, p.gate, sh.per_sample & DCONV_JOIN_GATE ? b * D : 0, D, me, 1.0f);
-  load_vector<W, V, TPR, EPT>(w, p.pre_weight, sh.per_sample & DCONV_JOIN_PRE_WEIGHT ? b * D : 0, D, me, 1.0f);
+  load_vector<W, R>(g, p.gate, sh.per_sample & DCONV_JOIN_GATE ? b * D : 0, D, me, 1.0f);
+  load_vector<W, R>(w, p.pre_weight, sh.per_sample & DCONV_JOIN_PRE_WEIGHT ? b * D : 0, D, me, 1.0f);
 #pragma unroll
   for (int k = 0; k < EPT; ++k) g[k] *= sh.branch_scale;
   float s_pw[EPT] = {}, s_g[EPT] = {}, s_w[EPT] = {}, s_bias[EPT] = {};
 
-  RowPart<T, V, TPR, EPT> x, br, dh, dy, x_next, br_next, dh_next, dy_next;
+  RowPart<T, R> x, br, dh, dy, x_next, br_next, dh_next, dy_next;
   float4 st, st_next;
   auto load = [&](int64_t n) {
     x_next.load((const T *)p.x + row_at(sh.x_stride, n, sh.T), D, me);
@@ -234,13 +255,13 @@ __global__ __launch_bounds__(join_block(TPR)) void join_backward(const dconv_joi
     x = x_next, br = br_next, dh = dh_next, dy = dy_next, st = st_next;
     if (n + 1 < run.end) load(n + 1);
     const float mb = st.x, rb = st.y, mh = st.z, rh = st.w;
-    auto all = [&](auto f) { each<V, TPR, EPT>(D, me, f); };
+    auto all = [&](auto f) { each<R>(D, me, f); };
     float nb[EPT] = {}, gh[EPT] = {};
-    if (p.branch) all([&](int k, int) { nb[k] = post ? (br.get(k) - mb) * rb : br.get(k); });
+    if (p.branch) all([&](int k) { nb[k] = post ? (br.get(k) - mb) * rb : br.get(k); });
     if (p.dy) {
       // t = N(h); dH = dh + r_h (dt - mean(dt) - t mean(dt t))
       float t[EPT] = {}, s1 = 0.0f, s2 = 0.0f;
-      all([&](int k, int) {
+      all([&](int k) {
         const float h = fmaf(sh.residual_scale, x.get(k), p.branch ? g[k] * (nb[k] * pw[k]) : 0.0f);
         const float d = dy.get(k);
         t[k] = (h - mh) * rh;
@@ -252,15 +273,15 @@ __global__ __launch_bounds__(join_block(TPR)) void join_backward(const dconv_joi
       });
       s1 = layer ? sum(s1) * inv : 0.0f;
       s2 = sum(s2) * inv;
-      all([&](int k, int) { gh[k] = rh * (gh[k] - s1 - t[k] * s2); });
+      all([&](int k) { gh[k] = rh * (gh[k] - s1 - t[k] * s2); });
     }
-    if (p.dh) all([&](int k, int) { gh[k] += dh.get(k); });
+    if (p.dh) all([&](int k) { gh[k] += dh.get(k); });
     float o[EPT] = {};
-    all([&](int k, int) { o[k] = sh.residual_scale * gh[k]; });
-    store_row<T, V, TPR>((T *)p.dx + n * D, D, me, o);
+    all([&](int k) { o[k] = sh.residual_scale * gh[k]; });
+    store_row<T, R>((T *)p.dx + n * D, D, me, o);
     if (!p.branch) continue;
     float q1 = 0.0f, q2 = 0.0f;
-    all([&](int k, int) {
+    all([&](int k) {
       const float u = gh[k] * nb[k];
       s_pw[k] = fmaf(u, g[k], s_pw[k]);
       s_g[k] = fmaf(u, pw[k], s_g[k]);
@@ -271,9 +292,9 @@ __global__ __launch_bounds__(join_block(TPR)) void join_backward(const dconv_joi
     if (post) {
       q1 = layer ? sum(q1) * inv : 0.0f;
       q2 = sum(q2) * inv;
-      all([&](int k, int) { o[k] = rb * (o[k] - q1 - nb[k] * q2); });
+      all([&](int k) { o[k] = rb * (o[k] - q1 - nb[k] * q2); });
     }
-    store_row<T, V, TPR>((T *)p.dbranch + n * D, D, me, o);
+    store_row<T, R>((T *)p.dbranch + n * D, D, me, o);
   }
 #pragma unroll
   for (int k = 0; k < EPT; ++k) s_g[k] *= sh.branch_scale;
@@ -281,9 +302,9 @@ __global__ __launch_bounds__(join_block(TPR)) void join_backward(const dconv_joi
   auto leave = [&](void *to, int bit, const float (&s)[EPT]) {
     if (!to) return;
     if (runs.runs == 1 && (runs.segments == 1 || (sh.per_sample & bit))) {
-      store_row<W, V, TPR>((W *)to + id * D, D, me, s);
+      store_row<W, R>((W *)to + id * D, D, me, s);
     } else {
-      store_row<float, V, TPR>(out, D, me, s);
+      store_row<float, R>(out, D, me, s);
       out += all_runs * D;
     }
   };
@@ -293,15 +314,21 @@ __global__ __launch_bounds__(join_block(TPR)) void join_backward(const dconv_joi
   leave(p.dpre_bias, DCONV_JOIN_PRE_BIAS, s_bias);
 }
 
-// Adds the runs' sums: 64 columns per workgroup, its 16 waves each every 16th run,
-// then the waves in order.
+// Adds the runs' sums of each vector (blockIdx.z): 64 columns per workgroup, its 16
+// waves each every 16th run, then the waves in order.
+struct JoinSums {
+  const float *partial[4];
+  void *out[4];
+  int runs[4], segments[4];
+};
 template <class W>
-__global__ __launch_bounds__(1024) void join_runs(const float *__restrict__ partial, W *__restrict__ out, int runs,
-                                                  int D) {
+__global__ __launch_bounds__(1024) void join_runs(const JoinSums sums, int D) {
   __shared__ float part[16][64];
   DCONV_POISON(poison_lds(&part[0][0], 1024));
+  const int z = blockIdx.z, runs = sums.runs[z];
+  if ((int)blockIdx.y >= sums.segments[z]) return;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, d = blockIdx.x * 64 + lane;
-  const float *from = partial + (int64_t)blockIdx.y * runs * D;
+  const float *from = sums.partial[z] + (int64_t)blockIdx.y * runs * D;
   float s[4] = {};
   if (d < D) {
     int r = wave;
@@ -316,26 +343,23 @@ __global__ __launch_bounds__(1024) void join_runs(const float *__restrict__ part
     float t = 0.0f;
 #pragma unroll
     for (int i = 0; i < 16; ++i) t += part[i][lane];
-    out[(int64_t)blockIdx.y * D + d] = from_f32<W>(t);
+    ((W *)sums.out[z])[(int64_t)blockIdx.y * D + d] = from_f32<W>(t);
   }
 }
 
 // ---------------------------------------------------------------------------
 // Launch
 // ---------------------------------------------------------------------------
-// f(V, TPR, EPT) as compile-time constants.
+// f(a Row as a value).
 template <class T, class F>
 void by_row(const JoinPlan &plan, F f) {
   constexpr int V = 16 / sizeof(T);
   auto at = [&](auto tpr) {
     constexpr int TPR = decltype(tpr)::value;
-    if (!plan.whole)
-      f(std::integral_constant<int, 1>(), tpr, std::integral_constant<int, 16>());
-    else if (plan.ept == 8)
-      f(std::integral_constant<int, V>(), tpr, std::integral_constant<int, 8>());
+    if (plan.ept == 8)
+      plan.whole ? f(Row<V, TPR, 8, true>()) : f(Row<V, TPR, 8, false>());
     else
-      f(std::integral_constant<int, V>(), tpr, std::integral_constant<int, 16>());
-    (void)TPR;
+      plan.whole ? f(Row<V, TPR, 16, true>()) : f(Row<V, TPR, 16, false>());
   };
   if (plan.tpr == 16) at(std::integral_constant<int, 16>());
   if (plan.tpr == 64) at(std::integral_constant<int, 64>());
@@ -348,28 +372,36 @@ void launch_join(const dconv_join_shape &sh, const JoinPtrs &p, const JoinPlan &
                  hipStream_t s) {
   const JoinRuns runs = {plan.segments, plan.rows, plan.runs, plan.run_rows};
   const int64_t all_runs = (int64_t)plan.segments * plan.runs;
-  by_row<T>(plan, [&](auto v, auto tpr, auto ept) {
-    constexpr int V = decltype(v)::value, TPR = decltype(tpr)::value, EPT = decltype(ept)::value;
-    const int per_block = join_block(TPR) / TPR;
-    const dim3 grid((unsigned)((all_runs + per_block - 1) / per_block)), block(join_block(TPR));
+  by_row<T>(plan, [&](auto row) {
+    typedef decltype(row) R;
+    const int per_block = join_block(R::TPR) / R::TPR;
+    const dim3 grid((unsigned)((all_runs + per_block - 1) / per_block)), block(join_block(R::TPR));
     if (all_runs == 0) return;
     if (!backward)
-      hipLaunchKernelGGL((join_forward<T, W, V, TPR, EPT>), grid, block, 0, s, sh, p, runs);
+      hipLaunchKernelGGL((join_forward<T, W, R>), grid, block, 0, s, sh, p, runs);
     else
-      hipLaunchKernelGGL((join_backward<T, W, V, TPR, EPT>), grid, block, 0, s, sh, p, runs, workspace);
+      hipLaunchKernelGGL((join_backward<T, W, R>), grid, block, 0, s, sh, p, runs, workspace);
   });
   if (!backward) return;
   const struct { void *out; int bit; } vectors[] = {{p.dpost_weight, DCONV_JOIN_POST_WEIGHT},
                                                     {p.dgate, DCONV_JOIN_GATE},
                                                     {p.dpre_weight, DCONV_JOIN_PRE_WEIGHT},
                                                     {p.dpre_bias, DCONV_JOIN_PRE_BIAS}};
+  JoinSums sums = {};
+  int n = 0, most = 0;
   for (const auto &g : vectors) {
     const bool per = sh.per_sample & g.bit;
     if (!g.out || (plan.runs == 1 && (plan.segments == 1 || per)) || (per && plan.segments == 0)) continue;
-    hipLaunchKernelGGL((join_runs<W>), dim3((sh.D + 63) / 64, per ? plan.segments : 1), dim3(1024), 0, s, workspace,
-                       (W *)g.out, per ? plan.runs : (int)all_runs, sh.D);
+    sums.partial[n] = workspace;
+    sums.out[n] = g.out;
+    sums.runs[n] = per ? plan.runs : (int)all_runs;
+    sums.segments[n] = per ? plan.segments : 1;
+    most = sums.segments[n] > most ? sums.segments[n] : most;
+    ++n;
     workspace += all_runs * sh.D;
   }
+  if (n > 0)
+    hipLaunchKernelGGL((join_runs<W>), dim3((sh.D + 63) / 64, most, n), dim3(1024), 0, s, sums, sh.D);
 }
 
 }  // namespace dconv
