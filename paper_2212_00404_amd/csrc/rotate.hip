@@ -28,6 +28,32 @@ __device__ __forceinline__ void turn_sincos(float position, float freq, float *s
   sincospif(2.0f * ((p - rintf(p)) + e), s, c);
 }
 
+// V elements; on an element's boundary only (the memory takes such accesses as
+// one) where rows are not whole 16-byte pieces.
+template <class T, int V, bool WHOLE>
+struct alignas(WHOLE ? V * sizeof(T) : sizeof(T)) Pack {
+  T v[V];
+};
+// n of the V elements, all of them in one access.
+template <class T, int V, bool WHOLE>
+__device__ __forceinline__ Pack<T, V, WHOLE> load_pack(const T *p, int n) {
+  Pack<T, V, WHOLE> x;
+  if (WHOLE || n >= V) return *reinterpret_cast<const Pack<T, V, WHOLE> *>(p);
+#pragma unroll
+  for (int i = 0; i < V; ++i) x.v[i] = i < n ? p[i] : from_f32<T>(0.0f);
+  return x;
+}
+template <class T, int V, bool WHOLE>
+__device__ __forceinline__ void store_pack(T *p, const Pack<T, V, WHOLE> &x, int n) {
+  if (WHOLE || n >= V) {
+    *reinterpret_cast<Pack<T, V, WHOLE> *>(p) = x;
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < V; ++i)
+    if (i < n) p[i] = x.v[i];
+}
+
 // Bound by memory: every element is read and written once.  A thread takes one
 // piece of a token (P pairs, or V elements past the pairs), computes its sines and
 // cosines once (some 60 instructions a pair) and turns that piece in every
@@ -38,17 +64,14 @@ struct Work {
   int64_t threads;
 };
 
-// V elements per access (16 bytes, or one).
-template <class T, int V, bool ADJACENT>
+// Pieces of V elements (16 bytes).  WHOLE: on 16-byte boundaries, without a
+// remainder in a piece of pairs or past them.
+template <class T, bool ADJACENT, bool WHOLE>
 __global__ __launch_bounds__(256) void rotate_pieces(const dconv_rotate_shape sh, const Work wk, const T *x,
                                                      const float *__restrict__ positions,
                                                      const float *__restrict__ freq, const int *__restrict__ axis,
                                                      T *out) {
-  constexpr int P = ADJACENT ? (V > 1 ? V / 2 : 1) : V;   // pairs per piece
-  constexpr bool kTwo = !ADJACENT || V == 1;               // a piece's pairs are in two places
-  struct alignas(V * sizeof(T)) Pack {
-    T v[V];
-  };
+  constexpr int V = 16 / sizeof(T), P = ADJACENT ? V / 2 : V;   // pairs per piece
   const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (id >= wk.threads) return;
   const int piece = (int)(id % wk.pieces);
@@ -61,11 +84,11 @@ __global__ __launch_bounds__(256) void rotate_pieces(const dconv_rotate_shape sh
   T *yr = out + b * sh.out_stride[0] + t * sh.out_stride[1];
 
   if (piece >= wk.pairs) {   // past the pairs: copied
-    const int e = (ADJACENT ? wk.pairs * (V > 1 ? V : 2) : 2 * sh.R) + (piece - wk.pairs) * V;
+    const int e = 2 * sh.R + (piece - wk.pairs) * V, n = sh.D - e;
 #pragma unroll 4
     for (int h = h0; h < sh.H; h += wk.split)
-      *reinterpret_cast<Pack *>(yr + h * sh.out_stride[2] + e) =
-          *reinterpret_cast<const Pack *>(xr + h * sh.x_stride[2] + e);
+      store_pack<T, V, WHOLE>(yr + h * sh.out_stride[2] + e,
+                              load_pack<T, V, WHOLE>(xr + h * sh.x_stride[2] + e, n), n);
     return;
   }
   const int r0 = piece * P;
@@ -92,44 +115,38 @@ __global__ __launch_bounds__(256) void rotate_pieces(const dconv_rotate_shape sh
       w = from_f32<T>(fmaf(fu, s[k], fw * c[k]));
     }
   };
-  const int eu = ADJACENT ? (V > 1 ? piece * V : 2 * r0) : r0;
-  const int ew = ADJACENT ? eu + 1 : r0 + sh.R;
+  const int eu = ADJACENT ? 2 * r0 : r0, n = ADJACENT ? 2 * (sh.R - r0) : sh.R - r0;
 #pragma unroll 4
   for (int h = h0; h < sh.H; h += wk.split) {
     const T *xh = xr + h * sh.x_stride[2];
     T *yh = yr + h * sh.out_stride[2];
-    Pack u = *reinterpret_cast<const Pack *>(xh + eu);
-    if constexpr (kTwo) {
-      Pack w = *reinterpret_cast<const Pack *>(xh + ew);
-#pragma unroll
-      for (int k = 0; k < P; ++k) turn(k, u.v[k], w.v[k]);
-      *reinterpret_cast<Pack *>(yh + ew) = w;
-    } else {
+    auto u = load_pack<T, V, WHOLE>(xh + eu, n);
+    if constexpr (ADJACENT) {
 #pragma unroll
       for (int k = 0; k < P; ++k) turn(k, u.v[2 * k], u.v[2 * k + 1]);
+    } else {
+      auto w = load_pack<T, V, WHOLE>(xh + eu + sh.R, n);
+#pragma unroll
+      for (int k = 0; k < P; ++k) turn(k, u.v[k], w.v[k]);
+      store_pack<T, V, WHOLE>(yh + eu + sh.R, w, n);
     }
-    *reinterpret_cast<Pack *>(yh + eu) = u;
+    store_pack<T, V, WHOLE>(yh + eu, u, n);
   }
 }
 
-template <class T, int V, bool ADJACENT>
+template <class T, bool ADJACENT, bool WHOLE>
 void launch_pieces(const dconv_rotate_shape &sh, const void *x, const float *positions, const float *freq,
                    const int *axis, void *out, hipStream_t s) {
+  constexpr int V = 16 / sizeof(T), P = ADJACENT ? V / 2 : V;
   Work wk;
-  if (ADJACENT) {
-    const int per = V > 1 ? V : 2;
-    wk.pairs = (2 * sh.R + per - 1) / per;
-    wk.pieces = wk.pairs + (sh.D - (wk.pairs * per < sh.D ? wk.pairs * per : sh.D)) / V;
-  } else {
-    wk.pairs = sh.R / V;
-    wk.pieces = wk.pairs + (sh.D - 2 * sh.R) / V;
-  }
+  wk.pairs = (sh.R + P - 1) / P;
+  wk.pieces = wk.pairs + (sh.D - 2 * sh.R + V - 1) / V;
   // Each thread takes as many heads as leave threads enough to fill the chip.
   const int64_t per_head = (int64_t)sh.B * sh.T * wk.pieces;
-  int64_t split = (kThreads + per_head - 1) / per_head;
+  const int64_t split = (kThreads + per_head - 1) / per_head;
   wk.split = (int)(split < sh.H ? split : sh.H);
   wk.threads = per_head * wk.split;
-  hipLaunchKernelGGL((rotate_pieces<T, V, ADJACENT>), dim3((unsigned)((wk.threads + 255) / 256)), dim3(256), 0, s,
+  hipLaunchKernelGGL((rotate_pieces<T, ADJACENT, WHOLE>), dim3((unsigned)((wk.threads + 255) / 256)), dim3(256), 0, s,
                      sh, wk, (const T *)x, positions, freq, axis, (T *)out);
 }
 
@@ -138,14 +155,14 @@ hipError_t launch(const dconv_rotate_shape &sh, const void *x, const float *posi
                   const int *axis, void *out, hipStream_t s) {
   constexpr int V = 16 / sizeof(T);
   bool whole = sh.D % V == 0 && (uintptr_t)x % 16 == 0 && (uintptr_t)out % 16 == 0 &&
-               (sh.adjacent || sh.R % V == 0);
+               sh.R % (sh.adjacent ? V / 2 : V) == 0;
   for (int i = 0; i < 3; ++i) whole = whole && sh.x_stride[i] % V == 0 && sh.out_stride[i] % V == 0;
   if (whole)
-    sh.adjacent ? launch_pieces<T, V, true>(sh, x, positions, freq, axis, out, s)
-                : launch_pieces<T, V, false>(sh, x, positions, freq, axis, out, s);
+    sh.adjacent ? launch_pieces<T, true, true>(sh, x, positions, freq, axis, out, s)
+                : launch_pieces<T, false, true>(sh, x, positions, freq, axis, out, s);
   else
-    sh.adjacent ? launch_pieces<T, 1, true>(sh, x, positions, freq, axis, out, s)
-                : launch_pieces<T, 1, false>(sh, x, positions, freq, axis, out, s);
+    sh.adjacent ? launch_pieces<T, true, false>(sh, x, positions, freq, axis, out, s)
+                : launch_pieces<T, false, false>(sh, x, positions, freq, axis, out, s);
   return hipGetLastError();
 }
 

@@ -49,6 +49,13 @@ def _tensor(t, name: str, ndim: int, dtype=None, device=None):
         raise ValueError("the last dimension of %s must be contiguous" % name)
 
 
+def _plain(t, ndim: int, dtype, index: int) -> bool:
+    """What ``_tensor`` asks for, without its messages (a small call is bound by
+    the host)."""
+    return (isinstance(t, torch.Tensor) and t.dtype is dtype and t.is_cuda and t.get_device() == index
+            and t.dim() == ndim and (t.stride(-1) == 1 or t.shape[-1] <= 1))
+
+
 def _shaped(t, name: str, shape):
     if tuple(t.shape) != tuple(shape):
         raise ValueError("%s must be %r, got %r" % (name, tuple(shape), tuple(t.shape)))
@@ -57,9 +64,10 @@ def _shaped(t, name: str, shape):
 def _workspace(query, shape: bytes, device):
     n = ctypes.c_longlong(0)
     _check(query(shape, ctypes.byref(n)))
-    if n.value == 0:
+    n = n.value
+    if n == 0:
         return None, 0
-    return torch.empty(n.value, dtype=torch.uint8, device=device), n.value
+    return torch.empty(n, dtype=torch.uint8, device=device), n
 
 
 def _ptr(t):
@@ -83,30 +91,33 @@ def rotate(x: torch.Tensor, positions: torch.Tensor, freq: torch.Tensor, axis: t
     inverse=True)``.  ``out`` may be ``x``.
     """
     _tensor(x, "x", 4)
-    dev = x.device
+    dev, index = x.device, x.get_device()
     B, T, H, D = x.shape
     if isinstance(positions, torch.Tensor) and positions.dim() == 2:
         positions = positions[:, None].expand(-1, B, -1)
-    if not isinstance(positions, torch.Tensor) or positions.dtype != torch.float32 or \
-            positions.device != dev or positions.dim() != 3:
+    if not (isinstance(positions, torch.Tensor) and positions.dtype is torch.float32
+            and positions.get_device() == index and positions.dim() == 3):
         raise ValueError("positions must be a float32 tensor [axes, B, T] or [axes, T] on %s" % dev)
-    if positions.shape[0] < 1:
+    axes, Bp, Tp = positions.shape
+    if axes < 1:
         raise ValueError("positions must have an axis")
-    _shaped(positions, "positions", (positions.shape[0], B, T))
-    _tensor(freq, "freq", 1, torch.float32, dev)
-    _tensor(axis, "axis", 1, torch.int32, dev)
+    if Bp != B or Tp != T:
+        _shaped(positions, "positions", (axes, B, T))
+    if not (_plain(freq, 1, torch.float32, index) and _plain(axis, 1, torch.int32, index)):
+        _tensor(freq, "freq", 1, torch.float32, dev)
+        _tensor(axis, "axis", 1, torch.int32, dev)
     R = freq.shape[0]
-    _shaped(axis, "axis", (R,))
+    if axis.shape[0] != R:
+        _shaped(axis, "axis", (R,))
     if 2 * R > D:
         raise ValueError("%d pairs do not fit a head of %d" % (R, D))
     if out is None:
-        out = torch.empty((B, T, H, D), dtype=x.dtype, device=dev)
+        out = torch.empty_like(x, memory_format=torch.contiguous_format)
     elif out is not x:
         _tensor(out, "out", 4, x.dtype, dev)
         _shaped(out, "out", x.shape)
-    shape = _ROTATE_SHAPE.pack(B, T, H, D, R, positions.shape[0], bool(adjacent), bool(inverse),
-                               _DTYPES[x.dtype], *x.stride()[:3], *out.stride()[:3],
-                               *positions.stride())
+    shape = _ROTATE_SHAPE.pack(B, T, H, D, R, axes, bool(adjacent), bool(inverse), _DTYPES[x.dtype],
+                               *x.stride()[:3], *out.stride()[:3], *positions.stride())
     _check(_call(load().dconv_rotate, x, shape, x.data_ptr(), positions.data_ptr(), freq.data_ptr(),
                  axis.data_ptr(), out.data_ptr()))
     return out
@@ -140,18 +151,18 @@ def _join_arguments(branch, x, norm, post, post_weight, gate, pre_weight, pre_bi
                     branch_scale, eps, dh=None, dy=None):
     """Checks, and the C struct."""
     _tensor(x, "x", 3)
-    dev = x.device
-    B, T, D = x.shape
+    dtype, index, size = x.dtype, x.get_device(), x.shape
+    B, T, D = size
     if norm not in _NORMS:
         raise ValueError("norm must be one of %s" % sorted(_NORMS))
     strides = []
     for t, name in ((branch, "branch"), (x, "x"), (dh, "dh"), (dy, "dy")):
         if t is None:
-            strides += [0, 0]
+            strides += (0, 0)
             continue
-        if t is not x:
-            _tensor(t, name, 3, x.dtype, dev)
-            _shaped(t, name, x.shape)
+        if t is not x and not (_plain(t, 3, dtype, index) and t.shape == size):
+            _tensor(t, name, 3, dtype, x.device)
+            _shaped(t, name, size)
         strides += t.stride()[:2]
     if branch is None and (gate is not None or post_weight is not None):
         raise ValueError("gate and post_weight need a branch")
@@ -162,17 +173,19 @@ def _join_arguments(branch, x, norm, post, post_weight, gate, pre_weight, pre_bi
                          (pre_weight, "pre_weight", _PRE_WEIGHT), (pre_bias, "pre_bias", _PRE_BIAS)):
         if t is None:
             continue
-        if not isinstance(t, torch.Tensor) or t.dtype not in (torch.float32, x.dtype) or \
-                t.device != dev or not t.is_contiguous():
-            raise ValueError("%s must be a contiguous tensor of float32 or %s on %s" % (name, x.dtype, dev))
-        if vt is not None and t.dtype != vt:
+        if not (isinstance(t, torch.Tensor) and (t.dtype is torch.float32 or t.dtype is dtype)
+                and t.is_cuda and t.get_device() == index and t.is_contiguous()):
+            raise ValueError("%s must be a contiguous tensor of float32 or %s on %s" % (name, dtype, x.device))
+        if vt is None:
+            vt = t.dtype
+        elif t.dtype is not vt:
             raise ValueError("the vectors must have one type")
-        vt = t.dtype
-        if t.dim() == 2 and tuple(t.shape) == (B, D):
+        shape = t.shape
+        if len(shape) == 2 and shape[0] == B and shape[1] == D:
             per |= bit
-        elif tuple(t.shape) != (D,):
-            raise ValueError("%s must be %r or %r, got %r" % (name, (D,), (B, D), tuple(t.shape)))
-    return _JOIN_SHAPE.pack(B, T, D, _DTYPES[x.dtype], _DTYPES[vt or x.dtype], _NORMS[norm],
+        elif len(shape) != 1 or shape[0] != D:
+            raise ValueError("%s must be %r or %r, got %r" % (name, (D,), (B, D), tuple(shape)))
+    return _JOIN_SHAPE.pack(B, T, D, _DTYPES[dtype], _DTYPES[vt or dtype], _NORMS[norm],
                             bool(post and branch is not None), per, residual_scale, branch_scale, eps,
                             *strides)
 
@@ -200,10 +213,9 @@ def join(branch: torch.Tensor | None, x: torch.Tensor, *, norm: str = "rms", pos
         raise ValueError("nothing to compute: no branch and pre=False")
     if not pre and (pre_weight is not None or pre_bias is not None):
         raise ValueError("pre_weight and pre_bias need pre=True")
-    h = None if branch is None else torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    y = torch.empty(x.shape, dtype=x.dtype, device=x.device) if pre else None
-    stats = torch.empty((x.shape[0], x.shape[1], 4), dtype=torch.float32, device=x.device) \
-        if return_stats else None
+    h = None if branch is None else torch.empty_like(x, memory_format=torch.contiguous_format)
+    y = torch.empty_like(x, memory_format=torch.contiguous_format) if pre else None
+    stats = torch.empty((*x.shape[:2], 4), dtype=torch.float32, device=x.device) if return_stats else None
     _check(_call(load().dconv_join, x, shape, _ptr(branch), x.data_ptr(), _ptr(post_weight), _ptr(gate),
                  _ptr(pre_weight), _ptr(pre_bias), _ptr(h), _ptr(y), _ptr(stats)))
     return (h, y, stats) if return_stats else (h, y)
@@ -224,8 +236,8 @@ def join_backward(dh, dy, branch, x: torch.Tensor, stats: torch.Tensor, *, norm:
         raise ValueError("stats must be contiguous")
     grads = {}
     if branch is not None:
-        grads["branch"] = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    grads["x"] = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        grads["branch"] = torch.empty_like(x, memory_format=torch.contiguous_format)
+    grads["x"] = torch.empty_like(x, memory_format=torch.contiguous_format)
     for t, name in ((post_weight, "post_weight"), (gate, "gate"), (pre_weight, "pre_weight"),
                     (pre_bias, "pre_bias")):
         if t is not None:
@@ -245,26 +257,27 @@ def join_backward(dh, dy, branch, x: torch.Tensor, stats: torch.Tensor, *, norm:
 # ---------------------------------------------------------------------------
 def _attend_arguments(q, k, v, left, right, sinks, scale, lengths, starts, out, dout=None):
     _tensor(q, "q", 4)
-    dt, dev = q.dtype, q.device
-    _tensor(k, "k", 4, dt, dev)
-    _tensor(v, "v", 4, dt, dev)
-    B, Tq, Hq, D = q.shape
-    Tk, Hkv = k.shape[1], k.shape[2]
-    _shaped(k, "k", (B, Tk, Hkv, D))
-    _shaped(v, "v", k.shape)
+    dt, dev, index = q.dtype, q.device, q.get_device()
+    B, Tq, Hq, D = size = q.shape
+    if not (_plain(k, 4, dt, index) and _plain(v, 4, dt, index)):
+        _tensor(k, "k", 4, dt, dev)
+        _tensor(v, "v", 4, dt, dev)
+    Bk, Tk, Hkv, Dk = k.shape
+    if Bk != B or Dk != D or v.shape != k.shape:
+        _shaped(k, "k", (B, Tk, Hkv, D))
+        _shaped(v, "v", k.shape)
     if Hkv < 1 or Hq % Hkv:
         raise ValueError("%d query heads do not share %d key heads" % (Hq, Hkv))
     if left < -1 or right < -1 or sinks < 0:
         raise ValueError("left and right must be -1 (no limit) or more, sinks 0 or more")
     for t, name in ((lengths, "lengths"), (starts, "starts")):
-        if t is not None:
+        if t is not None and not (_plain(t, 1, torch.int32, index) and t.shape[0] == B):
             _tensor(t, name, 1, torch.int32, dev)
             _shaped(t, name, (B,))
-    _tensor(out, "out", 4, dt, dev)
-    _shaped(out, "out", q.shape)
-    if dout is not None:
-        _tensor(dout, "dout", 4, dt, dev)
-        _shaped(dout, "dout", q.shape)
+    for t, name in ((out, "out"), (dout, "dout")):
+        if t is not None and not (_plain(t, 4, dt, index) and t.shape == size):
+            _tensor(t, name, 4, dt, dev)
+            _shaped(t, name, size)
     return _ATTEND_SHAPE.pack(
         B, Tq, Tk, Hq, Hkv, D, _DTYPES[dt], left, right, sinks,
         1.0 / math.sqrt(D) if scale is None else scale, *q.stride()[:3], *k.stride()[:3],
@@ -292,7 +305,7 @@ def attend(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *, left: int = -1,
     if out is None:
         if not isinstance(q, torch.Tensor):
             raise ValueError("q must be a torch.Tensor")
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
     shape = _attend_arguments(q, k, v, left, right, sinks, scale, lengths, starts, out)
     lse = torch.empty((q.shape[0], q.shape[2], q.shape[1]), dtype=torch.float32, device=q.device) \
         if return_lse else None
@@ -315,7 +328,7 @@ def attend_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: tor
     _shaped(lse, "lse", (q.shape[0], q.shape[2], q.shape[1]))
     if not lse.is_contiguous():
         raise ValueError("lse must be contiguous")
-    dq, dk, dv = (torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v))
+    dq, dk, dv = (torch.empty_like(t, memory_format=torch.contiguous_format) for t in (q, k, v))
     lib = load()
     ws, n = _workspace(lib.dconv_attend_backward_workspace, shape, q.device)
     _check(_call(lib.dconv_attend_backward, q, shape, dout.data_ptr(), q.data_ptr(), k.data_ptr(),
