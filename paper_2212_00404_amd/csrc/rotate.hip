@@ -82,25 +82,17 @@ __device__ __forceinline__ void store_pack(T *p, const Pack<T, V, WHOLE> &x, int
 struct Work {
   int pieces, pairs;   // pieces per token, those that hold pairs
   int split;           // threads that share a token's heads
-  int64_t threads;
+  uint32_t threads;    // per sequence
 };
 
 // Pieces of V elements (16 bytes).  WHOLE: on 16-byte boundaries, without a
 // remainder in a piece of pairs or past them.
 template <class T, bool ADJACENT, bool WHOLE>
-__global__ __launch_bounds__(256) void rotate_pieces(const dconv_rotate_shape sh, const Work wk, const T *x,
-                                                     const float *__restrict__ positions,
-                                                     const float *__restrict__ freq, const int *__restrict__ axis,
-                                                     T *out) {
+__device__ __forceinline__ void rotate_piece(const dconv_rotate_shape &sh, const Work &wk, const T *x,
+                                             const float *__restrict__ positions, const float *__restrict__ freq,
+                                             const int *__restrict__ axis, T *out, int piece, int h0, int64_t t,
+                                             int64_t b) {
   constexpr int V = 16 / sizeof(T), P = ADJACENT ? V / 2 : V;   // pairs per piece
-  const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (id >= wk.threads) return;
-  const int piece = (int)(id % wk.pieces);
-  const int64_t rest = id / wk.pieces;
-  const int h0 = (int)(rest % wk.split);
-  const int64_t token = rest / wk.split;
-  const int t = (int)(token % sh.T);
-  const int64_t b = token / sh.T;
   const T *xr = x + b * sh.x_stride[0] + t * sh.x_stride[1];
   T *yr = out + b * sh.out_stride[0] + t * sh.out_stride[1];
 
@@ -156,6 +148,19 @@ __global__ __launch_bounds__(256) void rotate_pieces(const dconv_rotate_shape sh
 }
 
 template <class T, bool ADJACENT, bool WHOLE>
+__global__ __launch_bounds__(256) void rotate_pieces(const dconv_rotate_shape sh, const Work wk, const T *x,
+                                                     const float *__restrict__ positions,
+                                                     const float *__restrict__ freq, const int *__restrict__ axis,
+                                                     T *out) {
+  const uint32_t id = blockIdx.x * 256u + threadIdx.x;
+  if (id >= wk.threads) return;
+  const uint32_t rest = id / wk.pieces, t = rest / wk.split;
+  const int piece = (int)(id - rest * wk.pieces), h0 = (int)(rest - t * wk.split);
+  for (int b = blockIdx.y; b < sh.B; b += gridDim.y)
+    rotate_piece<T, ADJACENT, WHOLE>(sh, wk, x, positions, freq, axis, out, piece, h0, t, b);
+}
+
+template <class T, bool ADJACENT, bool WHOLE>
 void launch_pieces(const dconv_rotate_shape &sh, const void *x, const float *positions, const float *freq,
                    const int *axis, void *out, hipStream_t s) {
   constexpr int V = 16 / sizeof(T), P = ADJACENT ? V / 2 : V;
@@ -166,9 +171,9 @@ void launch_pieces(const dconv_rotate_shape &sh, const void *x, const float *pos
   const int64_t per_head = (int64_t)sh.B * sh.T * wk.pieces;
   const int64_t split = (kThreads + per_head - 1) / per_head;
   wk.split = (int)(split < sh.H ? split : sh.H);
-  wk.threads = per_head * wk.split;
-  hipLaunchKernelGGL((rotate_pieces<T, ADJACENT, WHOLE>), dim3((unsigned)((wk.threads + 255) / 256)), dim3(256), 0, s,
-                     sh, wk, (const T *)x, positions, freq, axis, (T *)out);
+  wk.threads = (uint32_t)((int64_t)sh.T * wk.pieces * wk.split);
+  hipLaunchKernelGGL((rotate_pieces<T, ADJACENT, WHOLE>), dim3((wk.threads + 255) / 256, sh.B < 65535 ? sh.B : 65535),
+                     dim3(256), 0, s, sh, wk, (const T *)x, positions, freq, axis, (T *)out);
 }
 
 template <class T>
@@ -198,9 +203,9 @@ DCONV_EXPORT int dconv_rotate(const dconv_rotate_shape *shape, const void *x,
   if (sh.B < 0 || sh.T < 0 || sh.H < 1 || sh.D < 1 || sh.R < 0 || sh.R > sh.D / 2 ||
       sh.axes < 1 || (sh.adjacent & ~1) || (sh.inverse & ~1) || !dconv::element_size(sh.dtype))
     return DCONV_EINVAL;
-  // threads are counted by 2^31 workgroups of 256, a piece of an element each at most
-  if (sh.H > INT_MAX / sh.D || (int64_t)sh.B * sh.T > ((int64_t)INT_MAX * 256) / ((int64_t)sh.H * sh.D))
-    return DCONV_ERANGE;
+  // a sequence's pieces, one thread each at most, are counted in 32 bits
+  const int64_t pieces = (int64_t)sh.D * dconv::element_size(sh.dtype) / 16 + 3;
+  if (sh.H > INT_MAX / sh.D || sh.T > (int64_t)(UINT32_MAX - 255) / (sh.H * pieces)) return DCONV_ERANGE;
   if (sh.B == 0 || sh.T == 0) return DCONV_OK;
   if (!x || !out || (sh.R > 0 && (!positions || !freq || !axis))) return DCONV_ENULL;
   (void)hipGetLastError();  // report this launch only
