@@ -54,7 +54,7 @@ extern "C" {
 #define DCONV_OK 0
 #define DCONV_ENULL (-1)        /* a required pointer is NULL */
 #define DCONV_EINVAL (-2)       /* C, M or K < 1, K > Wx, K > Wy, or bad variant */
-#define DCONV_ERANGE (-3)       /* a tensor has more than 2^31-1 elements */
+#define DCONV_ERANGE (-3)       /* more elements (convolutions: 2^31-1) or rows than are counted */
 #define DCONV_EHIP (-4)         /* the HIP runtime reported an error */
 #define DCONV_EUNSUPPORTED (-5) /* the forced variant cannot run this shape */
 #define DCONV_EWORKSPACE (-6)   /* the workspace is smaller than the call needs */

@@ -217,10 +217,13 @@ DCONV_EXPORT const char *dconv_strerror(int status) {
     case DCONV_ENULL: return "a required pointer is NULL";
     case DCONV_EINVAL:
       return "invalid size, variant or plan (need C, M, K >= 1 and K <= min(Wx, Wy); a plan "
-             "must be one of the candidates for these sizes)";
-    case DCONV_ERANGE: return "a tensor has more than 2^31-1 elements";
+             "must be one of the candidates for these sizes), or another option out of its range";
+    case DCONV_ERANGE:
+      return "a tensor has more than 2^31-1 elements (the operators over tokens: more rows than "
+             "are counted)";
     case DCONV_EHIP: return "the HIP runtime reported an error";
     case DCONV_EUNSUPPORTED: return "the requested kernel family cannot run this shape";
+    case DCONV_EWORKSPACE: return "the workspace is smaller than the call needs";
     default: return "unknown status";
   }
 }
