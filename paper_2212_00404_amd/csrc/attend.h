@@ -200,12 +200,12 @@ void launch_attend(const dconv_attend_shape &sh, const AttendPtrs &p, const Forw
 
 // How a backward call runs (head sizes up to 128): dq by tiles of 128 rows; dk
 // and dv of the keys [0, first) by tiles of 32 with the rows divided
-// (attend_dkv_split), of the others by tiles of 128 (attend_dkv).
+// (attend_dkv_split), of the others by tiles of key_groups * 32 (attend_dkv).
 constexpr int kGradMaxD = 128;
 struct BackwardPlan {
   bool direct, near;
   int dp;
-  int row_tiles, key_tiles;
+  int row_tiles, key_tiles, key_groups;
   int first, first_tiles, parts;
   int64_t stats_bytes, workspace;
 };

@@ -103,11 +103,11 @@ BackwardPlan plan_backward(const dconv_attend_shape &sh) {
   const int G = sh.Hq / sh.Hkv;
   const int64_t rows = (int64_t)sh.Tq * G, heads = (int64_t)sh.B * sh.Hkv;
   f.row_tiles = (int)((rows + 127) / 128);
-  f.key_tiles = (sh.Tk + 127) / 128;
-  // the keys that every row sees, where the others are seen by a window of rows;
-  // all keys where 128 of them per workgroup would leave half the chip idle
+  // 128 keys per workgroup where that gives every compute unit one, else 64
+  f.key_groups = heads * ((sh.Tk + 127) / 128) >= 256 ? 4 : 2;
+  f.key_tiles = (sh.Tk + 32 * f.key_groups - 1) / (32 * f.key_groups);
+  // the keys that every row sees, where the others are seen by a window of rows
   f.first = sh.left < 0 ? 0 : sh.sinks < sh.Tk ? sh.sinks : sh.Tk;
-  if (heads * f.key_tiles < 128) f.first = sh.Tk;
   f.first_tiles = (f.first + 31) / 32;
   f.parts = 1;
   if (f.first > 0) {

@@ -23,6 +23,14 @@ struct GradTile {
   int parts;         // parts of the rows (attend_dkv_split)
 };
 
+// in_order() for head sizes whose operands fit the registers beside the sums.
+template <class T, int DP>
+constexpr bool kAhead = DP * sizeof(T) <= 128;
+template <class T, int DP>
+__device__ __forceinline__ void read_ahead() {
+  if constexpr (kAhead<T, DP>) in_order();
+}
+
 template <class T>
 __device__ __forceinline__ float frag_dot(typename Mma<T>::Frag a, typename Mma<T>::Frag b) {
   float s = 0.0f;
@@ -102,17 +110,31 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= 128 ? 2 : 1) void attend_dq(
   float miss = 0.0f;
 #pragma unroll
   for (int c = 0; c < DT; ++c) acc[c] = mean[c] = f32x16{};
+  auto columns = [&](Frag(&f)[DT], const T *t, int row) {
+#pragma unroll
+    for (int c = 0; c < DT; ++c) f[c] = Tile<T, DP>::column(t, row, c, lane);
+  };
   auto step = [&](const T *buf, int v0) {
     if (v0 >= to || (v0 + BN <= from && v0 >= sh.sinks)) return;
     const bool masked = !(v0 + BN <= all_to && (v0 >= all_from || v0 + BN <= sh.sinks));
     const T *ks = buf, *vs = buf + BN * DP;
 #pragma unroll
     for (int hb = 0; hb < BN / 32; ++hb) {
+      Frag a[KS], x[KS], col[2][DT];
+#pragma unroll
+      for (int k = 0; k < KS; ++k) a[k] = Tile<T, DP>::row(ks, 32 * hb, k, lane);
+#pragma unroll
+      for (int k = 0; k < KS; ++k) x[k] = Tile<T, DP>::row(vs, 32 * hb, k, lane);
+      read_ahead<T, DP>();
       f32x16 s = {}, dp = {};
 #pragma unroll
-      for (int k = 0; k < KS; ++k) s = Mma<T>::mac(Tile<T, DP>::row(ks, 32 * hb, k, lane), q[k], s);
+      for (int k = 0; k < KS; ++k) s = Mma<T>::mac(a[k], q[k], s);
+      if constexpr (kAhead<T, DP>) columns(col[0], ks, 32 * hb);
+      read_ahead<T, DP>();
 #pragma unroll
-      for (int k = 0; k < KS; ++k) dp = Mma<T>::mac(Tile<T, DP>::row(vs, 32 * hb, k, lane), g[k], dp);
+      for (int k = 0; k < KS; ++k) dp = Mma<T>::mac(x[k], g[k], dp);
+      if constexpr (kAhead<T, DP>) columns(col[1], ks, 32 * hb + 16);
+      read_ahead<T, DP>();
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         s[i] = power2<T>(fmaf(s[i], at.scale2, -lse2));
@@ -130,17 +152,17 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= 128 ? 2 : 1) void attend_dq(
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
         const Frag w = as_operand<T>(s, k), u = as_operand<T>(dp, k);
+        if constexpr (!kAhead<T, DP>) columns(col[k], ks, 32 * hb + 16 * k);
 #pragma unroll
         for (int c = 0; c < DT; ++c) {
-          const Frag x = Tile<T, DP>::column(ks, 32 * hb + 16 * k, c, lane);
-          acc[c] = Mma<T>::mac(x, u, acc[c]);
-          mean[c] = Mma<T>::mac(x, w, mean[c]);
+          acc[c] = Mma<T>::mac(col[k][c], u, acc[c]);
+          mean[c] = Mma<T>::mac(col[k][c], w, mean[c]);
         }
       }
     }
   };
   auto arrived = [&]() {
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    landed<0>();
     __syncthreads();
   };
   for (int v0 = 0; v0 < n; v0 += 2 * BN) {
@@ -207,16 +229,34 @@ struct KeyGrad {
   __device__ __forceinline__ void add(const T *qs, const T *gs, const f32x2 *st, int r, int lo, int hi, bool masked,
                                       float scale2, int lane) {
     const int half = lane >> 5;
+    // operands are read well before their products: LDS answers after some
+    // hundred clocks, and two waves per SIMD do not cover that for one another
+    Frag a[KS], b[KS], cg[2][DT], cq[2][DT];
+#pragma unroll
+    for (int x = 0; x < KS; ++x) a[x] = Tile<T, DP>::row(qs, 0, x, lane);
+#pragma unroll
+    for (int x = 0; x < KS; ++x) b[x] = Tile<T, DP>::row(gs, 0, x, lane);
+    read_ahead<T, DP>();
     f32x16 s = {}, dp = {};
 #pragma unroll
-    for (int x = 0; x < KS; ++x) s = Mma<T>::mac(Tile<T, DP>::row(qs, 0, x, lane), k[x], s);
+    for (int x = 0; x < KS; ++x) s = Mma<T>::mac(a[x], k[x], s);
+    // (base, delta) of the rows 8 i + 4 half .. + 3
+    f32x4 st4[8];
 #pragma unroll
-    for (int x = 0; x < KS; ++x) dp = Mma<T>::mac(Tile<T, DP>::row(gs, 0, x, lane), v[x], dp);
+    for (int i = 0; i < 4; ++i) {
+      st4[2 * i] = *reinterpret_cast<const f32x4 *>(st + 8 * i + 4 * half);
+      st4[2 * i + 1] = *reinterpret_cast<const f32x4 *>(st + 8 * i + 4 * half + 2);
+    }
+    read_ahead<T, DP>();
+#pragma unroll
+    for (int x = 0; x < KS; ++x) dp = Mma<T>::mac(b[x], v[x], dp);
+    if constexpr (kAhead<T, DP>) columns(cg[0], cq[0], gs, qs, 0, lane);
+    read_ahead<T, DP>();
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      const f32x2 x = st[acc_row(i, half)];
-      s[i] = power2<T>(fmaf(s[i], scale2, -x[0]));
-      dp[i] = s[i] * (dp[i] - x[1]);
+      const f32x4 x = st4[i / 4 * 2 + i % 4 / 2];
+      s[i] = power2<T>(fmaf(s[i], scale2, -x[i % 2 * 2]));
+      dp[i] = s[i] * (dp[i] - x[i % 2 * 2 + 1]);
     }
     if (masked) {
       no_speculation();
@@ -225,14 +265,25 @@ struct KeyGrad {
         dp[i] = on ? dp[i] : 0.0f;
       });
     }
+    if constexpr (kAhead<T, DP>) columns(cg[1], cq[1], gs, qs, 16, lane);
+    read_ahead<T, DP>();
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
       const Frag w = as_operand<T>(s, x), u = as_operand<T>(dp, x);
+      if constexpr (!kAhead<T, DP>) columns(cg[x], cq[x], gs, qs, 16 * x, lane);
 #pragma unroll
       for (int c = 0; c < DT; ++c) {
-        dv[c] = Mma<T>::mac(Tile<T, DP>::column(gs, 16 * x, c, lane), w, dv[c]);
-        dk[c] = Mma<T>::mac(Tile<T, DP>::column(qs, 16 * x, c, lane), u, dk[c]);
+        dv[c] = Mma<T>::mac(cg[x][c], w, dv[c]);
+        dk[c] = Mma<T>::mac(cq[x][c], u, dk[c]);
       }
+    }
+  }
+  static __device__ __forceinline__ void columns(Frag (&cg)[DT], Frag (&cq)[DT], const T *gs, const T *qs, int r,
+                                                 int lane) {
+#pragma unroll
+    for (int c = 0; c < DT; ++c) {
+      cg[c] = Tile<T, DP>::column(gs, r, c, lane);
+      cq[c] = Tile<T, DP>::column(qs, r, c, lane);
     }
   }
 };
@@ -336,34 +387,36 @@ struct RowTiles {
   }
 };
 
-constexpr int kGradKeys = 128;
 
-// 128 keys per workgroup, 32 per wave; tiles of 32 rows of queries and dout for
-// each row group in two LDS buffers, the next ones copied while the current ones
-// are used.  With two row groups of four waves each, a workgroup alone on its
-// compute unit (256 of them at 2 x 4096 keys and four key heads) has two waves per
-// SIMD to fill each other's waits; the second's sums are added to the first's at
-// the end.  Larger heads leave registers for one.
+// 32 keys per wave and KG key groups of them per workgroup; its waves form RG row
+// groups, which take kStepTiles tiles of 32 rows of queries and dout each per step
+// (one tile's products are too short for the next one's copies) and are added at
+// the end.  Eight waves, so that a workgroup alone on its compute unit has two waves
+// per SIMD to fill each other's waits (2 x 4096 keys, four key heads, 256 workgroups:
+// 75 us, 92 with four waves); larger heads leave registers for four.  KG = 4 reads
+// the rows least often; KG = 2 makes twice the workgroups.
 template <class T>
-constexpr int row_groups(int dp) { return dp * (int)sizeof(T) <= 192 ? 2 : 1; }
+constexpr int grad_waves(int dp) { return dp * (int)sizeof(T) <= 128 ? 8 : 4; }
 
-template <class T, int DP>
-__global__ __launch_bounds__(256 * row_groups<T>(DP)) void attend_dkv(const dconv_attend_shape sh, const AttendPtrs p,
-                                                                      const GradTile gt) {
-  constexpr int RG = row_groups<T>(DP), BM = 32 * RG, DT = DP / 32;
-  constexpr int kBuf = RG > 1 && 2 * BM * DP * sizeof(T) < 16384 ? 16384 / (int)sizeof(T) : 2 * BM * DP;
+template <class T, int DP, int KG>
+__global__ __launch_bounds__(64 * grad_waves<T>(DP)) void attend_dkv(const dconv_attend_shape sh, const AttendPtrs p,
+                                                                     const GradTile gt) {
+  constexpr int W = grad_waves<T>(DP), RG = W / KG, DT = DP / 32;
+  constexpr int R = 32 * RG * DP * (int)sizeof(T) <= 8192 ? 2 : 1, BM = 32 * RG * R;
+  constexpr int kMerge = KG * (RG - 1) * 1024 * 4 / (int)sizeof(T);   // sums of one 32-column part
+  constexpr int kBuf = 2 * BM * DP > kMerge ? 2 * BM * DP : kMerge;
   __shared__ __align__(16) T buf0[kBuf];
   __shared__ __align__(16) T buf1[kBuf];
   __shared__ __align__(16) f32x2 stats0[BM];
   __shared__ __align__(16) f32x2 stats1[BM];
-  __shared__ int span[2][4];
+  __shared__ int span[2][KG];
   DCONV_POISON(poison_lds(buf0, kBuf); poison_lds(buf1, kBuf); poison_lds(stats0, BM); poison_lds(stats1, BM));
   const AttendTile &at = gt.a;
   const int lane = threadIdx.x & 63, half = lane >> 5, wave = uniform(threadIdx.x >> 6);
-  const int kg = wave & 3, rg = wave >> 2;   // key group, row group
+  const int kg = wave % KG, rg = wave / KG;   // key group, row group
   const int id = xcd_remap(blockIdx.x, gridDim.x);
   const int bh = id / at.tiles, b = bh / sh.Hkv, hk = bh % sh.Hkv;
-  const int j = (id % at.tiles) * kGradKeys + 32 * kg + (lane & 31), jj = min(j, sh.Tk - 1);
+  const int j = (id % at.tiles) * (32 * KG) + 32 * kg + (lane & 31), jj = min(j, sh.Tk - 1);
   const Seq seq = seq_of(sh, p, b);
   const KeyRows see = key_rows(sh, seq, j, gt.first, sh.Tk);
   const TileRows mine = tile_rows(see);
@@ -372,22 +425,30 @@ __global__ __launch_bounds__(256 * row_groups<T>(DP)) void attend_dkv(const dcon
     span[1][kg] = mine.to;
   }
   __syncthreads();
-  const int from = uniform(min(min(span[0][0], span[0][1]), min(span[0][2], span[0][3])));
-  const int to = uniform(max(max(span[1][0], span[1][1]), max(span[1][2], span[1][3])));
+  int from = span[0][0], to = span[1][0];
+#pragma unroll
+  for (int x = 1; x < KG; ++x) {
+    from = min(from, span[0][x]);
+    to = max(to, span[1][x]);
+  }
+  from = uniform(from), to = uniform(to);
 
-  const RowTiles<T, DP, BM, 4 * RG> tiles(sh, p, gt, b, hk, wave, lane);
+  const RowTiles<T, DP, BM, W> tiles(sh, p, gt, b, hk, wave, lane);
   auto stage = [&](T *buf, f32x2 *st, int r) { tiles.stage(buf, st, sh, at.direct, r, to, wave, lane); };
   if (from < to) stage(buf0, stats0, from);
   KeyGrad<T, DP> acc;
   acc.load(sh, at, row_of<T>(p.k, sh.k_stride, b, jj, hk), row_of<T>(p.v, sh.v_stride, b, jj, hk), half);
   auto step = [&](const T *buf, const f32x2 *st, int r) {
-    buf += 32 * rg * DP, st += 32 * rg, r += 32 * rg;
-    if (r >= mine.to || r + 32 <= mine.from) return;
-    acc.add(buf, buf + BM * DP, st, r, see.lo, see.hi, !(r >= mine.all_from && r + 32 <= mine.all_to), at.scale2,
-            lane);
+#pragma unroll
+    for (int x = 0; x < R; ++x) {
+      const int row = 32 * (rg * R + x);
+      if (r + row >= mine.to || r + row + 32 <= mine.from) continue;
+      acc.add(buf + row * DP, buf + (BM + row) * DP, st + row, r + row, see.lo, see.hi,
+              !(r + row >= mine.all_from && r + row + 32 <= mine.all_to), at.scale2, lane);
+    }
   };
   auto arrived = [&]() {
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    landed<0>();
     __syncthreads();
   };
   for (int r = from; r < to; r += 2 * BM) {
@@ -400,27 +461,31 @@ __global__ __launch_bounds__(256 * row_groups<T>(DP)) void attend_dkv(const dcon
     step(buf1, stats1, r + BM);
   }
   if constexpr (RG > 1) {
-    float *xk = reinterpret_cast<float *>(buf0) + kg * 1024, *xv = reinterpret_cast<float *>(buf1) + kg * 1024;
 #pragma unroll
     for (int c = 0; c < DT; ++c) {
       __syncthreads();   // every wave is done with what the buffers hold
-      if (rg == 1) {
+      if (rg > 0) {
+        const int x = ((rg - 1) * KG + kg) * 1024 + lane;
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-          xk[64 * i + lane] = acc.dk[c][i];
-          xv[64 * i + lane] = acc.dv[c][i];
+          reinterpret_cast<float *>(buf0)[x + 64 * i] = acc.dk[c][i];
+          reinterpret_cast<float *>(buf1)[x + 64 * i] = acc.dv[c][i];
         }
       }
       __syncthreads();
       if (rg == 0) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          acc.dk[c][i] += xk[64 * i + lane];
-          acc.dv[c][i] += xv[64 * i + lane];
+        for (int g = 0; g < RG - 1; ++g) {
+          const int x = (g * KG + kg) * 1024 + lane;
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            acc.dk[c][i] += reinterpret_cast<const float *>(buf0)[x + 64 * i];
+            acc.dv[c][i] += reinterpret_cast<const float *>(buf1)[x + 64 * i];
+          }
         }
       }
     }
-    if (rg == 1) return;
+    if (rg > 0) return;
   }
 
   bool bad = false;
@@ -447,11 +512,10 @@ __global__ __launch_bounds__(256 * row_groups<T>(DP)) void attend_dkv(const dcon
       }
   }
   for (unsigned again = redo; again; again &= again - 1)
-    attend_row_dkv<T>(sh, p, b, hk, (id % at.tiles) * kGradKeys + 32 * kg + __ffs(again) - 1);
+    attend_row_dkv<T>(sh, p, b, hk, (id % at.tiles) * (32 * KG) + 32 * kg + __ffs(again) - 1);
 }
 
-// Keys [0, gt.first) in tiles of 32: the first keys, which every row sees, or all
-// keys of a small call.  The rows are divided over the waves, each with two LDS
+// Keys [0, gt.first) in tiles of 32: the first keys, which every row sees.  The rows are divided over the waves, each with two LDS
 // buffers of its own, and over gt.parts workgroups, which leave their sums in the
 // workspace.
 template <class T, int DP>
@@ -483,7 +547,7 @@ __global__ __launch_bounds__(64 * split_waves<T>(DP)) void attend_dkv_split(cons
     const T *from = buf + wave * 2 * kTile;
     acc.add(from, from + kTile, st + wave * 32, r, see.lo, see.hi, true, at.scale2, lane);
   };
-  auto arrived = [&]() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory"); };
+  auto arrived = [&]() { landed<0>(); };
   const int stride = 32 * gt.parts * W;
   if (mine.from < mine.to) {
     int r = mine.from + 32 * (part * W + wave);
@@ -572,8 +636,11 @@ void launch_attend_grad(const dconv_attend_shape &sh, const AttendPtrs &p, const
     }
     if (plan.first < sh.Tk) {
       gt.a.tiles = plan.key_tiles;
-      hipLaunchKernelGGL((attend_dkv<T, DP>), dim3(heads * plan.key_tiles),
-                         dim3(256 * row_groups<T>(DP)), 0, s, sh, p, gt);
+      const dim3 grid(heads * plan.key_tiles), block(64 * grad_waves<T>(DP));
+      if (plan.key_groups == 4)
+        hipLaunchKernelGGL((attend_dkv<T, DP, 4>), grid, block, 0, s, sh, p, gt);
+      else
+        hipLaunchKernelGGL((attend_dkv<T, DP, 2>), grid, block, 0, s, sh, p, gt);
     }
     if (plan.first > 0) {
       gt.a.tiles = plan.first_tiles;

@@ -202,6 +202,17 @@ __device__ __forceinline__ typename Mma<T>::Frag load_frag(const T *row, int d, 
   return f;
 }
 
+// Waits until at most N of this wave's copies, and no LDS operation, are on their
+// way.  (As an instruction that the compiler knows: it counts copies into LDS too,
+// and after a wait it cannot see it would put its own, for all of them, before the
+// first read.)
+template <int N>
+__device__ __forceinline__ void landed() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt((N & 15) | 7 << 4 | (N >> 4) << 14);   // vmcnt(N) lgkmcnt(0)
+  asm volatile("" ::: "memory");
+}
+
 // 2^x.  The instruction gives 0 below 2^-126; fp32 tensors keep such values, for
 // 16-bit ones they are far below what a probability is rounded to.
 template <class T>
@@ -517,7 +528,7 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1) void attend_til
       soft.add(buf, buf + BN * DP, q, v0, see, sh.sinks, at.scale2, lane);
   };
   auto arrived = [&]() {
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    landed<0>();
     __syncthreads();
   };
   if (n > 0) stage(buf0, 0);
@@ -654,7 +665,7 @@ __global__ __launch_bounds__(64 * split_waves<T>(DP), 1) void attend_split(const
     const T *mine = buf + wave * 2 * kTile;
     soft.add(mine, mine + kTile, q, v0, see, sh.sinks, at.scale2, lane);
   };
-  auto arrived = [&]() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory"); };
+  auto arrived = [&]() { landed<0>(); };
   // tiles part * W + wave, then every (splits * W)-th
   const int stride = 32 * at.splits * W;
   int v0 = 32 * (part * W + wave);
