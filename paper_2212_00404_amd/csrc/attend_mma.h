@@ -426,9 +426,9 @@ struct Softmax {
 
   // Adds 32 keys, v0 .., of the tiles ks, vs.
   __device__ __forceinline__ void add(const T *ks, const T *vs, const Frag (&q)[KS], int v0, const RowKeys &see,
-                                      int sinks, float scale2, int lane) {
+                                      int sinks, float scale2, bool masked, int lane) {
     f32x16 s = scores(ks, 0, q, lane);
-    mask(s, v0, see, sinks, lane);
+    if (masked) mask(s, v0, see, sinks, lane);
     follow(s, scale2, [] {});
     Frag w[2];
     probabilities(s, scale2, w);
@@ -519,13 +519,20 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1) void attend_til
   auto stage = [&](T *buf, int v0) { tiles.stage(buf, at, keys, n, v0, sh.D, wave, lane); };
   Softmax<T, DP> soft;
   soft.clear();
+  // keys v0 .. v0 + N - 1 by the wave's rows: none seen, all seen
+  auto unseen = [&](int v0, int N) { return v0 >= to || (v0 + N <= from && v0 >= sh.sinks); };
+  auto masked = [&](int v0, int N) { return !(v0 + N <= all_to && (v0 >= all_from || v0 + N <= sh.sinks)); };
   auto step = [&](const T *buf, int v0) {
-    if (v0 >= to || (v0 + BN <= from && v0 >= sh.sinks)) return;
-    const bool masked = !(v0 + BN <= all_to && (v0 >= all_from || v0 + BN <= sh.sinks));
-    if constexpr (BN == 64)
-      soft.add_two(buf, buf + BN * DP, q, v0, see, sh.sinks, at.scale2, masked, lane);
-    else
-      soft.add(buf, buf + BN * DP, q, v0, see, sh.sinks, at.scale2, lane);
+    if constexpr (BN == 64 && sizeof(T) == 2) {
+      if (!unseen(v0, BN))
+        soft.add_two(buf, buf + BN * DP, q, v0, see, sh.sinks, at.scale2, masked(v0, BN), lane);
+    } else {
+      // (fp32: a tile's products last long enough by themselves)
+#pragma unroll
+      for (int k = 0; k < BN; k += 32)
+        if (!unseen(v0 + k, 32))
+          soft.add(buf + k * DP, buf + (BN + k) * DP, q, v0 + k, see, sh.sinks, at.scale2, masked(v0 + k, 32), lane);
+    }
   };
   auto arrived = [&]() {
     landed<0>();
@@ -663,7 +670,7 @@ __global__ __launch_bounds__(64 * split_waves<T>(DP), 1) void attend_split(const
   soft.clear();
   auto step = [&](const T *buf, int v0) {
     const T *mine = buf + wave * 2 * kTile;
-    soft.add(mine, mine + kTile, q, v0, see, sh.sinks, at.scale2, lane);
+    soft.add(mine, mine + kTile, q, v0, see, sh.sinks, at.scale2, true, lane);
   };
   auto arrived = [&]() { landed<0>(); };
   // tiles part * W + wave, then every (splits * W)-th
