@@ -114,12 +114,15 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= 128 ? 2 : 1) void attend_dq(
 #pragma unroll
     for (int c = 0; c < DT; ++c) f[c] = Tile<T, DP>::column(t, row, c, lane);
   };
+  // keys v .. v + 31 by the wave's rows: none seen, all seen
+  auto unseen = [&](int v) { return v >= to || (v + 32 <= from && v >= sh.sinks); };
+  auto all_seen = [&](int v) { return v + 32 <= all_to && (v >= all_from || v + 32 <= sh.sinks); };
   auto step = [&](const T *buf, int v0) {
-    if (v0 >= to || (v0 + BN <= from && v0 >= sh.sinks)) return;
-    const bool masked = !(v0 + BN <= all_to && (v0 >= all_from || v0 + BN <= sh.sinks));
     const T *ks = buf, *vs = buf + BN * DP;
 #pragma unroll
     for (int hb = 0; hb < BN / 32; ++hb) {
+      if (unseen(v0 + 32 * hb)) continue;
+      const bool masked = !all_seen(v0 + 32 * hb);
       Frag a[KS], x[KS], col[2][DT];
 #pragma unroll
       for (int k = 0; k < KS; ++k) a[k] = Tile<T, DP>::row(ks, 32 * hb, k, lane);
@@ -520,8 +523,9 @@ __global__ __launch_bounds__(64 * grad_waves<T>(DP)) void attend_dkv(const dconv
 // workspace.
 template <class T, int DP>
 __global__ __launch_bounds__(64 * split_waves<T>(DP)) void attend_dkv_split(const dconv_attend_shape sh,
-                                                                            const AttendPtrs p, const GradTile gt) {
-  constexpr int DT = DP / 32, kTile = 32 * DP, W = split_waves<T>(DP);
+                                                                                 const AttendPtrs p,
+                                                                                 const GradTile gt) {
+  constexpr int kTile = 32 * DP, W = split_waves<T>(DP);
   __shared__ __align__(16) T buf0[W * 2 * kTile];
   __shared__ __align__(16) T buf1[W * 2 * kTile];
   __shared__ __align__(16) f32x2 stats0[W * 32];
@@ -562,47 +566,52 @@ __global__ __launch_bounds__(64 * split_waves<T>(DP)) void attend_dkv_split(cons
       step(buf1, stats1, r + stride);
     }
   }
-  // the waves' sums as rows in LDS: first dk, then dv
-  auto lds_row = [&](int w, int x) {
-    return reinterpret_cast<float *>(x < 16 ? buf0 : buf1) + (w * 16 + (x & 15)) * DP;
-  };
+  // the waves' sums in LDS: first dk, then dv
+  const WaveSums<T, DP, W> sums = {buf0, buf1};
   for (int which = 0; which < 2; ++which) {
     __syncthreads();
-#pragma unroll
-    for (int c = 0; c < DT; ++c)
-#pragma unroll
-      for (int i = 0; i < 16; ++i)
-        lds_row(wave, lane & 31)[32 * c + acc_row(i, half)] = which ? acc.dv[c][i] : acc.dk[c][i];
+    sums.leave(wave, lane, which ? acc.dv : acc.dk);
     __syncthreads();
     float *out = at.partial + ((int64_t)blockIdx.x * 2 + which) * kTile;
     for (int x = threadIdx.x; x < kTile; x += 64 * W) {
       float s = 0.0f;
-      for (int w = 0; w < W; ++w) s += lds_row(w, x / DP)[x % DP];
+#pragma unroll
+      for (int w = 0; w < W; ++w) s += sums.get(w, x / DP, x % DP);
       out[x] = s;
     }
   }
 }
 
-// A wave per key adds the parts.
+// Four waves per key add the parts, each every fourth, then the waves in order.
 template <class T, int DP>
-__global__ __launch_bounds__(64) void attend_dkv_join(const dconv_attend_shape sh, const AttendPtrs p,
-                                                      const GradTile gt) {
-  const int lane = threadIdx.x, j = blockIdx.x % gt.first, bh = blockIdx.x / gt.first;
+__global__ __launch_bounds__(256) void attend_dkv_join(const dconv_attend_shape sh, const AttendPtrs p,
+                                                       const GradTile gt) {
+  __shared__ float sum[4][2][DP];
+  DCONV_POISON(poison_lds(&sum[0][0][0], 8 * DP));
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, j = blockIdx.x % gt.first, bh = blockIdx.x / gt.first;
   const int b = bh / sh.Hkv, hk = bh % sh.Hkv;
   const float *part = gt.a.partial + ((int64_t)bh * gt.a.tiles + j / 32) * gt.parts * 64 * DP + j % 32 * DP;
-  float dk[DP / 64 + 1], dv[DP / 64 + 1];
+#pragma unroll
+  for (int d = lane; d < DP; d += 64) {
+    float k = 0.0f, v = 0.0f;
+#pragma unroll 8
+    for (int x = wave; x < gt.parts; x += 4) {
+      k += part[(int64_t)x * 64 * DP + d];
+      v += part[(int64_t)x * 64 * DP + 32 * DP + d];
+    }
+    sum[wave][0][d] = k;
+    sum[wave][1][d] = v;
+  }
+  __syncthreads();
+  if (wave > 0) return;
+  float dk[(DP + 63) / 64], dv[(DP + 63) / 64];
   bool bad = false;
 #pragma unroll
-  for (int i = 0; i <= DP / 64; ++i) {
+  for (int i = 0; i < (DP + 63) / 64; ++i) {
     const int d = lane + 64 * i;
-    dk[i] = dv[i] = 0.0f;
     if (d >= sh.D) continue;
-#pragma unroll 8
-    for (int x = 0; x < gt.parts; ++x) {
-      dk[i] += part[(int64_t)x * 64 * DP + d];
-      dv[i] += part[(int64_t)x * 64 * DP + 32 * DP + d];
-    }
-    dk[i] *= sh.scale;
+    dk[i] = sh.scale * ((sum[0][0][d] + sum[1][0][d]) + (sum[2][0][d] + sum[3][0][d]));
+    dv[i] = (sum[0][1][d] + sum[1][1][d]) + (sum[2][1][d] + sum[3][1][d]);
     bad |= !(fabsf(dk[i]) < INFINITY && fabsf(dv[i]) < INFINITY);
   }
   if (kSumAgain && __any(bad)) {
@@ -611,7 +620,7 @@ __global__ __launch_bounds__(64) void attend_dkv_join(const dconv_attend_shape s
   }
   const int64_t o = (((int64_t)b * sh.Tk + j) * sh.Hkv + hk) * sh.D;
 #pragma unroll
-  for (int i = 0; i <= DP / 64; ++i)
+  for (int i = 0; i < (DP + 63) / 64; ++i)
     if (lane + 64 * i < sh.D) {
       ((T *)p.dk)[o + lane + 64 * i] = from_f32<T>(dk[i]);
       ((T *)p.dv)[o + lane + 64 * i] = from_f32<T>(dv[i]);
@@ -646,7 +655,7 @@ void launch_attend_grad(const dconv_attend_shape &sh, const AttendPtrs &p, const
       gt.a.tiles = plan.first_tiles;
       hipLaunchKernelGGL((attend_dkv_split<T, DP>), dim3(heads * plan.first_tiles * plan.parts),
                          dim3(64 * split_waves<T>(DP)), 0, s, sh, p, gt);
-      hipLaunchKernelGGL((attend_dkv_join<T, DP>), dim3(heads * plan.first), dim3(64), 0, s, sh, p, gt);
+      hipLaunchKernelGGL((attend_dkv_join<T, DP>), dim3(heads * plan.first), dim3(256), 0, s, sh, p, gt);
     }
   };
   if (plan.dp == 32) launch(std::integral_constant<int, 32>());

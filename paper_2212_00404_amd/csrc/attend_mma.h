@@ -596,22 +596,48 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1) void attend_til
 template <class T>
 constexpr int split_waves(int dp) { return dp * (int)sizeof(T) <= 256 ? 4 : dp * (int)sizeof(T) <= 512 ? 2 : 1; }
 
+// The result registers of W waves in LDS (in two buffers of W 2 x 32 x DP elements):
+// register i of part c of wave w in a row of 64 lanes, 65 floats apart, so that both
+// a register's lanes and a result row's elements lie on different banks (rows of
+// DP floats, written a row per lane, would put all lanes on one).
+template <class T, int DP, int W>
+struct WaveSums {
+  static constexpr int DT = DP / 32, kWave = DT * 16 * 65, kHalf = (W + 1) / 2;
+  static_assert(kHalf * kWave * sizeof(float) <= W * 2 * 32 * DP * sizeof(T), "half the waves fit a buffer");
+  T *buf0, *buf1;
+  __device__ __forceinline__ float *of(int w) const {
+    return reinterpret_cast<float *>(w < kHalf ? buf0 : buf1) + (w < kHalf ? w : w - kHalf) * kWave;
+  }
+  __device__ __forceinline__ void leave(int w, int lane, const f32x16 (&o)[DT]) const {
+    float *to = of(w) + lane;
+#pragma unroll
+    for (int c = 0; c < DT; ++c)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) to[(16 * c + i) * 65] = o[c][i];
+  }
+  // Element d of column x of the wave's result.
+  __device__ __forceinline__ float get(int w, int x, int d) const {
+    const int i = (d >> 5) * 16 + (d >> 3 & 3) * 4 + (d & 3);
+    return of(w)[i * 65 + (d >> 2 & 1) * 32 + x];
+  }
+};
+
 // One row's parts joined: lane l gets elements l, l + 64, ... of the result.
-// part(i): {base, sum, row of unscaled results}.
-template <class T, class F>
+// base(i), sum(i) and value(i, d) of part i, not divided by its sum.
+template <class T, class M, class L, class V>
 __device__ __forceinline__ void join_parts(const dconv_attend_shape &sh, const AttendPtrs &p, int b, int h, int t,
-                                           bool none, int parts, F part) {
+                                           bool none, int parts, M base_of, L sum_of, V value) {
   const int lane = threadIdx.x & 63;
   float m = -INFINITY, l = 0.0f, acc[kRowParts] = {};
-  for (int i = 0; i < parts; ++i) m = fmaxf(m, part(i).m);
+  for (int i = 0; i < parts; ++i) m = fmaxf(m, base_of(i));
   const float base = m == -INFINITY ? 0.0f : m;
+#pragma unroll 4
   for (int i = 0; i < parts; ++i) {
-    const auto x = part(i);
-    const float w = exp2f(x.m - base);
-    l += w * x.l;
+    const float w = exp2f(base_of(i) - base);
+    l += w * sum_of(i);
 #pragma unroll
     for (int k = 0; k < kRowParts; ++k)
-      if (lane + 64 * k < sh.D) acc[k] = fmaf(w, x.o[lane + 64 * k], acc[k]);
+      if (lane + 64 * k < sh.D) acc[k] = fmaf(w, value(i, lane + 64 * k), acc[k]);
   }
   bool bad = false;
 #pragma unroll
@@ -631,11 +657,6 @@ __device__ __forceinline__ void join_parts(const dconv_attend_shape &sh, const A
     p.lse_out[((int64_t)b * sh.Hq + h) * sh.Tq + t] = none ? -INFINITY : log_sum(m, l);
 }
 
-struct Part {
-  float m, l;
-  const float *o;
-};
-
 // Floats of one part of 32 rows in the workspace: bases, sums, rows.
 template <int DP>
 constexpr int part_floats() { return attend_part_floats(DP); }
@@ -645,7 +666,7 @@ constexpr int part_floats() { return attend_part_floats(DP); }
 template <class T, int DP>
 __global__ __launch_bounds__(64 * split_waves<T>(DP), 1) void attend_split(const dconv_attend_shape sh,
                                                                         const AttendPtrs p, const AttendTile at) {
-  constexpr int KS = DP / 16, DT = DP / 32, kTile = 32 * DP, W = split_waves<T>(DP);
+  constexpr int KS = DP / 16, kTile = 32 * DP, W = split_waves<T>(DP);
   __shared__ __align__(16) T buf0[W * 2 * kTile];
   __shared__ __align__(16) T buf1[W * 2 * kTile];
   DCONV_POISON(poison_lds(buf0, W * 2 * kTile); poison_lds(buf1, W * 2 * kTile));
@@ -687,21 +708,12 @@ __global__ __launch_bounds__(64 * split_waves<T>(DP), 1) void attend_split(const
     step(buf1, v0 + stride);
   }
   const float l = half_sum(soft.l);
-  const int half = lane >> 5;
-  // each wave's sums as rows, in LDS (its own buffers, all read)
-  constexpr int kFloats = part_floats<DP>();
+  // each wave's sums in LDS, in the buffers that all have read
   __shared__ float ml[W][64];
+  const WaveSums<T, DP, W> sums = {buf0, buf1};
   __syncthreads();
-  // row r of wave w: DP floats; the first 16 rows in buf0, the others in buf1
-  auto lds_row = [&](int w, int r) {
-    return reinterpret_cast<float *>(r < 16 ? buf0 : buf1) + (w * 16 + (r & 15)) * DP;
-  };
-  static_assert(16 * DP * sizeof(float) <= 2 * kTile * sizeof(T), "half the rows fit a buffer");
-#pragma unroll
-  for (int c = 0; c < DT; ++c)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) lds_row(wave, lane & 31)[32 * c + acc_row(i, half)] = soft.o[c][i];
-  if (half == 0) {
+  sums.leave(wave, lane, soft.o);
+  if (lane < 32) {
     ml[wave][lane] = soft.m;
     ml[wave][32 + lane] = l;
   }
@@ -710,15 +722,15 @@ __global__ __launch_bounds__(64 * split_waves<T>(DP), 1) void attend_split(const
     const int tx = (r0 + x) / G, hx = hk * G + (r0 + x) % G;
     if (at.splits == 1) {
       const bool none = row_keys(sh, seq, keys, seq.start + tx).none;
-      join_parts<T>(sh, p, b, hx, tx, none, W,
-                    [&](int w) { return Part{ml[w][x], ml[w][32 + x], lds_row(w, x)}; });
+      join_parts<T>(sh, p, b, hx, tx, none, W, [&](int w) { return ml[w][x]; },
+                    [&](int w) { return ml[w][32 + x]; }, [&](int w, int d) { return sums.get(w, x, d); });
       continue;
     }
     // the workgroup's part: the waves joined, not divided yet
     float m = -INFINITY, sum = 0.0f;
     for (int w = 0; w < W; ++w) m = fmaxf(m, ml[w][x]);
     const float base = m == -INFINITY ? 0.0f : m;
-    float *out = at.partial + (int64_t)blockIdx.x * kFloats;
+    float *out = at.partial + (int64_t)blockIdx.x * part_floats<DP>();
     float f[W];
     for (int w = 0; w < W; ++w) {
       f[w] = exp2f(ml[w][x] - base);
@@ -726,7 +738,7 @@ __global__ __launch_bounds__(64 * split_waves<T>(DP), 1) void attend_split(const
     }
     for (int d = lane; d < DP; d += 64) {
       float o = 0.0f;
-      for (int w = 0; w < W; ++w) o = fmaf(f[w], lds_row(w, x)[d], o);
+      for (int w = 0; w < W; ++w) o = fmaf(f[w], sums.get(w, x, d), o);
       out[64 + x * DP + d] = o;
     }
     if (lane == 0) {
@@ -745,10 +757,10 @@ __global__ __launch_bounds__(64) void attend_join(const dconv_attend_shape sh, c
   const Seq seq = seq_of(sh, p, b);
   const Span see = span_of(sh, seq, seq.start + r / G);
   const float *base = at.partial + ((int64_t)bh * at.tiles + r / 32) * at.splits * part_floats<DP>();
-  join_parts<T>(sh, p, b, hk * G + r % G, r / G, see.hi - see.lo + see.first == 0, at.splits, [&](int i) {
-    const float *x = base + (int64_t)i * part_floats<DP>();
-    return Part{x[r & 31], x[32 + (r & 31)], x + 64 + (r & 31) * DP};
-  });
+  auto part = [&](int i) { return base + (int64_t)i * part_floats<DP>() + (r & 31); };
+  join_parts<T>(sh, p, b, hk * G + r % G, r / G, see.hi - see.lo + see.first == 0, at.splits,
+                [&](int i) { return part(i)[0]; }, [&](int i) { return part(i)[32]; },
+                [&](int i, int d) { return part(i)[64 + (r & 31) * (DP - 1) + d]; });
 }
 
 // ---------------------------------------------------------------------------
