@@ -35,9 +35,9 @@
  *     give.  The kernels on bf16 parts take sums that reach infinities, NaN,
  *     inputs of 2^112 and above or sums of 2^96 and above a second time, so
  *     such calls are slower (up to seven times where all of a map's sums do).
- *   - The library allocates no device memory and needs no workspace: every
- *     call reads and writes the caller's three tensors only (and the latency
- *     probe its own two arguments).
+ *   - The library allocates no device memory.  The convolutions need no
+ *     workspace: they read and write the caller's three tensors only (and the
+ *     latency probe its own two arguments).
  *   - Calls on different streams may run concurrently; the library keeps no
  *     state that two calls share except an immutable per-device property
  *     cache (compute-unit counts, read once).

@@ -80,7 +80,13 @@ ForwardPlan plan_forward(const dconv_attend_shape &sh) {
   ForwardPlan f = {};
   f.dp = padded_head(sh.D);
   const int64_t rows = (int64_t)sh.Tq * (sh.Hq / sh.Hkv), heads = (int64_t)sh.B * sh.Hkv;
-  f.few = rows <= 32 || heads * ((rows + 127) / 128) < 128;
+  // Keys divided over waves and workgroups: up to 32 rows, of which 128-row tiles
+  // would be mostly empty (16 sequences x 8 key heads x 32 rows, 4096 keys: 52 us
+  // against 85); and long walks of keys by few workgroups (32 workgroups of 128
+  // rows over 4096 keys: 35 us against 82).  Shorter walks, or more workgroups, lose
+  // more by the second launch than they gain (112 workgroups over 226 keys: 16
+  // against 10.5; 64 over 543 keys: 16.7 against 14).
+  f.few = rows <= 32 || (heads * ((rows + 31) / 32) <= 128 && most_keys(sh, 128) >= 1024);
   f.tiles = (int)(f.few ? (rows + 31) / 32 : (rows + 127) / 128);
   f.splits = 1;
   if (f.few) {
@@ -103,7 +109,9 @@ BackwardPlan plan_backward(const dconv_attend_shape &sh) {
   const int G = sh.Hq / sh.Hkv;
   const int64_t rows = (int64_t)sh.Tq * G, heads = (int64_t)sh.B * sh.Hkv;
   f.row_tiles = (int)((rows + 127) / 128);
-  // 128 keys per workgroup where that gives every compute unit one, else 64
+  // 128 keys per workgroup where that gives every compute unit one (256 workgroups:
+  // 116 us the whole gradient, against 129 with 64 keys each), else 64 (128: 65
+  // against 82; 48: 42 against 56)
   f.key_groups = heads * ((sh.Tk + 127) / 128) >= 256 ? 4 : 2;
   f.key_tiles = (sh.Tk + 32 * f.key_groups - 1) / (32 * f.key_groups);
   // the keys that every row sees, where the others are seen by a window of rows

