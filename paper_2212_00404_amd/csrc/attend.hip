@@ -110,12 +110,19 @@ BackwardPlan plan_backward(const dconv_attend_shape &sh) {
   const int64_t rows = (int64_t)sh.Tq * G, heads = (int64_t)sh.B * sh.Hkv;
   f.row_tiles = (int)((rows + 127) / 128);
   // 128 keys per workgroup where that gives every compute unit one (256 workgroups:
-  // 116 us the whole gradient, against 129 with 64 keys each), else 64 (128: 65
-  // against 82; 48: 42 against 56)
-  f.key_groups = heads * ((sh.Tk + 127) / 128) >= 256 ? 4 : 2;
+  // 116 us the whole gradient, against 129 with 64 keys each); else 64 where that
+  // does; else 32, by four or eight row groups (128 workgroups of 64 keys: 61 us
+  // against 72, 72 of them: 72 against 83).  Larger heads have LDS for two row groups
+  // only and gain nothing by it (58 us against 52).
+  if (heads * ((sh.Tk + 127) / 128) >= 256)
+    f.key_groups = 4;
+  else
+    f.key_groups = heads * ((sh.Tk + 63) / 64) >= 256 || f.dp * element_size(sh.dtype) > 256 ? 2 : 1;
   f.key_tiles = (sh.Tk + 32 * f.key_groups - 1) / (32 * f.key_groups);
-  // the keys that every row sees, where the others are seen by a window of rows
-  f.first = sh.left < 0 ? 0 : sh.sinks < sh.Tk ? sh.sinks : sh.Tk;
+  // the keys that every query sees, where that is more than twice what another tile
+  // of keys is seen by
+  const int64_t window = sh.left < 0 || sh.right < 0 ? sh.Tq : (int64_t)sh.left + sh.right + 32 * f.key_groups;
+  f.first = sh.Tq <= 2 * window ? 0 : sh.sinks < sh.Tk ? sh.sinks : sh.Tk;
   f.first_tiles = (f.first + 31) / 32;
   f.parts = 1;
   if (f.first > 0) {

@@ -401,14 +401,18 @@ struct RowTiles {
 // workgroups, bf16: 92 us with four waves, 75 with eight, 71 with operands read
 // ahead, 67 with two tiles per step: the matrix cores run 0.26 of the cycles, the
 // waves wait 0.43 of theirs, mostly for LDS and for copies.)  KG = 4 reads the rows
-// least often; KG = 2 makes twice the workgroups.
+// least often; KG = 2 and 1 make twice and four times the workgroups.
 template <class T>
-constexpr int grad_waves(int dp) { return dp * (int)sizeof(T) <= 128 ? 8 : 4; }
+constexpr int row_groups(int dp, int key_groups) {
+  const int bytes = dp * (int)sizeof(T);
+  if (key_groups == 1) return bytes <= 128 ? 8 : bytes <= 256 ? 4 : 2;   // (what two LDS buffers hold)
+  return (bytes <= 128 ? 8 : 4) / key_groups;
+}
 
-template <class T, int DP, int KG>
-__global__ __launch_bounds__(64 * grad_waves<T>(DP)) void attend_dkv(const dconv_attend_shape sh, const AttendPtrs p,
-                                                                     const GradTile gt) {
-  constexpr int W = grad_waves<T>(DP), RG = W / KG, DT = DP / 32;
+template <class T, int DP, int KG, int RG>
+__global__ __launch_bounds__(64 * KG * RG) void attend_dkv(const dconv_attend_shape sh, const AttendPtrs p,
+                                                           const GradTile gt) {
+  constexpr int W = KG * RG, DT = DP / 32;
   constexpr int R = 32 * RG * DP * (int)sizeof(T) <= 8192 ? 2 : 1, BM = 32 * RG * R;
   constexpr int kMerge = KG * (RG - 1) * 1024 * 4 / (int)sizeof(T);   // sums of one 32-column part
   constexpr int kBuf = 2 * BM * DP > kMerge ? 2 * BM * DP : kMerge;
@@ -650,11 +654,14 @@ void launch_attend_grad(const dconv_attend_shape &sh, const AttendPtrs &p, const
     }
     if (plan.first < sh.Tk) {
       gt.a.tiles = plan.key_tiles;
-      const dim3 grid(heads * plan.key_tiles), block(64 * grad_waves<T>(DP));
-      if (plan.key_groups == 4)
-        hipLaunchKernelGGL((attend_dkv<T, DP, 4>), grid, block, 0, s, sh, p, gt);
-      else
-        hipLaunchKernelGGL((attend_dkv<T, DP, 2>), grid, block, 0, s, sh, p, gt);
+      auto dkv = [&](auto groups) {
+        constexpr int KG = decltype(groups)::value, RG = row_groups<T>(DP, KG);
+        hipLaunchKernelGGL((attend_dkv<T, DP, KG, RG>), dim3(heads * plan.key_tiles), dim3(64 * KG * RG), 0, s, sh, p,
+                           gt);
+      };
+      if (plan.key_groups == 4) dkv(std::integral_constant<int, 4>());
+      if (plan.key_groups == 2) dkv(std::integral_constant<int, 2>());
+      if (plan.key_groups == 1) dkv(std::integral_constant<int, 1>());
     }
     if (plan.first > 0) {
       gt.a.tiles = plan.first_tiles;
