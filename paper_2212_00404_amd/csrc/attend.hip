@@ -57,10 +57,10 @@ bool whole_pieces(const void *p, const long long *stride, const dconv_attend_sha
          stride[2] % unit == 0;
 }
 
-// Whether 64 consecutive rows, of a head or of a group of heads, span less than
-// 2^31 bytes.
+// Whether as many rows as a tile has at most (256, of queries) span less than 2^31
+// bytes, as rows of one head and as the heads of a group.
 bool close_rows(const long long *stride, const dconv_attend_shape &sh) {
-  const long long most = (1ll << 31) / element_size(sh.dtype) / 64 / (sh.Hq / sh.Hkv) - sh.D;
+  const long long most = (1ll << 31) / element_size(sh.dtype) / 512 / (sh.Hq / sh.Hkv) - sh.D;
   return stride[1] >= 0 && stride[2] >= 0 && stride[1] < most && stride[2] < most;
 }
 
@@ -100,6 +100,14 @@ ForwardPlan plan_forward(const dconv_attend_shape &sh) {
   return f;
 }
 
+// A launch has less than 2^32 threads.
+bool launchable(int64_t workgroups, int threads) { return workgroups < (1ll << 32) / threads; }
+
+int forward_range(const dconv_attend_shape &sh) {
+  const int64_t rows = (int64_t)sh.Tq * (sh.Hq / sh.Hkv), heads = (int64_t)sh.B * sh.Hkv;
+  return launchable(heads * ((rows + 31) / 32), 256) ? DCONV_OK : DCONV_ERANGE;
+}
+
 int64_t forward_workspace(const dconv_attend_shape &sh) {
   return sh.B == 0 || sh.Tq == 0 ? 0 : plan_forward(sh).workspace;
 }
@@ -136,6 +144,17 @@ BackwardPlan plan_backward(const dconv_attend_shape &sh) {
   return f;
 }
 
+int backward_range(const dconv_attend_shape &sh) {
+  const int64_t heads = (int64_t)sh.B * sh.Hkv;
+  if (sh.D > kGradMaxD)   // attend_rows: a wave per row
+    return launchable((int64_t)sh.B * sh.Hq * sh.Tq, 64) && launchable(heads * sh.Tk, 64) ? DCONV_OK : DCONV_ERANGE;
+  const BackwardPlan f = plan_backward(sh);
+  return launchable(heads * f.row_tiles, 256) && launchable(heads * f.key_tiles, 512) &&
+                 launchable(heads * f.first, 256) && launchable(heads * f.first_tiles * f.parts, 256)
+             ? DCONV_OK
+             : DCONV_ERANGE;
+}
+
 int64_t backward_workspace(const dconv_attend_shape &sh) {
   return sh.B == 0 || sh.D > kGradMaxD ? 0 : plan_backward(sh).workspace;
 }
@@ -145,14 +164,16 @@ int64_t backward_workspace(const dconv_attend_shape &sh) {
 
 DCONV_EXPORT int dconv_attend_workspace(const dconv_attend_shape *shape, long long *bytes) {
   if (!shape || !bytes) return DCONV_ENULL;
-  const int rc = dconv::validate(*shape);
+  int rc = dconv::validate(*shape);
+  if (rc == DCONV_OK) rc = dconv::forward_range(*shape);
   if (rc == DCONV_OK) *bytes = dconv::forward_workspace(*shape);
   return rc;
 }
 
 DCONV_EXPORT int dconv_attend_backward_workspace(const dconv_attend_shape *shape, long long *bytes) {
   if (!shape || !bytes) return DCONV_ENULL;
-  const int rc = dconv::validate(*shape);
+  int rc = dconv::validate(*shape);
+  if (rc == DCONV_OK) rc = dconv::backward_range(*shape);
   if (rc == DCONV_OK) *bytes = dconv::backward_workspace(*shape);
   return rc;
 }
@@ -162,13 +183,15 @@ DCONV_EXPORT int dconv_attend(const dconv_attend_shape *shape, const void *q, co
                               float *lse, void *workspace, long long workspace_bytes, void *stream) {
   using namespace dconv;
   if (!shape) return DCONV_ENULL;
-  const int rc = validate(*shape);
+  int rc = validate(*shape);
+  if (rc == DCONV_OK) rc = forward_range(*shape);
   if (rc != DCONV_OK) return rc;
   if (shape->B == 0 || shape->Tq == 0) return DCONV_OK;
   if (!q || !out || (shape->Tk > 0 && (!k || !v))) return DCONV_ENULL;
   const int64_t need = forward_workspace(*shape);
   if (need > 0 && !workspace) return DCONV_ENULL;
   if (workspace_bytes < need) return DCONV_EWORKSPACE;
+  if (need > 0 && (uintptr_t)workspace % 16 != 0) return DCONV_EINVAL;
   AttendPtrs p = {};
   p.q = q;
   p.k = k;
@@ -195,7 +218,8 @@ DCONV_EXPORT int dconv_attend_backward(const dconv_attend_shape *shape, const vo
                                        long long workspace_bytes, void *stream) {
   using namespace dconv;
   if (!shape) return DCONV_ENULL;
-  const int rc = validate(*shape);
+  int rc = validate(*shape);
+  if (rc == DCONV_OK) rc = backward_range(*shape);
   if (rc != DCONV_OK) return rc;
   if (shape->B == 0) return DCONV_OK;
   if (shape->Tq > 0 && (!dout || !q || !out || !lse || !dq)) return DCONV_ENULL;
@@ -203,6 +227,7 @@ DCONV_EXPORT int dconv_attend_backward(const dconv_attend_shape *shape, const vo
   const int64_t need = backward_workspace(*shape);
   if (need > 0 && !workspace) return DCONV_ENULL;
   if (workspace_bytes < need) return DCONV_EWORKSPACE;
+  if (need > 0 && (uintptr_t)workspace % 16 != 0) return DCONV_EINVAL;
   AttendPtrs p = {};
   p.q = q;
   p.k = k;

@@ -44,6 +44,8 @@ int validate(const dconv_join_shape &sh) {
       (sh.per_sample & ~15) || !(sh.eps >= 0.0f))
     return DCONV_EINVAL;
   if (sh.D > kMaxD || (int64_t)sh.B * sh.T > INT_MAX) return DCONV_ERANGE;
+  // a launch has less than 2^32 threads, a run per sequence at least, of up to 1024
+  if (sh.per_sample && sh.B >= 1 << 22) return DCONV_ERANGE;
   return DCONV_OK;
 }
 
@@ -162,6 +164,7 @@ DCONV_EXPORT int dconv_join_backward(const dconv_join_shape *shape, const void *
   const int64_t need = workspace_bytes_of(*shape);
   if (!none && (!x || !stats || !dx || (need > 0 && !workspace))) return DCONV_ENULL;
   if (workspace_bytes < need) return DCONV_EWORKSPACE;
+  if (need > 0 && (uintptr_t)workspace % 16 != 0) return DCONV_EINVAL;
   JoinPtrs p = {};
   p.branch = branch;
   p.x = x;

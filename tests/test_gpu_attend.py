@@ -228,6 +228,19 @@ def test_offsets_past_32_bits():
     assert (out[:2] == 0).all()
 
 
+@pytest.mark.parametrize("what", ["queries", "keys"])
+def test_rows_far_apart(what):
+    """Tokens 16 MB apart: a tile of rows spans more than 2^32 bytes."""
+    dt, T, D = torch.bfloat16, 300, 64
+    q, k, v, dout = make(16, dt, 1, T, T, 1, 1, D)
+    far = torch.empty((1, T, 1, 1 << 23), dtype=dt, device=DEV)[..., :D]
+    far.copy_(q if what == "queries" else k)
+    args = (far, k, v, dout) if what == "queries" else (q, far, v, dout)
+    want, got = run_both(q, k, v, dout, left=200), run_both(*args, left=200)
+    for a, b in zip(want, got):
+        assert torch.equal(a, b)
+
+
 def test_equal_calls_give_equal_bits():
     q, k, v, dout = make(10, torch.bfloat16, 2, 333, 333, 8, 2, 64)
     how = dict(left=90, sinks=5)

@@ -102,6 +102,22 @@ def test_sizes_that_are_not_supported():
     assert rotate(rotate_shape(T=(1 << 31) - 1, H=64)) == dconv.ERANGE
 
 
+def test_launches_that_do_not_fit_are_refused():
+    """A launch has less than 2^32 threads."""
+    assert attend(attend_shape(B=1 << 24, Tq=1, Tk=1, Hq=1, Hkv=1)) == dconv.ERANGE
+    assert attend_backward(attend_shape(B=1 << 24, Tq=1, Tk=1, Hq=1, Hkv=1)) == dconv.ERANGE
+    assert attend_backward(attend_shape(B=1, Tq=1, Tk=1 << 28, Hq=1, Hkv=1, D=200)) == dconv.ERANGE
+    assert join(join_shape(B=1 << 22, T=1, per=1)) == dconv.ERANGE
+    n = ctypes.c_longlong()
+    assert dc.load().dconv_attend_workspace(attend_shape(B=1 << 24, Hq=1, Hkv=1), ctypes.byref(n)) == dconv.ERANGE
+
+
+def test_workspaces_off_their_boundary():
+    assert attend(attend_shape(B=1, Tq=1, Tk=100000, left=-1), ws=P + 8) == dconv.EINVAL
+    assert attend_backward(attend_shape(), ws=P + 4) == dconv.EINVAL
+    assert join_backward(join_shape(B=4, T=1000), ws=P + 8) == dconv.EINVAL
+
+
 def test_branch_and_gradients_that_do_not_go_together():
     assert join_backward(join_shape(), branch=None) == dconv.ENULL
     assert join_backward(join_shape(), branch=None, dbranch=None) == dconv.EINVAL
