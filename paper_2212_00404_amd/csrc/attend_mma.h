@@ -81,7 +81,16 @@ struct Tile {
 
   // Elements 16 s + 8 (l / 32) .. + 7 of row r0 + l % 32.
   static __device__ __forceinline__ Frag row(const T *t, int r0, int s, int lane) {
-    return *reinterpret_cast<const Frag *>(t + at(r0 + (lane & 31), 2 * s + (lane >> 5)));
+    const T *p = t + at(r0 + (lane & 31), 2 * s + (lane >> 5));
+    if constexpr (sizeof(T) == 4) {
+      // (two loads of 16 bytes: one of 32, split by the compiler, loses which
+      // buffer it reads and waits for the copies into the other one)
+      typedef float f32x4 __attribute__((ext_vector_type(4)));
+      const f32x4 a = *reinterpret_cast<const f32x4 *>(p), b = *reinterpret_cast<const f32x4 *>(p + 4);
+      return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+    } else {
+      return *reinterpret_cast<const Frag *>(p);
+    }
   }
   // Column 32 c + l % 32 of the rows r0 + 8 (e / 4) + 4 (l / 32) + e % 4
   // (r0 a multiple of 16).
@@ -439,7 +448,27 @@ struct Softmax {
   // matrix and the vector unit work at the same time within a wave.
   __device__ __forceinline__ void add_two(const T *ks, const T *vs, const Frag (&q)[KS], int v0, const RowKeys &see,
                                           int sinks, float scale2, bool masked, int lane) {
-    Frag kf[KS], vf[2][DT], w0[2], w1[2];
+    Frag w0[2], w1[2];
+    if constexpr (DP > 96) {
+      // (operands read ahead would not leave registers for two waves per SIMD, and
+      // a register that comes back from memory waits for the copies too)
+      f32x16 s0 = scores(ks, 0, q, lane);
+      if (masked) mask(s0, v0, see, sinks, lane);
+      follow(s0, scale2, [] {});
+      f32x16 s1 = scores(ks, 32, q, lane);
+      probabilities(s0, scale2, w0);
+      asm volatile("" ::"v"(w0[0]), "v"(w0[1]));   // here, not after the next branch
+      if (masked) mask(s1, v0 + 32, see, sinks, lane);
+      follow(s1, scale2, [&] {
+        values(vs, 0, w0, lane);
+        w0[0] = w0[1] = Frag{};
+      });
+      values(vs, 0, w0, lane);
+      probabilities(s1, scale2, w1);
+      values(vs, 32, w1, lane);
+      return;
+    }
+    Frag kf[KS], vf[2][DT];
     load_keys(kf, ks, 0, lane);
     in_order();
     f32x16 s0 = products(kf, q), s1;
@@ -451,7 +480,7 @@ struct Softmax {
     load_values(vf[0], vs, 0, lane);
     in_order();
     probabilities(s0, scale2, w0);
-    asm volatile("" ::"v"(w0[0]), "v"(w0[1]));   // here, not after the next branch
+    asm volatile("" ::"v"(w0[0]), "v"(w0[1]));
     if (masked) mask(s1, v0 + 32, see, sinks, lane);
     follow(s1, scale2, [&] {
       values(vs, 0, w0, lane);
