@@ -405,7 +405,7 @@ struct RowTiles {
 template <class T>
 constexpr int row_groups(int dp, int key_groups) {
   const int bytes = dp * (int)sizeof(T);
-  if (key_groups == 1) return bytes <= 128 ? 8 : bytes <= 256 ? 4 : 2;   // (what two LDS buffers hold)
+  if (key_groups == 1) return bytes <= 128 ? 8 : 4;   // (what two LDS buffers hold)
   return (bytes <= 128 ? 8 : 4) / key_groups;
 }
 
@@ -661,7 +661,8 @@ void launch_attend_grad(const dconv_attend_shape &sh, const AttendPtrs &p, const
       };
       if (plan.key_groups == 4) dkv(std::integral_constant<int, 4>());
       if (plan.key_groups == 2) dkv(std::integral_constant<int, 2>());
-      if (plan.key_groups == 1) dkv(std::integral_constant<int, 1>());
+      if constexpr (DP * sizeof(T) <= 256)
+        if (plan.key_groups == 1) dkv(std::integral_constant<int, 1>());
     }
     if (plan.first > 0) {
       gt.a.tiles = plan.first_tiles;
