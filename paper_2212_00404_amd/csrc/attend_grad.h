@@ -54,7 +54,7 @@ __device__ __forceinline__ void store4(T *row, int d, int D, bool whole, float a
 
 // ---------------------------------------------------------------------------
 // dq: 61 us for 2 x 4096 queries, 16 heads of 64, window 512, bf16; the matrix cores
-// run 0.29 of the cycles and vector instructions issue in 0.48 of them
+// run 0.29 of the cycles and vector instructions issue in 0.47 of them
 // ---------------------------------------------------------------------------
 template <class T, int DP>
 __global__ __launch_bounds__(256, DP * sizeof(T) <= 128 ? 2 : 1) void attend_dq(const dconv_attend_shape sh, const AttendPtrs p, const GradTile gt) {

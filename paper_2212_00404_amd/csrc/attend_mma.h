@@ -510,8 +510,8 @@ constexpr int kForwardRows = 128;
 // 128 rows per workgroup, 32 per wave; tiles of BN keys and values in two LDS
 // buffers, the next one copied while the current one is used.  Registers for two
 // workgroups per compute unit (a prompt of 8192 tokens, 32 heads of 128 over 8, window
-// 1024, bf16: 295 us with one, 183 with two, 129 GFLOP of seen scores).  There the
-// matrix cores run 0.39 of the cycles and vector instructions issue in 0.50 of them;
+// 1024, bf16: 295 us with one, 178 with two, 129 GFLOP of seen scores).  There the
+// matrix cores run 0.40 of the cycles and vector instructions issue in 0.50 of them;
 // leaving out the copies changes nothing, LDS is busy 0.2: what bounds it is vector
 // issue beside the products, some 110 instructions and 32 exponentials per 64 keys.
 template <class T, int DP>
