@@ -12,7 +12,7 @@
 
 namespace dconv {
 
-// A row's sum (in powers of two) and its delta, as the workspace holds them.
+// A row's sum (in powers of two, less kLift) and its delta, as the workspace holds them.
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
@@ -38,6 +38,57 @@ __device__ __forceinline__ float frag_dot(typename Mma<T>::Frag a, typename Mma<
   for (int e = 0; e < 8; ++e) s = fmaf(to_f32(a[e]), to_f32(b[e]), s);
   return s;
 }
+
+// Probabilities and their gradients are operands of the tensors' type.  fp16 has five
+// bits of exponent only: a probability is below its normal values from 2^-14 on, a
+// gradient, which is as small as dout over the number of keys, for ordinary losses,
+// and past its largest value for scaled ones.  So fp16 holds 2^15 times the
+// probabilities (they are 1 at most) and a power of two times their gradients, one
+// for each column of a tile of scores, that is for each row of dq and each key of dk:
+// it begins high enough for any fp16 inputs and falls when a value of the column
+// reaches 2, to bring the largest to 1/4 .. 1/2; the sums so far are scaled with it.
+// What is rounded below the normal values is then off by less than 2^-23 of the
+// column's largest, and the scales lose nothing, as they are powers of two.  Below 2
+// the first bit of the exponent is 0, so that one bit of each operand tells.  (It costs
+// fp16 5 to 15%, in the branch's moves of sums between register files: 2 x 4096
+// queries, 16 heads of 64 over 4, window 512: 130 -> 146 us.)
+template <class T>
+constexpr bool kScaled = std::is_same<T, f16_t>::value;
+template <class T>
+constexpr float kLift = kScaled<T> ? 15.0f : 0.0f;   // log2 of the probabilities' scale
+constexpr float kUnlift = 0x1p-15f;
+
+struct ColumnScale {
+  float up = 0x1p60f;
+  // x, scaled by up, as operands, after it has been brought into range.  sums(f):
+  // what has been summed up so far, times f.
+  template <class T, class F>
+  __device__ __forceinline__ void fit(f32x16 &x, typename Mma<T>::Frag (&u)[2], F sums) {
+    u[0] = as_operand<T>(x, 0);
+    u[1] = as_operand<T>(x, 1);
+    uint32_t bits[8], any = 0;
+    __builtin_memcpy(bits, u, sizeof(bits));
+#pragma unroll
+    for (int i = 0; i < 8; ++i) any |= bits[i];
+    if (__any((any & 0x40004000u) != 0)) {
+      no_speculation();
+      float top = 0.0f;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) top = fmaxf(top, fabsf(x[i]));
+      top = half_max(top);
+      // 2^(-2 - e) for a top of 2^e .. 2^(e + 1), past fp16's largest too; an infinity
+      // stays one
+      const float f = top >= 1.0f ? __uint_as_float((252u - min(__float_as_uint(top) >> 23, 250u)) << 23) : 1.0f;
+      x *= f;
+      up *= f;
+      sums(f);
+      u[0] = as_operand<T>(x, 0);
+      u[1] = as_operand<T>(x, 1);
+    }
+  }
+  // What takes the scales out of the sums of the gradients.
+  __device__ __forceinline__ float down() const { return kUnlift / up; }
+};
 
 // Stores four consecutive elements from column d on.
 template <class T>
@@ -100,7 +151,9 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= 128 ? 2 : 1) void attend_dq(
     delta += frag_dot<T>(g[k], load_frag(orow, d, sh.D, at.direct, 1.0f));
   }
   delta = half_sum(delta);
-  const float lse2 = see.none ? 0.0f : 1.4426950408889634f * p.lse[((int64_t)b * sh.Hq + h) * sh.Tq + t];
+  const float lse2 =
+      (see.none ? 0.0f : 1.4426950408889634f * p.lse[((int64_t)b * sh.Hq + h) * sh.Tq + t]) - kLift<T>;
+  ColumnScale scale;
 
   // out, rounded to the tensors' type, gives delta to within that rounding of
   // |dout| |out|.  Where a row's weight is on a few keys, dp - delta cancels and
@@ -142,7 +195,7 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= 128 ? 2 : 1) void attend_dq(
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         s[i] = power2<T>(fmaf(s[i], at.scale2, -lse2));
-        dp[i] = s[i] * (dp[i] - delta);
+        dp[i] = s[i] * (kScaled<T> ? fmaf(dp[i], scale.up, -delta * scale.up) : dp[i] - delta);
       }
       if (masked) {
         no_speculation();
@@ -151,16 +204,30 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= 128 ? 2 : 1) void attend_dq(
           dp[i] = on ? dp[i] : 0.0f;
         });
       }
+      // (before the branch in fit(), which nothing is moved across)
+      if constexpr (kScaled<T> && !kAhead<T, DP>) columns(col[0], ks, 32 * hb);
+      const Frag w[2] = {as_operand<T>(s, 0), as_operand<T>(s, 1)};
+      Frag u[2];
+      if constexpr (kScaled<T>) {
+        scale.fit<T>(dp, u, [&](float f) {
+#pragma unroll
+          for (int c = 0; c < DT; ++c) acc[c] *= f;
+          miss *= f;
+        });
+      } else {
+        u[0] = as_operand<T>(dp, 0);
+        u[1] = as_operand<T>(dp, 1);
+      }
 #pragma unroll
       for (int i = 0; i < 16; ++i) miss += dp[i];
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
-        const Frag w = as_operand<T>(s, k), u = as_operand<T>(dp, k);
-        if constexpr (!kAhead<T, DP>) columns(col[k], ks, 32 * hb + 16 * k);
+        if constexpr (!kAhead<T, DP>)
+          if (!kScaled<T> || k > 0) columns(col[k], ks, 32 * hb + 16 * k);
 #pragma unroll
         for (int c = 0; c < DT; ++c) {
-          acc[c] = Mma<T>::mac(col[k][c], u, acc[c]);
-          mean[c] = Mma<T>::mac(col[k][c], w, mean[c]);
+          acc[c] = Mma<T>::mac(col[k][c], u[k], acc[c]);
+          mean[c] = Mma<T>::mac(col[k][c], w[k], mean[c]);
         }
       }
     }
@@ -180,6 +247,14 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= 128 ? 2 : 1) void attend_dq(
   }
 
   miss = half_sum(miss);
+  if constexpr (kScaled<T>) {
+    miss *= scale.down();
+#pragma unroll
+    for (int c = 0; c < DT; ++c) {
+      acc[c] *= scale.down();
+      mean[c] *= kUnlift;
+    }
+  }
   if (half == 0 && r < rows) gt.stats[(int64_t)bh * rows + r] = f32x2{lse2, delta + miss};
   bool bad = false;
 #pragma unroll
@@ -216,6 +291,7 @@ struct KeyGrad {
   typedef typename Mma<T>::Frag Frag;
   Frag k[KS], v[KS];
   f32x16 dk[DT], dv[DT];   // dk[c][i]: element 32 c + acc_row(i, half) of the key
+  ColumnScale scale;
 
   __device__ __forceinline__ void load(const dconv_attend_shape &sh, const AttendTile &at, const T *krow,
                                        const T *vrow, int half) {
@@ -260,7 +336,7 @@ struct KeyGrad {
     for (int i = 0; i < 16; ++i) {
       const f32x4 x = st4[i / 4 * 2 + i % 4 / 2];
       s[i] = power2<T>(fmaf(s[i], scale2, -x[i % 2 * 2]));
-      dp[i] = s[i] * (dp[i] - x[i % 2 * 2 + 1]);
+      dp[i] = (kScaled<T> ? s[i] * scale.up : s[i]) * (dp[i] - x[i % 2 * 2 + 1]);
     }
     if (masked) {
       no_speculation();
@@ -269,16 +345,38 @@ struct KeyGrad {
         dp[i] = on ? dp[i] : 0.0f;
       });
     }
+    if constexpr (kScaled<T> && !kAhead<T, DP>) columns(cg[0], cq[0], gs, qs, 0, lane);
+    const Frag w[2] = {as_operand<T>(s, 0), as_operand<T>(s, 1)};
+    Frag u[2];
+    if constexpr (kScaled<T>) {
+      scale.fit<T>(dp, u, [&](float f) {
+#pragma unroll
+        for (int c = 0; c < DT; ++c) dk[c] *= f;
+      });
+    } else {
+      u[0] = as_operand<T>(dp, 0);
+      u[1] = as_operand<T>(dp, 1);
+    }
     if constexpr (kAhead<T, DP>) columns(cg[1], cq[1], gs, qs, 16, lane);
     read_ahead<T, DP>();
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
-      const Frag w = as_operand<T>(s, x), u = as_operand<T>(dp, x);
-      if constexpr (!kAhead<T, DP>) columns(cg[x], cq[x], gs, qs, 16 * x, lane);
+      if constexpr (!kAhead<T, DP>)
+        if (!kScaled<T> || x > 0) columns(cg[x], cq[x], gs, qs, 16 * x, lane);
 #pragma unroll
       for (int c = 0; c < DT; ++c) {
-        dv[c] = Mma<T>::mac(cg[x][c], w, dv[c]);
-        dk[c] = Mma<T>::mac(cq[x][c], u, dk[c]);
+        dv[c] = Mma<T>::mac(cg[x][c], w[x], dv[c]);
+        dk[c] = Mma<T>::mac(cq[x][c], u[x], dk[c]);
+      }
+    }
+  }
+  // After the last rows: the sums without their scales.
+  __device__ __forceinline__ void finish() {
+    if constexpr (kScaled<T>) {
+#pragma unroll
+      for (int c = 0; c < DT; ++c) {
+        dk[c] *= scale.down();
+        dv[c] *= kUnlift;
       }
     }
   }
@@ -471,6 +569,7 @@ __global__ __launch_bounds__(64 * KG * RG) void attend_dkv(const dconv_attend_sh
     if (r + 2 * BM < to) stage(buf0, stats0, r + 2 * BM);
     step(buf1, stats1, r + BM);
   }
+  acc.finish();
   if constexpr (RG > 1) {
 #pragma unroll
     for (int c = 0; c < DT; ++c) {
@@ -575,6 +674,7 @@ __global__ __launch_bounds__(64 * split_waves<T>(DP)) void attend_dkv_split(cons
       step(buf1, stats1, r + stride);
     }
   }
+  acc.finish();
   // the waves' sums in LDS: first dk, then dv
   const WaveSums<T, DP, W> sums = {buf0, buf1};
   for (int which = 0; which < 2; ++which) {
