@@ -72,23 +72,26 @@ __device__ __forceinline__ float row_dot(const T *a, const T *b, int D) {
 }
 
 // acc += w * row, each lane its elements lane, lane + 64, ...
-template <class T>
-__device__ __forceinline__ void row_add(float *acc, float w, const T *row, int D, int lane) {
+template <class A, class T>
+__device__ __forceinline__ void row_add(A *acc, float w, const T *row, int D, int lane) {
 #pragma unroll
   for (int i = 0; i < kRowParts; ++i)
-    if (lane + 64 * i < D) acc[i] = fmaf(w, to_f32(row[lane + 64 * i]), acc[i]);
+    if (lane + 64 * i < D) acc[i] = fma((A)w, (A)to_f32(row[lane + 64 * i]), acc[i]);
 }
 
 // One query of one head by one wave: 64 keys at a time, a key per lane for the
 // products and a part of the head per lane for the sum.  Only visible keys and
-// values are read.
+// values are read.  The sums are in 64 bits: rows come here whose sum of values,
+// before it is divided by that of the weights, is past fp32's largest, and their
+// mean is not.
 template <class T>
 __device__ void attend_row(const dconv_attend_shape &sh, const AttendPtrs &p, int b, int h, int t) {
   const int lane = threadIdx.x & 63, D = sh.D, hk = h / (sh.Hq / sh.Hkv);
   const Seq s = seq_of(sh, p, b);
   const Span see = span_of(sh, s, s.start + t);
   const T *q = row_of<T>(p.q, sh.q_stride, b, t, h);
-  float m = -INFINITY, l = 0.0f, acc[kRowParts] = {};
+  float m = -INFINITY;
+  double l = 0.0, acc[kRowParts] = {};
   for (int part = 0; part < 2; ++part) {
     const int end = part ? see.hi : see.first;
     for (int j0 = part ? see.lo : 0; j0 < end; j0 += 64) {
@@ -112,9 +115,9 @@ __device__ void attend_row(const dconv_attend_shape &sh, const AttendPtrs &p, in
   T *o = (T *)p.o + b * sh.out_stride[0] + t * sh.out_stride[1] + h * sh.out_stride[2];
 #pragma unroll
   for (int i = 0; i < kRowParts; ++i)
-    if (lane + 64 * i < D) o[lane + 64 * i] = from_f32<T>(none ? 0.0f : acc[i] / l);
+    if (lane + 64 * i < D) o[lane + 64 * i] = from_f32<T>(none ? 0.0f : (float)(acc[i] / l));
   if (p.lse_out && lane == 0)
-    p.lse_out[((int64_t)b * sh.Hq + h) * sh.Tq + t] = none ? -INFINITY : m + logf(l);
+    p.lse_out[((int64_t)b * sh.Hq + h) * sh.Tq + t] = none ? -INFINITY : m + logf((float)l);
 }
 
 // dq of one query of one head by one wave.

@@ -2,6 +2,8 @@
 import pytest
 import torch
 
+import paper_2212_00404_amd as dc
+import token_ref as ref
 from test_gpu_attend import TYPE_IDS, TYPES, compare, make
 
 pytestmark = pytest.mark.gpu
@@ -53,3 +55,29 @@ def test_gradients_of_mixed_size(case, order, dt):
             e = e.flip(0)
         return (t.float() * torch.exp2(e)[None, :, None, None]).to(dt)
     compare(q * 16, k / 16, along(v, -8, 4), along(dout, -16, 4), **how)
+
+
+@pytest.mark.parametrize("dt", TYPES, ids=TYPE_IDS)
+@pytest.mark.parametrize("case", [(1, 200, 200, 2, 1, 64, dict(left=20)), (1, 1, 300, 4, 1, 64, dict()),
+                                  (2, 3, 2000, 2, 2, 40, dict()), (1, 1, 5, 1, 1, 128, dict()),
+                                  (1, 70, 70, 2, 2, 200, dict())], ids=str)
+def test_values_at_the_end_of_the_range(case, dt):
+    """Equal scores over values of the type's largest and lowest: their mean, though
+    their sum is past the range; one sign in the first half of a head, both in turn
+    in the second.  Within a row the weights are one number, so that the mean is as
+    good as fp32 (the definition's value rounded once, and one unit of fp32 for the
+    weight)."""
+    B, Tq, Tk, Hq, Hkv, D, how = case
+    big = torch.finfo(dt).max
+    q = torch.zeros((B, Tq, Hq, D), dtype=dt, device=DEV)
+    k = torch.ones((B, Tk, Hkv, D), dtype=dt, device=DEV)
+    v = torch.full((B, Tk, Hkv, D), big, dtype=dt, device=DEV)
+    v[..., ::2] = -big
+    v[:, ::2, :, D // 2:] *= -1
+    out, lse = dc.attend(q, k, v, return_lse=True, **how)
+    r = ref.Attend(q, k, v, **how)
+    tol = ref.UNIT[dt] * r.out.abs() + 2 * ref.UNIT[torch.float32] * big
+    ref.check(out, r.out, tol, "out")
+    ref.check(lse, r.lse, r.lse_tol, "lse")
+    one = dc.attend(q, k, torch.full_like(v, big), **how)
+    assert (one == big).all()
