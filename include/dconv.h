@@ -451,8 +451,9 @@ int dconv_join_backward(const dconv_join_shape *shape, const void *dh, const voi
  *   starts : int32 [B] or NULL: lengths[b] - Tq (the queries are the last ones)
  *   workspace : dconv_attend_workspace bytes (0 for many calls: then NULL will
  *     do), 16-byte aligned
- * 1 <= D <= 256; B * Hq * (Tq, Tk) below 2^31 and what a launch can hold (2^24
- * tiles of 32 queries of a key head's heads), else DCONV_ERANGE.  B = 0, Tq = 0 is
+ * 1 <= D <= 256; B * Hq * (Tq, Tk) below 2^31, Tk and Tq * Hq / Hkv below 2^31 -
+ * 2^16, and what a launch can hold (2^24 tiles of 32 queries of a key head's heads),
+ * else DCONV_ERANGE.  B = 0, Tq = 0 is
  * a call without work; Tk = 0 writes zeros.
  */
 typedef struct dconv_attend_shape {

@@ -43,8 +43,11 @@ int validate(const dconv_attend_shape &sh) {
       !std::isfinite(sh.scale))
     return DCONV_EINVAL;
   if (sh.D > kAttendMaxD) return DCONV_EUNSUPPORTED;
-  // rows of queries and of keys are counted in 32 bits
-  if ((int64_t)sh.B * sh.Hq > INT_MAX / ((int64_t)(sh.Tq > sh.Tk ? sh.Tq : sh.Tk) + 1))
+  // rows of queries and of keys are counted in 32 bits, and walked by steps that end
+  // past the last one: two strides of at most 32 (a tile) x 4 (waves) x 256 (parts)
+  constexpr int kMost = INT_MAX - 2 * 32 * 4 * 256;
+  if ((int64_t)sh.B * sh.Hq > INT_MAX / ((int64_t)(sh.Tq > sh.Tk ? sh.Tq : sh.Tk) + 1) || sh.Tk > kMost ||
+      (int64_t)sh.Tq * (sh.Hq / sh.Hkv) > kMost)
     return DCONV_ERANGE;
   return DCONV_OK;
 }

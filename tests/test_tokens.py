@@ -112,6 +112,26 @@ def test_launches_that_do_not_fit_are_refused():
     assert dc.load().dconv_attend_workspace(attend_shape(B=1 << 24, Hq=1, Hkv=1), ctypes.byref(n)) == dconv.ERANGE
 
 
+@pytest.mark.parametrize("sizes", [dict(Tq=1, Tk=(1 << 31) - 2), dict(Tq=1, Tk=(1 << 31) - (1 << 16)),
+                                   dict(Tq=(1 << 31) - (1 << 16), Tk=1), dict(Tq=(1 << 28) - 100, Tk=1, Hq=8)],
+                         ids=str)
+def test_walks_past_32_bits_are_refused(sizes):
+    """Keys and rows are counted in 32 bits by steps that end up to 2^16 past the last
+    one."""
+    shape = attend_shape(**{**dict(B=1, Hq=1, Hkv=1, D=1, left=-1), **sizes})
+    assert attend(shape) == dconv.ERANGE
+    assert attend_backward(shape) == dconv.ERANGE
+    n = ctypes.c_longlong()
+    assert dc.load().dconv_attend_workspace(shape, ctypes.byref(n)) == dconv.ERANGE
+    assert dc.load().dconv_attend_backward_workspace(shape, ctypes.byref(n)) == dconv.ERANGE
+
+
+def test_the_longest_walk_is_accepted():
+    shape = attend_shape(B=1, Tq=1, Tk=(1 << 31) - 1 - (1 << 16), Hq=1, Hkv=1, D=1, left=-1)
+    n = ctypes.c_longlong()
+    assert dc.load().dconv_attend_workspace(shape, ctypes.byref(n)) == 0
+
+
 def test_workspaces_off_their_boundary():
     assert attend(attend_shape(B=1, Tq=1, Tk=100000, left=-1), ws=P + 8) == dconv.EINVAL
     assert attend_backward(attend_shape(), ws=P + 4) == dconv.EINVAL
