@@ -161,8 +161,9 @@ DCONV_EXPORT int dconv_join_backward(const dconv_join_shape *shape, const void *
     return DCONV_EINVAL;
   if ((dpost_weight && !post_weight) || (dgate && !gate) || (dpre_weight && !pre_weight))
     return DCONV_ENULL;
+  // (without rows too: the sums of none of them are left there)
   const int64_t need = workspace_bytes_of(*shape);
-  if (!none && (!x || !stats || !dx || (need > 0 && !workspace))) return DCONV_ENULL;
+  if ((!none && (!x || !stats || !dx)) || (need > 0 && !workspace)) return DCONV_ENULL;
   if (workspace_bytes < need) return DCONV_EWORKSPACE;
   if (need > 0 && (uintptr_t)workspace % 16 != 0) return DCONV_EINVAL;
   JoinPtrs p = {};

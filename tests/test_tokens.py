@@ -163,6 +163,16 @@ def test_workspaces():
         assert f(None, ctypes.byref(n)) == dconv.ENULL and f(attend_shape(), None) == dconv.ENULL
 
 
+def test_a_workspace_is_needed_without_rows_too():
+    """The gradients of vectors are written (zeros) where there are no rows, by way of
+    the workspace where there are several sequences."""
+    none = join_shape(B=3, T=0, per=2)
+    n = ctypes.c_longlong()
+    assert dc.load().dconv_join_workspace(none, ctypes.byref(n)) == 0 and n.value > 0
+    assert join_backward(none, ws=None) == dconv.ENULL
+    assert join_backward(none, ws=None, n=0) == dconv.ENULL
+
+
 def test_calls_without_work_need_no_device():
     assert rotate(rotate_shape(B=0), x=None, out=None) == 0
     assert rotate(rotate_shape(T=0)) == 0
