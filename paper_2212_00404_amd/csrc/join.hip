@@ -75,7 +75,7 @@ JoinPlan plan_join(const dconv_join_shape &sh, bool backward) {
   if (runs < 1) runs = 1;
   f.run_rows = (int)((f.rows + runs - 1) / runs);
   if (f.run_rows < 1) f.run_rows = 1;
-  f.runs = (f.rows + f.run_rows - 1) / f.run_rows;
+  f.runs = (int)(((int64_t)f.rows + f.run_rows - 1) / f.run_rows);
   if (f.runs < 1) f.runs = 1;
   return f;
 }

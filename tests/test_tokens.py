@@ -173,6 +173,16 @@ def test_a_workspace_is_needed_without_rows_too():
     assert join_backward(none, ws=None, n=0) == dconv.ENULL
 
 
+def test_as_many_rows_as_are_counted_are_divided_into_runs():
+    """2^31 - 1 rows take as many runs, whose sums the workspace holds, as 2^30 do."""
+    n = ctypes.c_longlong()
+    sizes = []
+    for T in (1 << 30, (1 << 31) - 1):
+        assert dc.load().dconv_join_workspace(join_shape(B=1, T=T, D=1), ctypes.byref(n)) == 0
+        sizes.append(n.value)
+    assert sizes[0] > 0 and abs(sizes[1] - sizes[0]) <= sizes[0] // 100
+
+
 def test_calls_without_work_need_no_device():
     assert rotate(rotate_shape(B=0), x=None, out=None) == 0
     assert rotate(rotate_shape(T=0)) == 0
