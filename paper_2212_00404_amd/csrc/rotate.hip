@@ -156,7 +156,7 @@ __global__ __launch_bounds__(256) void rotate_pieces(const dconv_rotate_shape sh
   if (id >= wk.threads) return;
   const uint32_t rest = id / wk.pieces, t = rest / wk.split;
   const int piece = (int)(id - rest * wk.pieces), h0 = (int)(rest - t * wk.split);
-  for (int b = blockIdx.y; b < sh.B; b += gridDim.y)
+  for (int64_t b = blockIdx.y; b < sh.B; b += gridDim.y)
     rotate_piece<T, ADJACENT, WHOLE>(sh, wk, x, positions, freq, axis, out, piece, h0, t, b);
 }
 

@@ -140,3 +140,15 @@ def test_another_stream_and_a_graph():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(y, dc.rotate(x, at, freq, axis))
+
+
+def test_as_many_sequences_as_are_counted():
+    """2^31 - 1 of them: the workgroups' steps over them pass 32 bits.  (No pair is
+    turned, the one value of each is copied.)"""
+    B = (1 << 31) - 1
+    x = torch.empty((B, 1, 1, 1), dtype=torch.float16, device=DEV)
+    x.view(-1).copy_((torch.arange(1 << 12, device=DEV) % 2039).half().repeat(1 << 19)[:B])
+    at = torch.zeros((1, 1, 1), device=DEV).expand(1, B, 1)
+    none = torch.zeros(0, device=DEV)
+    out = dc.rotate(x, at, none, none.int())
+    assert torch.equal(out, x)
