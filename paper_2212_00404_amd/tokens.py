@@ -29,6 +29,13 @@ _JOIN_SHAPE = struct.Struct("@8i3f8q")
 _ATTEND_SHAPE = struct.Struct("@10if15q")
 
 
+def _pack(layout: struct.Struct, *values) -> bytes:
+    try:
+        return layout.pack(*values)
+    except struct.error as e:
+        raise ValueError("a size or an option is not a whole number of 32 bits (%s)" % e) from None
+
+
 def _tensor(t, name: str, ndim: int, dtype=None, device=None):
     """A tensor of ``ndim`` dimensions on a HIP device whose last dimension is
     contiguous."""
@@ -116,8 +123,8 @@ def rotate(x: torch.Tensor, positions: torch.Tensor, freq: torch.Tensor, axis: t
     elif out is not x:
         _tensor(out, "out", 4, x.dtype, dev)
         _shaped(out, "out", x.shape)
-    shape = _ROTATE_SHAPE.pack(B, T, H, D, R, axes, bool(adjacent), bool(inverse), _DTYPES[x.dtype],
-                               *x.stride()[:3], *out.stride()[:3], *positions.stride())
+    shape = _pack(_ROTATE_SHAPE, B, T, H, D, R, axes, bool(adjacent), bool(inverse), _DTYPES[x.dtype],
+                  *x.stride()[:3], *out.stride()[:3], *positions.stride())
     _check(_call(load().dconv_rotate, x, shape, x.data_ptr(), positions.data_ptr(), freq.data_ptr(),
                  axis.data_ptr(), out.data_ptr()))
     return out
@@ -185,9 +192,8 @@ def _join_arguments(branch, x, norm, post, post_weight, gate, pre_weight, pre_bi
             per |= bit
         elif len(shape) != 1 or shape[0] != D:
             raise ValueError("%s must be %r or %r, got %r" % (name, (D,), (B, D), tuple(shape)))
-    return _JOIN_SHAPE.pack(B, T, D, _DTYPES[dtype], _DTYPES[vt or dtype], _NORMS[norm],
-                            bool(post and branch is not None), per, residual_scale, branch_scale, eps,
-                            *strides)
+    return _pack(_JOIN_SHAPE, B, T, D, _DTYPES[dtype], _DTYPES[vt or dtype], _NORMS[norm],
+                 bool(post and branch is not None), per, residual_scale, branch_scale, eps, *strides)
 
 
 def join(branch: torch.Tensor | None, x: torch.Tensor, *, norm: str = "rms", post: bool = False,
@@ -278,8 +284,8 @@ def _attend_arguments(q, k, v, left, right, sinks, scale, lengths, starts, out, 
         if t is not None and not (_plain(t, 4, dt, index) and t.shape == size):
             _tensor(t, name, 4, dt, dev)
             _shaped(t, name, size)
-    return _ATTEND_SHAPE.pack(
-        B, Tq, Tk, Hq, Hkv, D, _DTYPES[dt], left, right, sinks,
+    return _pack(
+        _ATTEND_SHAPE, B, Tq, Tk, Hq, Hkv, D, _DTYPES[dt], left, right, sinks,
         1.0 / math.sqrt(D) if scale is None else scale, *q.stride()[:3], *k.stride()[:3],
         *v.stride()[:3], *out.stride()[:3], *((0, 0, 0) if dout is None else dout.stride()[:3]))
 

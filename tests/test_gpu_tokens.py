@@ -133,3 +133,11 @@ def test_binding_refusals():
                 lambda: dc.join_backward(x, x, x, x, torch.zeros((2, 3, 3), device=DEV))):
         with pytest.raises(ValueError):
             bad()
+
+
+@pytest.mark.parametrize("option", [dict(left=1 << 31), dict(right=1 << 40), dict(sinks=1 << 31), dict(left=3.0)],
+                         ids=str)
+def test_options_past_32_bits_are_refused_by_the_binding(option):
+    q = torch.zeros((1, 2, 1, 16), device=DEV)
+    with pytest.raises(ValueError):
+        dc.attend(q, q, q, **option)
