@@ -12,7 +12,7 @@
 namespace dconv {
 
 // Debug builds (-DDCONV_POISON_LDS, libdconv_poison.so): every LDS buffer of
-// a kernel starts filled with ones in every bit, NaN as fp32 and as bf16, so an
+// a kernel starts filled with ones in every bit, NaN as fp32, fp16 and bf16, so an
 // output computed from LDS that the kernel did not write first (a missing
 // copy, wait or barrier before the first use of a buffer) comes out non-finite;
 // and the kernels on bf16 triples leave non-finite sums as they are
@@ -22,8 +22,9 @@ namespace dconv {
 constexpr bool kSumAgain = false;
 template <class T>
 __device__ __forceinline__ void poison_lds(T *p, int n) {
+  static_assert(sizeof(T) == 2 || sizeof(T) % 4 == 0, "whole words, or an even number of halves");
   uint32_t *w = reinterpret_cast<uint32_t *>(p);
-  const int nw = n * (int)(sizeof(T) / sizeof(uint32_t));
+  const int nw = (int)(n * sizeof(T) / sizeof(uint32_t));
   for (int i = threadIdx.x; i < nw; i += blockDim.x) w[i] = 0xffffffffu;
 }
 #define DCONV_POISON(...) \

@@ -12,7 +12,7 @@ import torch
 
 import paper_2212_00404_amd as dc
 import token_ref as ref
-from paper_2212_00404_amd import dconv, tokens
+from paper_2212_00404_amd import build, dconv, tokens
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 P = 0x1000      # never dereferenced: validation comes first
@@ -276,3 +276,22 @@ def test_reference_rotation_keeps_lengths_and_composes():
         assert torch.allclose(twice, y, atol=1e-12)
         assert torch.equal(y[..., 10:], x[..., 10:].double())
         assert torch.allclose(ref.rotate(y, one * 3, freq, axis, adjacent, inverse=True), x.double(), atol=1e-12)
+
+
+@pytest.mark.skipif(shutil.which(build._hipcc()) is None, reason="needs hipcc")
+@pytest.mark.parametrize("element", ["_Float16", "__bf16", "float", "float2"])
+def test_the_poisoning_build_fills_lds_of_any_element(tmp_path, element):
+    """Its kernels begin by writing their LDS: the code of one that only does that and
+    reads it back has a write, whatever the elements' size."""
+    src = tmp_path / "fill.hip"
+    src.write_text('#include "internal.h"\n'
+                   "extern \"C\" __global__ void fill(%s *out) {\n"
+                   "  __shared__ __align__(16) %s buf[256];\n"
+                   "  DCONV_POISON(dconv::poison_lds(buf, 256));\n"
+                   "  out[threadIdx.x] = buf[255 - threadIdx.x];\n}\n" % (element, element))
+    res = subprocess.run([build._hipcc()] + build.CFLAGS + ["-DDCONV_POISON_LDS", "--offload-device-only", "-S",
+                                                            str(src), "-o", str(tmp_path / "fill.s")],
+                         capture_output=True, text=True)
+    assert res.returncode == 0, res.stderr
+    code = (tmp_path / "fill.s").read_text()
+    assert "ds_read" in code and "ds_write" in code
