@@ -257,3 +257,38 @@ def test_gradients_against_differences():
         want = (f(1) - f(-1)) / 2e-4
         terms = grads[n].cpu().double() * d
         assert abs(terms.sum() - want) <= 1e-5 * terms.abs().sum() + 1e-6, n
+
+
+@pytest.mark.parametrize("types", PAIRS, ids=PAIR_IDS)
+@pytest.mark.parametrize("size", [(3, 17, 65), (2, 33, 512), (4, 700, 96), (5, 1, 1000)], ids=str)
+@pytest.mark.parametrize("norm", ["rms", "layer"])
+def test_every_vector_for_each_sequence(size, types, norm):
+    """post_weight too, which make() gives one row to."""
+    st, dh, dy, how = make(50, *types, *size, norm, True, True)
+    g = torch.Generator().manual_seed(51)
+    B, _, D = size
+    st["post_weight"] = (torch.randn((B, D), generator=g) * 0.3 + 0.8).to(types[1]).to(DEV)
+    compare_per_sample_post(st, dh, dy, how)
+
+
+def compare_per_sample_post(st, dh, dy, how):
+    """compare(), one sequence at a time in 64 bits (a [1, D] post_weight there is a [D]
+    one): the bounds of each sequence are its own."""
+    dt, D = st["x"].dtype, st["x"].shape[-1]
+    how_f = dict(how, **{n: st[n] for n in VECTORS})
+    h, y, stats = dc.join(st["branch"], st["x"], return_stats=True, **how_f)
+    grads = dc.join_backward(dh, dy, st["branch"], st["x"], stats, **how_f)
+    for b in range(st["x"].shape[0]):
+        one = {n: t[b] if n in VECTORS else t[b:b + 1] for n, t in st.items()}
+        wh, wy, wg = reference(one, dh[b:b + 1], dy[b:b + 1], how)
+        big_x, big_b = before_cancelling(one, dy[b:b + 1], how, wh, wg)
+        ref.check(h[b:b + 1], wh, row_tol(wh, dt, D), "h")
+        ref.check(y[b:b + 1], wy, row_tol(wy, dt, D), "y")
+        ref.check(grads["x"][b:b + 1], wg["x"], row_tol(wg["x"], dt, D, big_x), "dx")
+        ref.check(grads["branch"][b:b + 1], wg["branch"], row_tol(wg["branch"], dt, D, big_b), "dbranch")
+        rows = st["x"].shape[1]
+        for n in VECTORS:
+            gt = wg[n]
+            tol = 2 * ref.UNIT[st[n].dtype] * gt.abs() + (math.sqrt(D) + 16 + math.sqrt(rows)) * 2.0 ** -23 * \
+                math.sqrt(rows) * 8 * max(1.0, gt.abs().max().item())
+            ref.check(grads[n][b], gt, tol, "d" + n)
