@@ -1,9 +1,12 @@
 """The operators over tokens without a GPU: refusals of the C ABI and of the
 binding, the packed structs, workspace queries, and the 64-bit forms that the GPU
 tests compare with."""
+import ast
 import ctypes
+import inspect
 import math
 import os
+import re
 import shutil
 import subprocess
 
@@ -295,3 +298,17 @@ def test_the_poisoning_build_fills_lds_of_any_element(tmp_path, element):
     assert res.returncode == 0, res.stderr
     code = (tmp_path / "fill.s").read_text()
     assert "ds_read" in code and "ds_write" in code
+
+
+def test_the_readme_calls_what_there_is():
+    """Its calls fit the functions' signatures, and the tables of a rotation are made on
+    a device (rotate takes no others)."""
+    with open(os.path.join(ROOT, "README.md"), encoding="utf-8") as f:
+        blocks = re.findall(r"```python\n(.*?)```", f.read(), re.S)
+    calls = [c for b in blocks for c in ast.walk(ast.parse(b)) if isinstance(c, ast.Call)
+             and isinstance(c.func, ast.Attribute) and getattr(c.func.value, "id", None) == "dc"]
+    assert {"attend", "attend_backward", "rotate", "join"} <= {c.func.attr for c in calls}
+    for c in calls:
+        inspect.signature(getattr(dc, c.func.attr)).bind(*c.args, **{k.arg: k.value for k in c.keywords})
+        if c.func.attr in ("rotary_table", "map_positions"):
+            assert "device" in [k.arg for k in c.keywords], ast.unparse(c)
