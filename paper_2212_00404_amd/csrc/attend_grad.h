@@ -1,8 +1,8 @@
 // The gradients of windowed attention on the matrix cores.  Probabilities are
 // computed again from the scores and the forward call's sums; with
 //   ds = p (dout . v - delta),  delta = dout . out
-// the two kernels below need three and four products per tile of scores.
-// attend_dq walks the keys for each tile of rows as the forward kernel does, and
+// the kernels below take four products per tile of scores each (attend_dq one of
+// them for delta's rounding).  attend_dq walks the keys for each tile of rows as the forward kernel does, and
 // leaves each row's sum and delta for the others; attend_dkv and attend_dkv_split
 // walk the rows for each tile of keys.  Nothing is added by atomics: the order
 // of every sum is fixed.

@@ -7,6 +7,10 @@ Argument marshalling only, as in ``dconv.py``: every computation runs in the
 HIP kernels of ``libdconv.so`` (``include/dconv.h`` has the definitions); this
 module checks the tensors, allocates outputs and workspaces on the current
 torch stream and passes device pointers.  fp32, fp16 and bf16.
+
+Nothing here is recorded by autograd: results do not require gradients, whatever
+the arguments do.  The gradients are calls of their own, which the caller makes or
+wraps in a ``torch.autograd.Function`` (``examples/token_block.py`` has one for each).
 """
 from __future__ import annotations
 
@@ -327,7 +331,8 @@ def attend_backward(dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: tor
                     sinks: int = 0, scale: float | None = None, lengths: torch.Tensor | None = None,
                     starts: torch.Tensor | None = None):
     """``(dq, dk, dv)`` of ``attend`` for the gradient ``dout`` of its output.
-    ``out`` and ``lse`` are what it returned, the other arguments what it took."""
+    ``out`` and ``lse`` are what it returned, the other arguments what it took.
+    (Heads of more than 128 are some hundred times slower.)"""
     _tensor(dout, "dout", 4)
     shape = _attend_arguments(q, k, v, left, right, sinks, scale, lengths, starts, out, dout)
     _tensor(lse, "lse", 3, torch.float32, q.device)
