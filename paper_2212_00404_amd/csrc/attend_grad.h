@@ -50,8 +50,8 @@ __device__ __forceinline__ float frag_dot(typename Mma<T>::Frag a, typename Mma<
 // What is rounded below the normal values is then off by less than 2^-23 of the
 // column's largest, and the scales lose nothing, as they are powers of two.  Below 2
 // the first bit of the exponent is 0, so that one bit of each operand tells.  (It costs
-// fp16 5 to 15%, in the branch's moves of sums between register files: 2 x 4096
-// queries, 16 heads of 64 over 4, window 512: 130 -> 146 us.)
+// fp16 1 to 16%, in the branch's moves of sums between register files: 2 x 4096
+// queries, 16 heads of 64 over 4, window 512: 132 -> 147 us.)
 template <class T>
 constexpr bool kScaled = std::is_same<T, f16_t>::value;
 template <class T>
