@@ -134,7 +134,7 @@ def _lengths(case):
     B, most = case["B"], case["longest"]
     if not case["ragged"]:
         return [most] * B
-    return [max(r, most - b * (most // (B + 1)) - (b * 37) % max(1, most // 8))
+    return [max(r, most - b * (most // (B + 1)) - (b * 37) % max(1, most // (2 * B + 2)))
             for b, r in enumerate(_rows(case))]
 
 
