@@ -490,6 +490,116 @@ int dconv_attend_backward(const dconv_attend_shape *shape, const void *dout, con
                           const int *lengths, const int *starts, void *dq, void *dk, void *dv,
                           void *workspace, long long workspace_bytes, void *stream);
 
+/* ==========================================================================
+ * A cache of keys and values in pages
+ *
+ * Sequences of different lengths share one pool of pages, each of page_size
+ * tokens.  Token i of sequence b is in slot i % page_size of page
+ * table[b][i / page_size].  What the three calls below have in common:
+ *
+ *   rows : N tokens of B sequences, one sequence behind another.  Sequence b
+ *     has the rows offsets[b] .. offsets[b+1] - 1 (int32 [B+1], taken as 0 .. N,
+ *     none where they fall), or, with offsets NULL, N / B rows like every
+ *     other (N a multiple of B).  They are its last tokens: row t of its n rows
+ *     stands at position lengths[b] - n + t.  Rows of no sequence (behind
+ *     offsets[B]) are neither read nor written.
+ *   lengths : int32 [B], the tokens of each sequence, its rows among them;
+ *     taken as 0 .. table_width * page_size
+ *   table : int32 [B][table_width] with a stride for sequences; an entry that is
+ *     no page (negative, or not below `pages`) is a page without tokens
+ *   k, v of the cache : [pages][page_size][Hkv][D] with strides for page, slot
+ *     and head, that count stored elements
+ *
+ * A cache is plain (elements of a type of its own), or holds 8 or 4 bits for an
+ * element and one byte for each 32 neighbours of a head, the exponent s of a
+ * scale 2^(s - 127) (255: not a number).  Then D is a multiple of 32, elements
+ * are bytes (of two elements in 4 bits, the first in the low half) and k_scale,
+ * v_scale are [pages][page_size][Hkv][D / 32] with strides like those of k, v.
+ *   DCONV_CACHE_E4M3 : sign, 4 bits of exponent, 3 of mantissa, up to M = 448
+ *   DCONV_CACHE_E2M1 : sign, 2 bits of exponent, 1 of mantissa, up to M = 6
+ * Every element stands for exactly code * scale.
+ * ======================================================================== */
+#define DCONV_CACHE_PLAIN 0
+#define DCONV_CACHE_E4M3 1
+#define DCONV_CACHE_E2M1 2
+
+typedef struct dconv_cache {
+  int pages, page_size, Hkv, D;
+  int format;
+  int dtype; /* of a plain cache's elements */
+  long long k_stride[3], v_stride[3], k_scale_stride[3], v_scale_stride[3];
+} dconv_cache;
+
+typedef struct dconv_cache_rows {
+  int B, N, table_width;
+  int dtype; /* of k and v; a plain cache's own */
+  long long table_stride;
+  long long k_stride[2], v_stride[2]; /* of the rows: token, head */
+} dconv_cache_rows;
+
+/*
+ * dconv_cache_write -- the rows k, v [N][Hkv][D] into their places.  A row whose
+ * position is negative, or whose page is none, is left out.
+ *
+ * For 8 and 4 bits each block of 32 neighbours is limited to +-L, L the largest
+ * value of the format's mantissa in the rows' type (1.875 x 2^15 for e4m3 of
+ * fp16, 1.5 x 2^15 for e2m1; x 2^127 for bf16 and fp32), so that all that is
+ * finite reads back as finite.  The scale is the smallest power of two from
+ * 2^-127 on by which no element exceeds M, and each element is rounded once, to
+ * nearest even.  A block that holds an infinity or NaN reads back as NaN.
+ * What a slot holds that one call writes twice is not defined.
+ */
+int dconv_cache_write(const dconv_cache *cache, const dconv_cache_rows *rows, const void *k,
+                      const void *v, void *cache_k, void *cache_v, void *k_scale, void *v_scale,
+                      const int *table, const int *lengths, const int *offsets, void *stream);
+
+/*
+ * dconv_cache_read -- the same rows back, into k, v [N][Hkv][D], rounded to
+ * their type; zeros for a row whose position is negative or whose page is none.
+ */
+int dconv_cache_read(const dconv_cache *cache, const dconv_cache_rows *rows, const void *cache_k,
+                     const void *cache_v, const void *k_scale, const void *v_scale,
+                     const int *table, const int *lengths, const int *offsets, void *k, void *v,
+                     void *stream);
+
+/*
+ * dconv_cache_attend -- dconv_attend of new tokens over the cache.  The query of
+ * a row at position i sees key j of its sequence if
+ *     j < length,  i >= 0,  j <= i + right,  (j >= i - left or j < sinks),
+ * and the key's page is one.  Head h reads the keys and values of head
+ * h / (Hq / Hkv); out, lse, left, right, sinks and scale are dconv_attend's.
+ *
+ *   q, out : [N][Hq][D], strides for token and head; out must not overlap q
+ *   lse : NULL or fp32 [N][Hq], written
+ *   max_rows : no sequence has more rows than this (0: N); with offsets NULL
+ *     it is N / B.  A sequence that has more is left out: its rows of out
+ *     are not written.  (With few rows one kernel is launched, not two.)
+ *   workspace : dconv_cache_attend_workspace bytes, 16-byte aligned
+ * Keys and values that are not seen do not reach a result, whatever they, their
+ * scales and the table's entries behind a sequence's last page hold.  Values of
+ * 8 and 4 bits are rounded to the type of q (which changes nothing for bf16).
+ * 1 <= D <= 256; table_width * page_size and N * Hq below 2^31 - 2^16, B up to
+ * 2^20, else DCONV_ERANGE.
+ */
+typedef struct dconv_cache_attend_shape {
+  int B, N, table_width;
+  int Hq, dtype;
+  int left, right, sinks;
+  int max_rows;
+  float scale;
+  long long table_stride;
+  long long q_stride[2], out_stride[2];
+} dconv_cache_attend_shape;
+
+int dconv_cache_attend_workspace(const dconv_cache *cache, const dconv_cache_attend_shape *shape,
+                                 long long *bytes);
+
+int dconv_cache_attend(const dconv_cache *cache, const dconv_cache_attend_shape *shape,
+                       const void *q, const void *cache_k, const void *cache_v,
+                       const void *k_scale, const void *v_scale, const int *table,
+                       const int *lengths, const int *offsets, void *out, float *lse,
+                       void *workspace, long long workspace_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -40,7 +40,8 @@ EXPORTED = ("dconv_single", "dconv_single_variant", "dconv_multi", "dconv_multi_
             "dconv_plan_single_paper", "dconv_probe_latency", "dconv_rotate", "dconv_join",
             "dconv_join_workspace", "dconv_join_backward", "dconv_attend",
             "dconv_attend_workspace", "dconv_attend_backward",
-            "dconv_attend_backward_workspace")
+            "dconv_attend_backward_workspace", "dconv_cache_write", "dconv_cache_read",
+            "dconv_cache_attend", "dconv_cache_attend_workspace")
 
 
 class Plan(ctypes.Structure):
@@ -174,8 +175,13 @@ def load(path: str | None = None):
     lib.dconv_attend_workspace.argtypes = [vp, size]
     lib.dconv_attend_backward.argtypes = [vp] * 13 + [ll, vp]
     lib.dconv_attend_backward_workspace.argtypes = [vp, size]
+    lib.dconv_cache_write.argtypes = [vp] * 12
+    lib.dconv_cache_read.argtypes = [vp] * 12
+    lib.dconv_cache_attend.argtypes = [vp] * 13 + [ll, vp]
+    lib.dconv_cache_attend_workspace.argtypes = [vp, vp, size]
     for name in ("rotate", "join", "join_workspace", "join_backward", "attend", "attend_workspace",
-                 "attend_backward", "attend_backward_workspace"):
+                 "attend_backward", "attend_backward_workspace", "cache_write", "cache_read",
+                 "cache_attend", "cache_attend_workspace"):
         getattr(lib, "dconv_" + name).restype = i
     if path is None:
         _lib = lib
