@@ -94,4 +94,26 @@ __device__ void cache_attend_row(const dconv_cache &c, const dconv_cache_attend_
   if (p.lse && lane == 0) p.lse[(int64_t)row * sh.Hq + h] = any ? m + logf((float)l) : -INFINITY;
 }
 
+// Rows of one key head that are joined from parts: its sums are those that `parts`
+// workgroups from `first` on have left.
+struct CacheJoin {
+  int parts, first;
+  int b, hk, r0, rows;
+};
+
+// How a call runs: workgroups for sequences of up to 32 rows of a key head
+// (cache_few) and for others (cache_tiles), 0 for a kernel that is not needed.
+struct CachePlan {
+  int dp;                       // head size the kernels are built for
+  bool direct, pieces, near;    // as in CacheTile
+  int few, tiles;               // workgroups
+  int few_least, tiles_least;   // least work of one, in keys
+  int64_t joins_bytes, workspace;
+};
+
+// Instantiated in cache_attend_*.hip.
+template <class T, int FORMAT>
+void launch_cache_attend(const dconv_cache &c, const dconv_cache_attend_shape &sh, const Batch &t,
+                         const CacheAttendPtrs &p, const CachePlan &plan, char *workspace, hipStream_t s);
+
 }  // namespace dconv

@@ -10,20 +10,6 @@
 namespace dconv {
 namespace {
 
-// One wave per row and head, four per workgroup.
-template <class T, int FORMAT>
-__global__ __launch_bounds__(256) void cache_attend_rows(const dconv_cache c, const dconv_cache_attend_shape sh,
-                                                         const Batch t, const CacheAttendPtrs p) {
-  const int64_t i = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (i >= (int64_t)t.N * sh.Hq) return;
-  const int row = (int)(i / sh.Hq), h = (int)(i % sh.Hq);
-  const int b = sequence_of(t, p.cache, row);
-  if (b < 0) return;
-  const Rows s = rows_of(t, p.cache, b);
-  if (sh.max_rows > 0 && s.n > sh.max_rows) return;
-  cache_attend_row<T, FORMAT>(c, sh, t, p, b, s, row, h);
-}
-
 template <class F>
 void by_type(int dtype, F f) {
   if (dtype == DCONV_F32) return f((float *)nullptr);
@@ -42,6 +28,60 @@ int validate(const dconv_cache &c, const dconv_cache_attend_shape &sh) {
   return batch_range(sh.B, sh.N, sh.table_width, c.page_size);
 }
 
+// Rows in memory as whole 16-byte pieces on 4-byte boundaries.
+bool whole_pieces(const void *p, int D, int es, std::initializer_list<long long> strides) {
+  bool whole = D * es % 16 == 0 && (uintptr_t)p % 4 == 0;
+  for (long long s : strides) whole = whole && s % (4 / es) == 0;
+  return whole;
+}
+
+int padded_head(int D) { return D <= 32 ? 32 : D <= 64 ? 64 : D <= 96 ? 96 : D <= 128 ? 128 : 256; }
+
+CachePlan plan_attend(const dconv_cache &c, const dconv_cache_attend_shape &sh) {
+  CachePlan f = {};
+  f.dp = padded_head(c.D);
+  const int es = element_size(sh.dtype), G = sh.Hq / c.Hkv;
+  const int64_t rows = (int64_t)(sh.max_rows > 0 ? sh.max_rows : sh.N) * G;
+  const int64_t keys = (int64_t)sh.table_width * c.page_size + 64;
+  // Two workgroups per compute unit, where LDS and registers hold them; no more than
+  // there is work for.
+  auto groups = [](int64_t most, int64_t work, int least) {
+    const int64_t n = (work + least - 1) / least;
+    return (int)(n < 1 ? 1 : n < most ? n : most);
+  };
+  f.few_least = 256;
+  f.tiles_least = 512;
+  f.few = groups(f.dp * es <= 256 ? 512 : 256, (int64_t)sh.B * c.Hkv * keys, f.few_least);
+  if (rows > 32) {
+    const int64_t tiles = ((int64_t)sh.N * G / 128 + sh.B) * c.Hkv;
+    f.tiles = groups(f.dp * es <= 256 ? 512 : 256, tiles * keys, f.tiles_least);
+  }
+  f.joins_bytes = ((int64_t)(f.few + f.tiles) * (int64_t)sizeof(CacheJoin) + 15) / 16 * 16;
+  f.workspace = f.joins_bytes + ((int64_t)f.few * 32 + (int64_t)f.tiles * 128) * 2 * (f.dp + 2) * 4;
+  return f;
+}
+
+int launch(const dconv_cache &c, const dconv_cache_attend_shape &sh, const Batch &t, const CacheAttendPtrs &p,
+           CachePlan &plan, void *workspace, void *stream) {
+  const int es = element_size(sh.dtype);
+  plan.direct = whole_pieces(p.q, c.D, es, {sh.q_stride[0], sh.q_stride[1]}) &&
+                whole_pieces(p.out, c.D, es, {sh.out_stride[0], sh.out_stride[1]});
+  if (c.format == DCONV_CACHE_PLAIN) {
+    plan.pieces = whole_pieces(p.cache.k, c.D, es, {c.k_stride[0], c.k_stride[1], c.k_stride[2]}) &&
+                  whole_pieces(p.cache.v, c.D, es, {c.v_stride[0], c.v_stride[1], c.v_stride[2]});
+    const long long far = (1ll << 31) / es / 64 - c.D;   // (a copy has 16 rows at most)
+    plan.near = plan.pieces && c.k_stride[1] >= 0 && c.k_stride[1] < far && c.v_stride[1] >= 0 && c.v_stride[1] < far;
+  }
+  (void)hipGetLastError();  // report this launch only
+  by_type(sh.dtype, [&](auto *type) {
+    by_format(c.format, [&](auto format) {
+      launch_cache_attend<std::remove_pointer_t<decltype(type)>, decltype(format)::value>(
+          c, sh, t, p, plan, static_cast<char *>(workspace), (hipStream_t)stream);
+    });
+  });
+  return hipGetLastError() == hipSuccess ? DCONV_OK : DCONV_EHIP;
+}
+
 }  // namespace
 }  // namespace dconv
 
@@ -49,7 +89,7 @@ DCONV_EXPORT int dconv_cache_attend_workspace(const dconv_cache *cache, const dc
                                               long long *bytes) {
   if (!cache || !shape || !bytes) return DCONV_ENULL;
   const int rc = dconv::validate(*cache, *shape);
-  if (rc == DCONV_OK) *bytes = 0;
+  if (rc == DCONV_OK) *bytes = shape->B == 0 || shape->N == 0 ? 0 : dconv::plan_attend(*cache, *shape).workspace;
   return rc;
 }
 
@@ -71,14 +111,12 @@ DCONV_EXPORT int dconv_cache_attend(const dconv_cache *cache, const dconv_cache_
   p.lse = lse;
   if (!q || !out || !cache_pointers(*cache, p.cache) || !lengths || (shape->table_width > 0 && !table)) return DCONV_ENULL;
   const Batch t = batch_of(*cache, shape->B, shape->N, shape->table_width, shape->table_stride, offsets);
-  const unsigned grid = (unsigned)(((int64_t)shape->N * shape->Hq + 3) / 4);
-  (void)hipGetLastError();  // report this launch only
-  by_type(shape->dtype, [&](auto *type) {
-    using T = std::remove_pointer_t<decltype(type)>;
-    by_format(cache->format, [&](auto format) {
-      hipLaunchKernelGGL((cache_attend_rows<T, decltype(format)::value>), dim3(grid), dim3(256), 0,
-                         (hipStream_t)stream, *cache, *shape, t, p);
-    });
-  });
-  return hipGetLastError() == hipSuccess ? DCONV_OK : DCONV_EHIP;
+  dconv_cache_attend_shape sh = *shape;
+  if (!offsets) sh.max_rows = t.each;
+  CachePlan plan = plan_attend(*cache, sh);
+  if (plan.workspace > 0 && !workspace) return DCONV_ENULL;
+  if (workspace_bytes < plan.workspace) return DCONV_EWORKSPACE;
+  if ((uintptr_t)workspace % 16 != 0) return DCONV_EINVAL;
+  if (!offsets && plan.tiles > 0) plan.few = 0;   // all sequences are alike
+  return launch(*cache, sh, t, p, plan, workspace, stream);
 }

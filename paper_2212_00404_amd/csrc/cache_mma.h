@@ -1,0 +1,861 @@
+// Attention over a cache in pages on the matrix cores: the products and the
+// running softmax of attend_mma.h over tiles of keys whose places a table gives.
+// Instantiated per type and format in cache_attend_*.hip.
+#pragma once
+
+#include "attend_mma.h"
+#include "cache_attend.h"
+
+namespace dconv {
+
+// What the host hands to the kernels beside the shape.
+struct CacheTile {
+  float scale2, sign;   // as in AttendTile
+  bool direct;          // queries and results in 16-byte pieces
+  bool pieces, near;    // rows of a plain cache too; and those of one copy span less than 2^31 bytes
+  int groups, least;    // workgroups, the least work of one
+  float *partial;       // two parts of each workgroup's
+  CacheJoin *joins;     // one of each workgroup's
+};
+
+// ---------------------------------------------------------------------------
+// The keys of a tile of rows
+// ---------------------------------------------------------------------------
+// Keys [0, first) and [lo, hi), as tiles of BN that begin on multiples of BN: so a
+// tile lies within a page, or consists of whole pages, for every page size that is a
+// power of two.
+template <int BN>
+struct KeyRange {
+  int first, lo, hi;
+  int front, from, n;   // tiles of the first keys, first tile of the others, tiles
+  __device__ __forceinline__ KeyRange(const dconv_cache_attend_shape &sh, int len, int i0, int i1) {
+    first = lo = hi = front = from = n = 0;
+    if (i1 < 0) return;
+    const KeySpan a = keys_seen(sh, len, max(i0, 0)), b = keys_seen(sh, len, i1);
+    first = uniform(a.first);
+    lo = uniform(a.lo);
+    hi = uniform(b.hi);
+    front = (first + BN - 1) / BN;
+    from = max(front, lo / BN);
+    n = front + max(hi > lo ? (hi + BN - 1) / BN - from : 0, 0);
+  }
+  __device__ __forceinline__ int start(int u) const { return (u < front ? u : u - front + from) * BN; }
+  // j, or where no row sees it a key that one sees.
+  __device__ __forceinline__ int key(int j) const {
+    if (j < first) return j;
+    if (j < lo) return first > 0 ? first - 1 : lo;
+    return min(j, hi - 1);
+  }
+  __device__ __forceinline__ bool whole(int j0) const { return (j0 >= lo && j0 + BN <= hi) || j0 + BN <= first; }
+};
+
+// Where the keys of a tile are, key l of it in lane l (and l + 32 for 32 keys): asked
+// for a tile ahead, as the table's entry comes from memory.
+struct Asked {
+  int page, slot;
+};
+struct Found {
+  int64_t k, v, ks, vs;   // bytes from the head's base
+  uint64_t gone;          // keys without a page, whose places are the first page's
+};
+template <class T, int FORMAT, int BN>
+struct Finder {
+  static constexpr int64_t kBytes = FORMAT == DCONV_CACHE_PLAIN ? sizeof(T) : 1;
+  const int *table;
+  FastDiv page;
+  int pages;
+  __device__ __forceinline__ Asked ask(const KeyRange<BN> &keys, int j0) const {
+    const uint32_t j = (uint32_t)keys.key(j0 + (int)(threadIdx.x & (BN - 1)));
+    const uint32_t at = page.div(j);
+    return {table[at], (int)(j - at * page.d)};
+  }
+  __device__ __forceinline__ Found find(const dconv_cache &c, const Asked &a) const {
+    const bool there = a.page >= 0 && a.page < pages;
+    const int64_t p = there ? a.page : 0;
+    Found f;
+    f.k = (p * c.k_stride[0] + a.slot * c.k_stride[1]) * kBytes;
+    f.v = (p * c.v_stride[0] + a.slot * c.v_stride[1]) * kBytes;
+    f.ks = f.vs = 0;
+    if constexpr (FORMAT != DCONV_CACHE_PLAIN) {
+      f.ks = p * c.k_scale_stride[0] + a.slot * c.k_scale_stride[1];
+      f.vs = p * c.v_scale_stride[0] + a.slot * c.v_scale_stride[1];
+    }
+    f.gone = __ballot(!there);
+    return f;
+  }
+};
+
+__device__ __forceinline__ int64_t from_lane(int64_t x, int lane) {
+  const int lo = __shfl((int)x, lane), hi = __shfl((int)(x >> 32), lane);
+  return (int64_t)hi << 32 | (uint32_t)lo;
+}
+__device__ __forceinline__ int64_t from_uniform_lane(int64_t x, int lane) {
+  const int lo = __builtin_amdgcn_readlane((int)x, lane), hi = __builtin_amdgcn_readlane((int)(x >> 32), lane);
+  return (int64_t)hi << 32 | (uint32_t)lo;
+}
+
+// ---------------------------------------------------------------------------
+// Tiles of a plain cache: copied into LDS
+// ---------------------------------------------------------------------------
+template <class T, int DP, int BN, int NW>
+struct PlainTiles {
+  typedef Copy<T, DP, BN, NW> C;
+  static constexpr int kRows = 64 / C::kPieces;           // of one copy of a wave, where they are whole
+  static constexpr bool kWhole = 64 % C::kPieces == 0;
+  uint32_t offset[C::kStep ? 1 : C::kCopies];             // of the lane's pieces from the copy's first row
+
+  __device__ __forceinline__ void init(int D, int64_t slot_stride, int wave, int lane) {
+    if constexpr (kWhole) {
+#pragma unroll
+      for (int i = 0; i < (C::kStep ? 1 : C::kCopies); ++i)
+        offset[i] = (uint32_t)(C::row(i, wave, lane) % kRows) * (uint32_t)slot_stride * (uint32_t)sizeof(T) +
+                    C::element(i, wave, lane, D) * (uint32_t)sizeof(T);
+    }
+  }
+  // The tile whose rows' places the lanes hold in `at`.  `close`: the rows of a copy
+  // stand in one page: a scalar base and a 32-bit offset each.
+  __device__ __forceinline__ void stage(T *lds, const char *base, int64_t at, bool close, bool pieces, int D, int wave,
+                                        int lane) const {
+    if constexpr (kWhole) {
+      if (close) {
+#pragma unroll
+        for (int i = 0; i < C::kCopies; ++i) {
+          if (!C::has(i, wave)) break;
+          uint32_t o = offset[C::kStep ? 0 : i];
+          asm volatile("" : "+v"(o));
+          const char *row = base + from_uniform_lane(at, (i * C::kThreads + 64 * wave) / C::kPieces);
+          __builtin_amdgcn_global_load_lds(row + o, (lds_ptr)C::to(lds, i, wave), 16, 0, 0);
+        }
+        return;
+      }
+    }
+    auto row = [&](int r) { return reinterpret_cast<const T *>(base + from_lane(at, r)); };
+    if (pieces) {
+      C::rows(lds, D, wave, lane, row);
+      return;
+    }
+    // rows that are no whole pieces: element by element, zeros past D
+    for (int x = 64 * wave + lane; x < BN * DP; x += C::kThreads) {
+      const int r = x / DP, d = x % DP;
+      const T *from = row(r);   // (by all lanes: places are in lanes)
+      lds[Tile<T, DP>::at(r, d >> 3) + (d & 7)] = d < D ? from[d] : from_f32<T>(0.0f);
+    }
+  }
+};
+
+// ---------------------------------------------------------------------------
+// Tiles of 8 and 4 bits: read into registers a tile ahead, converted into LDS
+// ---------------------------------------------------------------------------
+// A thread takes blocks of 32 neighbours with their scale, of keys and values both.
+template <class T, int DP, int BN, int NT, int FORMAT>
+struct CodeTiles {
+  static constexpr int kBlocks = DP / kBlock, kTensor = BN * kBlocks, kAll = 2 * kTensor;
+  static constexpr int kPer = (kAll + NT - 1) / NT, kWords = kBlock / codes_per_word<FORMAT>();
+  struct __attribute__((packed, aligned(1))) Raw {
+    uint32_t w[kWords];
+  };
+  Raw raw[kPer];
+  uint32_t scale[kPer];
+
+  static __device__ __forceinline__ bool has(int u) { return kAll % NT == 0 || u < kAll; }
+  __device__ __forceinline__ void load(const char *k, const char *v, const uint8_t *ks, const uint8_t *vs,
+                                       const Found &f, int D, int thread) {
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const int u = i * NT + thread, x = u % kTensor, row = x / kBlocks, blk = x % kBlocks;
+      int64_t at, sat;
+      bool value = u >= kTensor;
+      if constexpr (kTensor % 64 == 0) {
+        value = uniform(value);   // a wave's are of one tensor
+        at = from_lane(value ? f.v : f.k, row);
+        sat = from_lane(value ? f.vs : f.ks, row);
+      } else {
+        const int64_t ak = from_lane(f.k, row), av = from_lane(f.v, row), sk = from_lane(f.ks, row),
+                      sv = from_lane(f.vs, row);
+        at = value ? av : ak;
+        sat = value ? sv : sk;
+      }
+      raw[i] = {};
+      scale[i] = 0;
+      if (has(u) && blk * kBlock < D) {
+        raw[i] = *reinterpret_cast<const Raw *>((value ? v : k) + at + blk * (kWords * 4));
+        scale[i] = (value ? vs : ks)[sat + blk];
+      }
+    }
+  }
+  // (a block past the head's end is zeros: codes 0 times 2^-127)
+  __device__ __forceinline__ void store(T *kt, T *vt, int thread) const {
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const int u = i * NT + thread, x = u % kTensor, row = x / kBlocks, blk = x % kBlocks;
+      if (!has(u)) break;
+      T *to = u >= kTensor ? vt : kt;
+      constexpr int kPairs = codes_per_word<FORMAT>() / 2;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        struct alignas(16) {
+          T x[8];
+        } y;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          decode_pair<T, FORMAT>(raw[i].w[(4 * j + e) / kPairs], (4 * j + e) % kPairs, scale_of(scale[i]), y.x + 2 * e);
+        __builtin_memcpy(__builtin_assume_aligned(to + Tile<T, DP>::at(row, 4 * blk + j), 16), &y, sizeof(y));
+      }
+    }
+  }
+};
+
+// ---------------------------------------------------------------------------
+// Division of the work
+// ---------------------------------------------------------------------------
+// An item is a tile of rows of one key head of one sequence; its work is its number
+// of keys and a constant.  Lengths are on the device, so every workgroup sums all
+// sequences' work and takes an equal share of it, a range of a line on which the
+// items stand one behind another: parts of two items, and whole ones between them.
+// A wave's lanes take as many sequences each.  Cuts depend on the line alone, so the
+// workgroups agree on them, and sums are joined in a fixed order.
+constexpr int kFewRows = 32, kTileRows = 128;
+
+template <bool FEW>
+struct Work {
+  int rows, tiles;          // of a key head
+  int64_t base, cap, step;  // work of tile i: min(base + i step, cap) + kFixed
+  static constexpr int kFixed = 64;
+  __device__ __forceinline__ Work(const dconv_cache_attend_shape &sh, int G, const Rows &s, int most) {
+    rows = s.n * G;
+    tiles = 0;
+    base = cap = step = 0;
+    if (s.n <= 0 || s.n > most || (rows <= kFewRows) != FEW) return;
+    tiles = FEW ? 1 : (rows + kTileRows - 1) / kTileRows;
+    step = FEW ? 0 : max(kTileRows / G, 1);
+    const int i0 = s.start(), i1 = i0 + (FEW ? s.n : min(s.n, (int)step)) - 1;
+    cap = s.len;
+    if (sh.left >= 0)
+      cap = min(cap, (int64_t)sh.left + max(sh.right, 0) + 1 + (sh.right < 0 ? s.len : step + s.n * FEW) + sh.sinks);
+    if (i1 >= 0) {
+      const KeySpan a = keys_seen(sh, s.len, max(i0, 0)), b = keys_seen(sh, s.len, i1);
+      base = min((int64_t)a.first + max(b.hi - a.lo, 0), cap);
+    }
+  }
+  __device__ __forceinline__ int64_t of(int i) const { return min(base + i * step, cap) + kFixed; }
+  // Work of the tiles before i.
+  __device__ __forceinline__ int64_t before(int64_t i) const {
+    const int64_t rising = step > 0 ? min(i, (cap - base) / step + 1) : i;
+    return i * kFixed + rising * base + step * (rising * (rising - 1) / 2) + (i - rising) * cap;
+  }
+  // The tile that holds point z < before(tiles).
+  __device__ __forceinline__ int at(int64_t z) const {
+    int lo = 0, hi = tiles;
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (before(mid) <= z) lo = mid;
+      else hi = mid;
+    }
+    return lo;
+  }
+};
+
+__device__ __forceinline__ int64_t uniform64(int64_t x) {
+  return (int64_t)uniform((int)(x >> 32)) << 32 | (uint32_t)uniform((int)x);
+}
+
+// A workgroup's range of the line: it begins `at` work into sequence b.
+struct Range {
+  int id, b;
+  int64_t at, begin, end, share;
+};
+struct RangeScratch {
+  int64_t wave[4], at;
+  int b;
+};
+template <bool FEW, int NT>
+__device__ __forceinline__ Range find_range(const dconv_cache &c, const dconv_cache_attend_shape &sh, const Batch &t,
+                                            const CachePtrs &p, const CacheTile &ct, int most, RangeScratch &lds) {
+  const int tid = threadIdx.x, G = sh.Hq / c.Hkv;
+  const int per = (t.B + NT - 1) / NT, b0 = min(tid * per, t.B), b1 = min(b0 + per, t.B);
+  auto work = [&](int b) {
+    const Work<FEW> w(sh, G, rows_of(t, p, b), most);
+    return w.tiles > 0 ? w.before(w.tiles) * c.Hkv : (int64_t)0;
+  };
+  int64_t mine = 0;
+  for (int b = b0; b < b1; ++b) mine += work(b);
+  int64_t upto = mine;   // of the wave's lanes up to this one
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int64_t x = from_lane(upto, (int)(tid & 63) - d);
+    if ((tid & 63) >= d) upto += x;
+  }
+  if ((tid & 63) == 63) lds.wave[tid >> 6] = upto;
+  if (tid == 0) lds.b = t.B;
+  __syncthreads();
+  int64_t total = 0;
+#pragma unroll
+  for (int w = 0; w < NT / 64; ++w) {
+    if (w < (tid >> 6)) upto += lds.wave[w];
+    total += lds.wave[w];
+  }
+  Range r;
+  r.id = xcd_remap(blockIdx.x, ct.groups);
+  r.share = max((total + ct.groups - 1) / ct.groups, (int64_t)ct.least);
+  r.begin = r.id * r.share;
+  r.end = min(r.begin + r.share, total);
+  int64_t from = upto - mine;
+  if (r.begin < total && from <= r.begin && r.begin < upto) {
+    int b = b0;
+    for (;; ++b) {
+      const int64_t x = work(b);
+      if (r.begin < from + x || b + 1 >= b1) break;
+      from += x;
+    }
+    lds.b = b;
+    lds.at = r.begin - from;
+  }
+  __syncthreads();
+  r.b = uniform(lds.b);
+  r.at = r.b < t.B ? uniform64(lds.at) : 0;
+  r.share = uniform64(r.share);
+  r.begin = uniform64(r.begin);
+  r.end = uniform64(r.end);
+  return r;
+}
+
+// A value that the compiler computes again where it is used: what a loop over
+// segments would otherwise carry in registers (masks of a head's end, addresses in
+// LDS) does not fit them.
+__device__ __forceinline__ int again_scalar(int x) {
+  asm volatile("" : "+s"(x));
+  return x;
+}
+__device__ __forceinline__ int again_vector(int x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+
+// A segment of an item: from `pos` to `end` of its work.
+struct Segment {
+  int b, hk, tile;
+  Rows s;
+  int64_t pos, end, work, item;   // item: where the item begins on the line
+};
+
+// Steps that lie before point pos of an item with `steps` of them.  (Cuts near an
+// end go to it: a sliver costs as much as the constant.)
+__device__ __forceinline__ int cut(int64_t pos, int64_t work, int steps, int64_t share) {
+  if (pos < work && pos <= share / 8) return 0;
+  if (work - pos <= share / 8) return steps;
+  return (int)(pos * steps / work);
+}
+
+template <bool FEW, class F>
+__device__ __forceinline__ void for_segments(const dconv_cache &c, const dconv_cache_attend_shape &sh, const Batch &t,
+                                             const CachePtrs &p, const Range &r, int most, F f) {
+  const int G = sh.Hq / c.Hkv;
+  int64_t x = r.begin, at = r.at;
+  for (int b = r.b; b < t.B && x < r.end; ++b) {
+    Rows s = rows_of(t, p, b);
+    s = {uniform(s.row), uniform(s.n), uniform(s.len)};
+    const Work<FEW> w(sh, G, s, most);
+    if (w.tiles == 0) continue;
+    const int64_t head = w.before(w.tiles);
+    int hk = 0, tile = 0;
+    if (at > 0) {
+      hk = (int)(at / head);
+      at -= hk * head;
+      tile = w.at(at);
+      at -= w.before(tile);
+    }
+    for (; hk < c.Hkv && x < r.end; ++hk, tile = 0)
+      for (; tile < w.tiles && x < r.end; ++tile) {
+        Segment g = {b, uniform(hk), uniform(tile), s, at, 0, w.of(tile), x - at};
+        g.end = min(g.work, at + (r.end - x));
+        f(g);
+        x += g.end - at;
+        at = 0;
+      }
+  }
+}
+
+// Parts of R rows: sums, bases and totals.
+template <int R, int DP>
+constexpr int cache_part() { return R * (DP + 2); }
+
+// ---------------------------------------------------------------------------
+// 128 rows: four waves of 32 share tiles of keys
+// ---------------------------------------------------------------------------
+template <class T, int DP, int FORMAT>
+__global__ __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1) void cache_tiles(const dconv_cache c,
+                                                                                 const dconv_cache_attend_shape sh,
+                                                                                 const Batch t, const CacheAttendPtrs p,
+                                                                                 const CacheTile ct) {
+  constexpr int BN = forward_keys<T>(DP), KS = DP / 16, DT = DP / 32;
+  typedef typename Mma<T>::Frag Frag;
+  __shared__ __align__(16) T buf0[2 * BN * DP];
+  __shared__ __align__(16) T buf1[2 * BN * DP];
+  __shared__ RangeScratch scratch;
+  DCONV_POISON(poison_lds(buf0, 2 * BN * DP); poison_lds(buf1, 2 * BN * DP));
+  const int wave = uniform(threadIdx.x >> 6), G = sh.Hq / c.Hkv;
+  const int most = sh.max_rows > 0 ? sh.max_rows : t.N;
+  const Range range = find_range<false, 256>(c, sh, t, p.cache, ct, most, scratch);
+  CacheJoin join = {0, 0, 0, 0, 0, 0};
+
+  for_segments<false>(c, sh, t, p.cache, range, most, [&](const Segment &g) {
+    const int lane = again_vector(threadIdx.x & 63), D = again_scalar(c.D);
+    const int rows = g.s.n * G, r0 = g.tile * kTileRows, start = g.s.start();
+    const KeyRange<BN> keys(sh, g.s.len, start + r0 / G, start + (min(r0 + kTileRows, rows) - 1) / G);
+    const int u0 = uniform(cut(g.pos, g.work, keys.n, range.share)), u1 = uniform(cut(g.end, g.work, keys.n, range.share));
+    // nothing of it, and no part of it: all lies before, or after
+    if (u0 == u1 && (keys.n == 0 ? g.pos > 0 : u0 == 0)) return;
+    const bool complete = u0 == 0 && u1 == keys.n;
+
+    const int r = r0 + 32 * wave + (lane & 31), rr = min(r, rows - 1), row = g.s.row + rr / G, h = g.hk * G + rr % G;
+    const KeySpan span = keys_seen(sh, g.s.len, start + rr / G);
+    const RowKeys see = {span.lo, span.none() ? 0 : span.hi, span.none()};
+    // the wave's keys: none outside [from, to) but for the first ones, all seen by
+    // all rows inside [all_from, all_to)
+    int from = see.lo, to = see.hi, all_from = see.lo, all_to = see.hi;
+#pragma unroll
+    for (int x = 16; x > 0; x >>= 1) {
+      from = min(from, __shfl_xor(from, x));
+      to = max(to, __shfl_xor(to, x));
+      all_from = max(all_from, __shfl_xor(all_from, x));
+      all_to = min(all_to, __shfl_xor(all_to, x));
+    }
+    from = uniform(from), to = uniform(to), all_from = uniform(all_from), all_to = uniform(all_to);
+    if (r0 + 32 * wave >= rows) to = 0, from = 0x7fffffff;   // a wave without rows sees nothing
+    const bool idle = r0 + 32 * wave >= rows;
+
+    Frag q[KS];
+    const T *qrow = static_cast<const T *>(p.q) + row * sh.q_stride[0] + h * sh.q_stride[1];
+#pragma unroll
+    for (int k = 0; k < KS; ++k) q[k] = load_frag(qrow, 16 * k + 8 * (lane >> 5), D, ct.direct, ct.sign);
+
+    const Finder<T, FORMAT, BN> finder = {p.cache.table + g.b * t.table_stride, t.page, t.pages};
+    const int64_t es = Finder<T, FORMAT, BN>::kBytes;
+    const char *kb = static_cast<const char *>(p.cache.k) + g.hk * c.k_stride[2] * es;
+    const char *vb = static_cast<const char *>(p.cache.v) + g.hk * c.v_stride[2] * es;
+    Softmax<T, DP> soft;
+    soft.clear();
+    auto step = [&](const T *buf, int j0, uint64_t gone) {
+      auto unseen = [&](int v0, int N) { return idle || v0 >= to || (v0 + N <= from && v0 >= sh.sinks); };
+      auto masked = [&](int v0, int N) {
+        return gone != 0 || !(v0 + N <= all_to && (v0 >= all_from || v0 + N <= sh.sinks));
+      };
+      if constexpr (BN == 64 && sizeof(T) == 2) {
+        if (!unseen(j0, BN))
+          soft.add_two(buf, buf + BN * DP, q, j0, see, sh.sinks, ct.scale2, masked(j0, BN), lane, gone);
+      } else {
+#pragma unroll
+        for (int k = 0; k < BN; k += 32)
+          if (!unseen(j0 + k, 32))
+            soft.add(buf + k * DP, buf + (BN + k) * DP, q, j0 + k, see, sh.sinks, ct.scale2, masked(j0 + k, 32), lane,
+                     (uint32_t)(gone >> k));
+      }
+    };
+    __syncthreads();   // the segment before is through with the buffers
+    if (u0 < u1) {
+      Asked asked = finder.ask(keys, keys.start(u0));
+      if constexpr (FORMAT == DCONV_CACHE_PLAIN) {
+        PlainTiles<T, DP, BN, 4> kt, vt;
+        kt.init(D, c.k_stride[1], wave, lane);
+        vt.init(D, c.v_stride[1], wave, lane);
+        const bool near = ct.near && t.page.d % PlainTiles<T, DP, BN, 4>::kRows == 0;
+        // stages tile u and asks for the one after it
+        auto stage = [&](T *buf, int u) {
+          const Found f = finder.find(c, asked);
+          const bool close = near && keys.whole(keys.start(u));
+          kt.stage(buf, kb, f.k, close, ct.pieces, D, wave, lane);
+          vt.stage(buf + BN * DP, vb, f.v, close, ct.pieces, D, wave, lane);
+          if (u + 1 < u1) asked = finder.ask(keys, keys.start(u + 1));
+          return f.gone;
+        };
+        auto arrived = [&]() {
+          landed<0>();
+          __syncthreads();
+        };
+        uint64_t gone0 = stage(buf0, u0), gone1 = 0;
+        for (int u = u0; u < u1; u += 2) {
+          arrived();
+          if (u + 1 < u1) gone1 = stage(buf1, u + 1);
+          step(buf0, keys.start(u), gone0);
+          if (u + 1 >= u1) break;
+          arrived();
+          if (u + 2 < u1) gone0 = stage(buf0, u + 2);
+          step(buf1, keys.start(u + 1), gone1);
+        }
+      } else {
+        const uint8_t *ksb = p.cache.k_scale + g.hk * c.k_scale_stride[2], *vsb = p.cache.v_scale + g.hk * c.v_scale_stride[2];
+        CodeTiles<T, DP, BN, 256, FORMAT> codes;
+        uint64_t next = 0;
+        auto load = [&](int u) {
+          const Found f = finder.find(c, asked);
+          codes.load(kb, vb, ksb, vsb, f, D, threadIdx.x);
+          next = f.gone;
+          if (u + 1 < u1) asked = finder.ask(keys, keys.start(u + 1));
+        };
+        load(u0);
+        codes.store(buf0, buf0 + BN * DP, threadIdx.x);
+        uint64_t gone = next;
+        if (u0 + 1 < u1) load(u0 + 1);
+        __syncthreads();
+        for (int u = u0; u < u1; ++u) {
+          T *now = (u - u0) & 1 ? buf1 : buf0, *then = (u - u0) & 1 ? buf0 : buf1;
+          step(now, keys.start(u), gone);
+          if (u + 1 >= u1) break;
+          codes.store(then, then + BN * DP, threadIdx.x);
+          gone = next;
+          if (u + 2 < u1) load(u + 2);
+          __syncthreads();
+        }
+      }
+    }
+
+    const float l = half_sum(soft.l);
+    if (!complete) {
+      float *part = ct.partial + ((int64_t)range.id * 2 + (u0 == 0)) * cache_part<kTileRows, DP>();
+      const int x = 32 * wave + (lane & 31);
+#pragma unroll
+      for (int k = 0; k < DT; ++k)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4) {
+          const float y[4] = {soft.o[k][i], soft.o[k][i + 1], soft.o[k][i + 2], soft.o[k][i + 3]};
+          __builtin_memcpy(__builtin_assume_aligned(part + x * DP + 32 * k + acc_row(i, lane >> 5), 16), y, 16);
+        }
+      if (lane < 32) {
+        part[kTileRows * DP + x] = soft.m;
+        part[kTileRows * (DP + 1) + x] = l;
+      }
+      if (u0 == 0)
+        join = {(int)((g.item + g.work - 1) / range.share) - range.id + 1, range.id, g.b, g.hk, r0,
+                min(kTileRows, rows - r0)};
+      return;
+    }
+    const float inv = see.none ? 0.0f : 1.0f / l;
+    bool bad = false;
+#pragma unroll
+    for (int k = 0; k < DT; ++k)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        soft.o[k][i] = see.none ? 0.0f : soft.o[k][i] * inv;
+        bad |= 32 * k + acc_row(i, lane >> 5) < D && !(fabsf(soft.o[k][i]) < INFINITY);
+      }
+    const unsigned long long any = __ballot(bad && r < rows);
+    const unsigned redo = kSumAgain ? (unsigned)(any | (any >> 32)) : 0u;
+    if (r < rows && !(redo >> (lane & 31) & 1)) {
+      T *o = static_cast<T *>(p.out) + row * sh.out_stride[0] + h * sh.out_stride[1];
+#pragma unroll
+      for (int k = 0; k < DT; ++k)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4) {
+          const int d = 32 * k + acc_row(i, lane >> 5);
+          T x[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x[e] = from_f32<T>(soft.o[k][i + e]);
+          if (ct.direct && d + 4 <= D) {
+            __builtin_memcpy(__builtin_assume_aligned(o + d, 4), x, sizeof(x));
+          } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (d + e < D) o[d + e] = x[e];
+          }
+        }
+      if (p.lse && lane < 32) p.lse[(int64_t)row * sh.Hq + h] = see.none ? -INFINITY : log_sum(soft.m, l);
+    }
+    // A row with a result that is not finite is taken again by the plain form, which
+    // reads seen keys and values only: a zero probability times an infinity or NaN
+    // that the row does not see has made a NaN here (or it sees no page).
+    for (unsigned again = redo; again; again &= again - 1) {
+      const int x = r0 + 32 * wave + __ffs(again) - 1;
+      cache_attend_row<T, FORMAT>(c, sh, t, p, g.b, g.s, g.s.row + x / G, g.hk * G + x % G);
+    }
+  });
+  if (threadIdx.x == 0) ct.joins[range.id] = join;
+}
+
+// ---------------------------------------------------------------------------
+// Up to 32 rows: each wave takes tiles of 32 keys by itself
+// ---------------------------------------------------------------------------
+template <class T, int DP, int FORMAT>
+__global__ __launch_bounds__(64 * split_waves<T>(DP), split_waves<T>(DP) == 4 ? 2 : 1) void cache_few(
+    const dconv_cache c, const dconv_cache_attend_shape sh, const Batch t, const CacheAttendPtrs p,
+    const CacheTile ct) {
+  constexpr int KS = DP / 16, DT = DP / 32, BN = 32, kTile = BN * DP, W = split_waves<T>(DP);
+  typedef typename Mma<T>::Frag Frag;
+  __shared__ __align__(16) T kbuf[W * kTile];
+  __shared__ __align__(16) T vbuf[W * kTile];
+  __shared__ float ml[W][64];
+  __shared__ unsigned again;
+  __shared__ RangeScratch scratch;
+  DCONV_POISON(poison_lds(kbuf, W * kTile); poison_lds(vbuf, W * kTile));
+  const int wave = uniform(threadIdx.x >> 6), G = sh.Hq / c.Hkv;
+  const int most = sh.max_rows > 0 ? sh.max_rows : t.N;
+  const Range range = find_range<true, 64 * W>(c, sh, t, p.cache, ct, most, scratch);
+  CacheJoin join = {0, 0, 0, 0, 0, 0};
+
+  for_segments<true>(c, sh, t, p.cache, range, most, [&](const Segment &g) {
+    const int lane = again_vector(threadIdx.x & 63), D = again_scalar(c.D);
+    const int rows = g.s.n * G, start = g.s.start();
+    const KeyRange<BN> keys(sh, g.s.len, start, start + g.s.n - 1);
+    const int steps = (keys.n + W - 1) / W;
+    const int u0 = uniform(cut(g.pos, g.work, steps, range.share)), u1 = uniform(cut(g.end, g.work, steps, range.share));
+    if (u0 == u1 && (steps == 0 ? g.pos > 0 : u0 == 0)) return;
+    const bool complete = u0 == 0 && u1 == steps;
+
+    const int r = lane & 31, rr = min(r, rows - 1), row = g.s.row + rr / G, h = g.hk * G + rr % G;
+    const KeySpan span = keys_seen(sh, g.s.len, start + rr / G);
+    const RowKeys see = {span.lo, span.none() ? 0 : span.hi, span.none()};
+    Frag q[KS];
+    const T *qrow = static_cast<const T *>(p.q) + row * sh.q_stride[0] + h * sh.q_stride[1];
+#pragma unroll
+    for (int k = 0; k < KS; ++k) q[k] = load_frag(qrow, 16 * k + 8 * (lane >> 5), D, ct.direct, ct.sign);
+
+    const Finder<T, FORMAT, BN> finder = {p.cache.table + g.b * t.table_stride, t.page, t.pages};
+    const int64_t es = Finder<T, FORMAT, BN>::kBytes;
+    const char *kb = static_cast<const char *>(p.cache.k) + g.hk * c.k_stride[2] * es;
+    const char *vb = static_cast<const char *>(p.cache.v) + g.hk * c.v_stride[2] * es;
+    Softmax<T, DP> soft;
+    soft.clear();
+    T *kt = kbuf + wave * kTile, *vt = vbuf + wave * kTile;
+    // this wave's tiles: u0 W + wave, and every W-th from there
+    const int end = min(u1 * W, keys.n);
+    int u = u0 * W + wave;
+    if (u < end) {
+      Asked asked = finder.ask(keys, keys.start(u));
+      if constexpr (FORMAT == DCONV_CACHE_PLAIN) {
+        typedef PlainTiles<T, DP, BN, 1> Tiles;
+        Tiles ck, cv;
+        ck.init(D, c.k_stride[1], 0, lane);
+        cv.init(D, c.v_stride[1], 0, lane);
+        const bool near = ct.near && t.page.d % Tiles::kRows == 0;
+        Found f = finder.find(c, asked);
+        bool close = near && keys.whole(keys.start(u));
+        ck.stage(kt, kb, f.k, close, ct.pieces, D, 0, lane);
+        if (u + W < end) asked = finder.ask(keys, keys.start(u + W));
+        cv.stage(vt, vb, f.v, close, ct.pieces, D, 0, lane);
+        for (; u < end; u += W) {
+          const int j0 = keys.start(u);
+          const uint32_t gone = (uint32_t)f.gone;
+          landed<Tiles::C::kCopies>();   // the values may still be on their way
+          f32x16 s = soft.scores(kt, 0, q, lane);
+          landed<Tiles::C::kCopies>();
+          if (u + W < end) {
+            f = finder.find(c, asked);
+            close = near && keys.whole(keys.start(u + W));
+            ck.stage(kt, kb, f.k, close, ct.pieces, D, 0, lane);
+          }
+          soft.mask(s, j0, see, sh.sinks, lane, gone);
+          soft.follow(s, ct.scale2, [] {});
+          Frag w[2];
+          soft.probabilities(s, ct.scale2, w);
+          if (u + W < end) landed<Tiles::C::kCopies>();
+          else landed<0>();
+          soft.values(vt, 0, w, lane);
+          if (u + W < end) {
+            if (u + 2 * W < end) asked = finder.ask(keys, keys.start(u + 2 * W));
+            landed<63>();
+            cv.stage(vt, vb, f.v, close, ct.pieces, D, 0, lane);
+          }
+        }
+      } else {
+        const uint8_t *ksb = p.cache.k_scale + g.hk * c.k_scale_stride[2], *vsb = p.cache.v_scale + g.hk * c.v_scale_stride[2];
+        CodeTiles<T, DP, BN, 64, FORMAT> codes;
+        Found f = finder.find(c, asked);
+        if (u + W < end) asked = finder.ask(keys, keys.start(u + W));
+        codes.load(kb, vb, ksb, vsb, f, D, lane);
+        for (; u < end; u += W) {
+          codes.store(kt, vt, lane);
+          const uint32_t gone = (uint32_t)f.gone;
+          if (u + W < end) {
+            f = finder.find(c, asked);
+            if (u + 2 * W < end) asked = finder.ask(keys, keys.start(u + 2 * W));
+            codes.load(kb, vb, ksb, vsb, f, D, lane);
+          }
+          soft.add(kt, vt, q, keys.start(u), see, sh.sinks, ct.scale2, true, lane, gone);
+        }
+      }
+    }
+
+    // the waves' sums, on the largest of their bases; wave k % W adds columns 32 k ..
+    const float lw = half_sum(soft.l);
+    if (threadIdx.x == 0) again = 0;
+    if (lane < 32) {
+      ml[wave][lane] = soft.m;
+      ml[wave][32 + lane] = lw;
+    }
+    __syncthreads();   // (and every wave is through with its tiles)
+    float m = -INFINITY, l = 0.0f;
+#pragma unroll
+    for (int w = 0; w < W; ++w) m = fmaxf(m, ml[w][r]);
+    const float base = m == -INFINITY ? 0.0f : m;
+#pragma unroll
+    for (int w = 0; w < W; ++w) l += exp2f(ml[w][r] - base) * ml[w][32 + r];
+    const float mine = exp2f(soft.m - base);
+    constexpr int kSlots = W * kTile * (int)sizeof(T) / 4096;   // of 16 registers, in each buffer
+    auto slot = [&](int k, int w) {   // of wave w's columns 32 k .., w not their owner
+      const int i = k * (W - 1) + (w < k % W ? w : w - 1);
+      return reinterpret_cast<float *>(i < kSlots ? kbuf : vbuf) + (i < kSlots ? i : i - kSlots) * 1024;
+    };
+    static_assert(DT * (W - 1) <= 2 * kSlots, "the waves' sums fit the buffers");
+#pragma unroll
+    for (int k = 0; k < DT; ++k) {
+      soft.o[k] *= mine;
+      if (k % W == wave) continue;
+      float *to = slot(k, wave) + lane;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) to[64 * i] = soft.o[k][i];
+    }
+    __syncthreads();
+    float *part = ct.partial + ((int64_t)range.id * 2 + (u0 == 0)) * cache_part<kFewRows, DP>();
+    const float inv = see.none ? 0.0f : 1.0f / l;
+    bool bad = false;
+    T *o = static_cast<T *>(p.out) + row * sh.out_stride[0] + h * sh.out_stride[1];
+#pragma unroll
+    for (int k = 0; k < DT; ++k) {
+      if (k % W != wave) continue;
+#pragma unroll
+      for (int w = 0; w < W; ++w) {   // (this wave's own stands where it stands in the order of all)
+        if (w == wave) continue;
+        const float *x = slot(k, w) + lane;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) soft.o[k][i] += x[64 * i];
+      }
+#pragma unroll
+      for (int i = 0; i < 16; i += 4) {
+        const int d = 32 * k + acc_row(i, lane >> 5);
+        float y[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[e] = soft.o[k][i + e];
+        if (!complete) {
+          __builtin_memcpy(__builtin_assume_aligned(part + r * DP + d, 16), y, 16);
+          continue;
+        }
+        T x[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          y[e] = see.none ? 0.0f : y[e] * inv;
+          bad |= d + e < D && !(fabsf(y[e]) < INFINITY);
+          x[e] = from_f32<T>(y[e]);
+        }
+        if (r >= rows) continue;
+        if (ct.direct && d + 4 <= D) {
+          __builtin_memcpy(__builtin_assume_aligned(o + d, 4), x, sizeof(x));
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (d + e < D) o[d + e] = x[e];
+        }
+      }
+    }
+    if (!complete) {
+      if (wave == 0 && lane < 32) {
+        part[kFewRows * DP + lane] = m;
+        part[kFewRows * (DP + 1) + lane] = l;
+      }
+      if (u0 == 0)
+        join = {(int)((g.item + g.work - 1) / range.share) - range.id + 1, range.id, g.b, g.hk, 0, rows};
+      __syncthreads();
+      return;
+    }
+    if (p.lse && wave == 0 && lane < rows)
+      p.lse[(int64_t)row * sh.Hq + h] = see.none ? -INFINITY : log_sum(m, l);
+    const unsigned long long any = __ballot(bad && r < rows);
+    if (kSumAgain && any && lane == 0) atomicOr(&again, (unsigned)(any | (any >> 32)));
+    __syncthreads();
+    // (see cache_tiles; the stores above come first, a row's by this workgroup alone)
+    const unsigned redo = again;
+    for (int x = wave; x < rows; x += W)
+      if (redo >> x & 1) cache_attend_row<T, FORMAT>(c, sh, t, p, g.b, g.s, g.s.row + x / G, g.hk * G + x % G);
+    __syncthreads();
+  });
+  if (threadIdx.x == 0) ct.joins[range.id] = join;
+}
+
+// ---------------------------------------------------------------------------
+// Parts joined: a wave per row
+// ---------------------------------------------------------------------------
+template <class T, int DP, int FORMAT, int R>
+__device__ __forceinline__ void join_rows(const dconv_cache &c, const dconv_cache_attend_shape &sh, const Batch &t,
+                                          const CacheAttendPtrs &p, const CacheTile &ct, int id) {
+  const CacheJoin j = ct.joins[id];
+  if (j.parts == 0) return;
+  const int lane = threadIdx.x & 63, G = sh.Hq / c.Hkv;
+  const Rows s = rows_of(t, p.cache, j.b);
+  // the first part is its workgroup's second one
+  auto part = [&](int i) { return ct.partial + ((int64_t)(j.first + i) * 2 + (i == 0)) * cache_part<R, DP>(); };
+  for (int x = blockIdx.y * 4 + (threadIdx.x >> 6); x < j.rows; x += 4 * gridDim.y) {
+    const int r = j.r0 + x, row = s.row + r / G, h = j.hk * G + r % G;
+    const bool none = keys_seen(sh, s.len, s.start() + r / G).none();
+    // bases and totals, a part per lane
+    float m = -INFINITY;
+    for (int i = lane; i < j.parts; i += 64) m = fmaxf(m, part(i)[R * DP + x]);
+    m = lanes_max<64>(m);
+    const float base = m == -INFINITY ? 0.0f : m;
+    float l = 0.0f, acc[kLaneParts] = {};
+    for (int i0 = 0; i0 < j.parts; i0 += 64) {
+      const int i = i0 + lane;
+      float w = 0.0f;
+      if (i < j.parts) w = exp2f(part(i)[R * DP + x] - base);
+      if (w != 0.0f) l += w * part(i)[R * (DP + 1) + x];
+#pragma unroll 4
+      for (int k = 0; k < 64 && i0 + k < j.parts; ++k) {
+        const float f = __shfl(w, k);
+        const float *y = part(i0 + k) + x * DP;
+#pragma unroll
+        for (int e = 0; e < (DP + 63) / 64; ++e)
+          if (lane + 64 * e < c.D) acc[e] = fmaf(f, y[lane + 64 * e], acc[e]);
+      }
+    }
+    l = lanes_sum<64>(l);
+    bool bad = false;
+#pragma unroll
+    for (int e = 0; e < (DP + 63) / 64; ++e) {
+      acc[e] = none ? 0.0f : acc[e] / l;
+      bad |= lane + 64 * e < c.D && !(fabsf(acc[e]) < INFINITY);
+    }
+    if (kSumAgain && __any(bad)) {
+      cache_attend_row<T, FORMAT>(c, sh, t, p, j.b, s, row, h);
+      continue;
+    }
+    T *o = static_cast<T *>(p.out) + row * sh.out_stride[0] + h * sh.out_stride[1];
+#pragma unroll
+    for (int e = 0; e < (DP + 63) / 64; ++e)
+      if (lane + 64 * e < c.D) o[lane + 64 * e] = from_f32<T>(acc[e]);
+    if (p.lse && lane == 0) p.lse[(int64_t)row * sh.Hq + h] = none ? -INFINITY : log_sum(m, l);
+  }
+}
+
+// The workgroups of both kernels, those of few rows first.
+template <class T, int DP, int FORMAT>
+__global__ __launch_bounds__(256) void cache_join(const dconv_cache c, const dconv_cache_attend_shape sh, const Batch t,
+                                                  const CacheAttendPtrs p, const CacheTile few, const CacheTile tiles) {
+  if ((int)blockIdx.x < few.groups) join_rows<T, DP, FORMAT, kFewRows>(c, sh, t, p, few, blockIdx.x);
+  else join_rows<T, DP, FORMAT, kTileRows>(c, sh, t, p, tiles, blockIdx.x - few.groups);
+}
+
+template <class T, int FORMAT>
+void launch_cache_attend(const dconv_cache &c, const dconv_cache_attend_shape &sh, const Batch &t,
+                         const CacheAttendPtrs &p, const CachePlan &plan, char *workspace, hipStream_t s) {
+  const AttendTile scale = [&] {
+    dconv_attend_shape a = {};
+    a.scale = sh.scale;
+    return attend_tile(a, false, false);
+  }();
+  CacheTile few = {scale.scale2, scale.sign, plan.direct, plan.pieces, plan.near, plan.few, plan.few_least, nullptr, nullptr};
+  CacheTile tiles = few;
+  tiles.groups = plan.tiles;
+  tiles.least = plan.tiles_least;
+  few.joins = reinterpret_cast<CacheJoin *>(workspace);
+  tiles.joins = few.joins + plan.few;
+  few.partial = reinterpret_cast<float *>(workspace + plan.joins_bytes);
+  by_width(plan.dp, [&](auto dp) {
+    constexpr int DP = decltype(dp)::value;
+    tiles.partial = few.partial + (int64_t)plan.few * 2 * cache_part<kFewRows, DP>();
+    if (plan.few > 0)
+      hipLaunchKernelGGL((cache_few<T, DP, FORMAT>), dim3(plan.few), dim3(64 * split_waves<T>(DP)), 0, s, c, sh, t, p, few);
+    if (plan.tiles > 0)
+      hipLaunchKernelGGL((cache_tiles<T, DP, FORMAT>), dim3(plan.tiles), dim3(256), 0, s, c, sh, t, p, tiles);
+    hipLaunchKernelGGL((cache_join<T, DP, FORMAT>), dim3(plan.few + plan.tiles, plan.tiles > 0 ? 8 : 2), dim3(256), 0, s,
+                       c, sh, t, p, few, tiles);
+  });
+}
+
+}  // namespace dconv
