@@ -18,6 +18,23 @@ struct CacheTile {
   CacheJoin *joins;     // one of each workgroup's
 };
 
+// A kernel's one argument.  What it holds is read from the argument's own memory
+// where it is used (fresh), as a hundred scalars that stay in registers through the
+// loops over segments would push out those of the loops over keys.
+struct CacheCall {
+  dconv_cache c;
+  dconv_cache_attend_shape sh;
+  Batch t;
+  CacheAttendPtrs p;
+  CacheTile ct;
+};
+__device__ __forceinline__ const CacheCall &fresh() {
+  typedef const __attribute__((address_space(4))) CacheCall *Arg;
+  Arg a = (Arg)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(a));
+  return *(const CacheCall *)a;
+}
+
 // ---------------------------------------------------------------------------
 // The keys of a tile of rows
 // ---------------------------------------------------------------------------
@@ -146,26 +163,31 @@ struct PlainTiles {
 // ---------------------------------------------------------------------------
 // Tiles of 8 and 4 bits: read into registers a tile ahead, converted into LDS
 // ---------------------------------------------------------------------------
-// A thread takes blocks of 32 neighbours with their scale, of keys and values both.
-template <class T, int DP, int BN, int NT, int FORMAT>
+// A thread takes blocks of 32 neighbours with their scale: sixteen lanes the same
+// block of sixteen rows (whose chunks lie on different banks of LDS), the next sixteen
+// the next block of them.  TENSORS: keys and values, or values alone.
+template <int WORDS>
+struct __attribute__((packed, aligned(1))) RawCodes {
+  uint32_t w[WORDS];
+};
+template <class T, int DP, int BN, int NT, int FORMAT, int TENSORS>
 struct CodeTiles {
-  static constexpr int kBlocks = DP / kBlock, kTensor = BN * kBlocks, kAll = 2 * kTensor;
+  static constexpr int kBlocks = DP / kBlock, kTensor = BN * kBlocks, kAll = TENSORS * kTensor;
   static constexpr int kPer = (kAll + NT - 1) / NT, kWords = kBlock / codes_per_word<FORMAT>();
-  struct __attribute__((packed, aligned(1))) Raw {
-    uint32_t w[kWords];
-  };
-  Raw raw[kPer];
+  RawCodes<kWords> raw[kPer];
   uint32_t scale[kPer];
 
   static __device__ __forceinline__ bool has(int u) { return kAll % NT == 0 || u < kAll; }
+  static __device__ __forceinline__ int row_of(int u) { return (u & 15) + u % kTensor / (16 * kBlocks) * 16; }
+  static __device__ __forceinline__ int block_of(int u) { return (u >> 4) % kBlocks; }
   __device__ __forceinline__ void load(const char *k, const char *v, const uint8_t *ks, const uint8_t *vs,
                                        const Found &f, int D, int thread) {
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
-      const int u = i * NT + thread, x = u % kTensor, row = x / kBlocks, blk = x % kBlocks;
+      const int u = i * NT + thread, row = row_of(u), blk = block_of(u);
       int64_t at, sat;
-      bool value = u >= kTensor;
-      if constexpr (kTensor % 64 == 0) {
+      bool value = TENSORS == 1 || u >= kTensor;
+      if constexpr (TENSORS == 1 || kTensor % 64 == 0) {
         value = uniform(value);   // a wave's are of one tensor
         at = from_lane(value ? f.v : f.k, row);
         sat = from_lane(value ? f.vs : f.ks, row);
@@ -178,7 +200,7 @@ struct CodeTiles {
       raw[i] = {};
       scale[i] = 0;
       if (has(u) && blk * kBlock < D) {
-        raw[i] = *reinterpret_cast<const Raw *>((value ? v : k) + at + blk * (kWords * 4));
+        raw[i] = *reinterpret_cast<const RawCodes<kWords> *>((value ? v : k) + at + blk * (kWords * 4));
         scale[i] = (value ? vs : ks)[sat + blk];
       }
     }
@@ -187,9 +209,9 @@ struct CodeTiles {
   __device__ __forceinline__ void store(T *kt, T *vt, int thread) const {
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
-      const int u = i * NT + thread, x = u % kTensor, row = x / kBlocks, blk = x % kBlocks;
+      const int u = i * NT + thread, row = row_of(u), blk = block_of(u);
       if (!has(u)) break;
-      T *to = u >= kTensor ? vt : kt;
+      T *to = TENSORS == 1 || u >= kTensor ? vt : kt;
       constexpr int kPairs = codes_per_word<FORMAT>() / 2;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
@@ -202,6 +224,193 @@ struct CodeTiles {
         __builtin_memcpy(__builtin_assume_aligned(to + Tile<T, DP>::at(row, 4 * blk + j), 16), &y, sizeof(y));
       }
     }
+  }
+};
+
+// The codes of one key's half row as row operands, straight from memory: the lane of
+// key l % 32 takes elements 32 b + 16 (l / 32) .. + 15 of every block b, and the
+// queries are taken in the same order (order_of), as the inner index has none.
+template <class T, int DP, int FORMAT>
+struct KeyCodes {
+  typedef typename Mma<T>::Frag Frag;
+  static constexpr int kBlocks = DP / kBlock, kWords = 16 / codes_per_word<FORMAT>();
+  RawCodes<kWords> raw[kBlocks];
+  uint32_t scale[kBlocks];
+  static __device__ __forceinline__ int order_of(int k, int half) { return 32 * (k / 2) + 16 * half + 8 * (k & 1); }
+  __device__ __forceinline__ void load(const char *row, const uint8_t *scales, int D, int half) {
+#pragma unroll
+    for (int b = 0; b < kBlocks; ++b) {
+      raw[b] = {};
+      scale[b] = 0;
+      if (b * kBlock < D) {
+        raw[b] = *reinterpret_cast<const RawCodes<kWords> *>(row + (2 * b + half) * (kWords * 4));
+        scale[b] = scales[b];
+      }
+    }
+  }
+  __device__ __forceinline__ Frag frag(int k) const {
+    struct alignas(16) {
+      T x[8];
+    } y;
+    constexpr int kPairs = codes_per_word<FORMAT>() / 2;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      decode_pair<T, FORMAT>(raw[k / 2].w[(4 * (k & 1) + e) / kPairs], (4 * (k & 1) + e) % kPairs,
+                             scale_of(scale[k / 2]), y.x + 2 * e);
+    Frag f;
+    __builtin_memcpy(&f, &y, sizeof(f));
+    return f;
+  }
+};
+
+// ---------------------------------------------------------------------------
+// Operands from LDS
+// ---------------------------------------------------------------------------
+// What Tile::row and Tile::column read, from four numbers of a lane: a chunk's place
+// in its row is an exclusive or with constants, so an address is one instruction
+// (v_xad) from two of them.  Kept as addresses they would take a sixth of the registers.
+template <class T, int DP>
+struct Reader {
+  typedef typename Mma<T>::Frag Frag;
+  static constexpr uint32_t kRow = DP * sizeof(T), kChunk = 8 * sizeof(T);
+  uint32_t rx, rb, cx, cb;
+  __device__ __forceinline__ explicit Reader(int lane) {
+    const int row = lane & 31, half = lane >> 5;
+    rb = row * kRow;
+    rx = (half ^ Tile<T, DP>::swizzle(row)) * kChunk;
+    if constexpr (sizeof(T) == 2) {
+      const int r = 4 * half + ((lane & 15) >> 2);
+      cb = r * kRow + 4 * (lane & 1) * sizeof(T);
+      cx = ((2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ Tile<T, DP>::swizzle(r)) * kChunk;
+    } else {
+      cb = 4 * half * kRow + (lane & 7) * sizeof(T);
+      cx = ((row >> 3) ^ Tile<T, DP>::swizzle(4 * half)) * kChunk;
+    }
+  }
+  // (computed again from here on, not kept)
+  __device__ __forceinline__ void again() { asm volatile("" : "+v"(rx), "+v"(rb), "+v"(cx), "+v"(cb)); }
+  static __device__ __forceinline__ const char *bytes(const T *t) { return reinterpret_cast<const char *>(t); }
+
+  __device__ __forceinline__ Frag row(const T *t, int r0, int k) const {
+    const char *p = bytes(t) + ((rx ^ 2 * k * kChunk) + rb) + r0 * kRow;
+    if constexpr (sizeof(T) == 4) {
+      typedef float f32x4 __attribute__((ext_vector_type(4)));   // (two loads: see Tile::row)
+      const f32x4 a = *reinterpret_cast<const f32x4 *>(p), b = *reinterpret_cast<const f32x4 *>(p + 16);
+      return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+    } else {
+      return *reinterpret_cast<const Frag *>(p);
+    }
+  }
+  __device__ __forceinline__ Frag column(const T *t, int r0, int c) const {
+    Frag f;
+    if constexpr (sizeof(T) == 2) {
+      typedef short s16x4 __attribute__((ext_vector_type(4)));
+      typedef __attribute__((address_space(3))) s16x4 *lds_s16x4;
+      s16x4 v[2];
+#pragma unroll
+      for (int j = 0; j < 2; ++j)   // (rows 8 further: two chunks further, exclusively or)
+        v[j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+            (lds_s16x4)(bytes(t) + ((cx ^ (4 * c ^ 2 * j) * kChunk) + cb) + (r0 + 8 * j) * kRow));
+      __builtin_memcpy(&f, v, 16);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        f[e] = *reinterpret_cast<const T *>(bytes(t) + ((cx ^ (4 * c ^ e % 4) * kChunk) + cb) +
+                                            (r0 + 8 * (e / 4) + e % 4) * kRow);
+    }
+    return f;
+  }
+};
+
+// The running softmax of 32 rows, with operands by a Reader.
+template <class T, int DP>
+struct CacheSoftmax : Softmax<T, DP> {
+  typedef Softmax<T, DP> Base;
+  typedef typename Mma<T>::Frag Frag;
+  static constexpr int KS = Base::KS, DT = Base::DT;
+  using Base::o;
+
+  static __device__ __forceinline__ f32x16 scores(const Reader<T, DP> &rd, const T *ks, int k0, const Frag (&q)[KS]) {
+    f32x16 s = {};
+#pragma unroll
+    for (int k = 0; k < KS; ++k) s = Mma<T>::mac(rd.row(ks, k0, k), q[k], s);
+    return s;
+  }
+  __device__ __forceinline__ void values(const Reader<T, DP> &rd, const T *vs, int k0, const Frag (&w)[2]) {
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+#pragma unroll
+      for (int c = 0; c < DT; ++c) o[c] = Mma<T>::mac(rd.column(vs, k0 + 16 * k, c), w[k], o[c]);
+  }
+  // Adds 32 keys, j0 .., of the tiles ks, vs.
+  __device__ __forceinline__ void add(Reader<T, DP> rd, const T *ks, const T *vs, const Frag (&q)[KS], int j0,
+                                      const RowKeys &see, int sinks, float scale2, bool masked, int lane,
+                                      uint32_t gone) {
+    rd.again();
+    f32x16 s = scores(rd, ks, 0, q);
+    if (masked) Base::mask(s, j0, see, sinks, lane, gone);
+    Base::follow(s, scale2, [] {});
+    Frag w[2];
+    Base::probabilities(s, scale2, w);
+    values(rd, vs, 0, w);
+  }
+  // Adds 64 keys, the matrix and the vector unit at the same time (Softmax::add_two).
+  __device__ __forceinline__ void add_two(Reader<T, DP> rd, const T *ks, const T *vs, const Frag (&q)[KS], int j0,
+                                          const RowKeys &see, int sinks, float scale2, bool masked, int lane,
+                                          uint64_t gone) {
+    const uint32_t gone0 = (uint32_t)gone, gone1 = (uint32_t)(gone >> 32);
+    Frag w0[2], w1[2];
+    rd.again();
+    if constexpr (DP > 96) {
+      f32x16 s0 = scores(rd, ks, 0, q);
+      if (masked) Base::mask(s0, j0, see, sinks, lane, gone0);
+      Base::follow(s0, scale2, [] {});
+      f32x16 s1 = scores(rd, ks, 32, q);
+      Base::probabilities(s0, scale2, w0);
+      asm volatile("" ::"v"(w0[0]), "v"(w0[1]));   // here, not after the next branch
+      if (masked) Base::mask(s1, j0 + 32, see, sinks, lane, gone1);
+      Base::follow(s1, scale2, [&] {
+        values(rd, vs, 0, w0);
+        w0[0] = w0[1] = Frag{};
+      });
+      values(rd, vs, 0, w0);
+      Base::probabilities(s1, scale2, w1);
+      values(rd, vs, 32, w1);
+      return;
+    }
+    Frag kf[KS], vf[2][DT];
+    auto load_keys = [&](int k0) {
+#pragma unroll
+      for (int k = 0; k < KS; ++k) kf[k] = rd.row(ks, k0, k);
+      in_order();
+    };
+    auto load_values = [&](Frag(&f)[DT], int k0) {
+#pragma unroll
+      for (int c = 0; c < DT; ++c) f[c] = rd.column(vs, k0, c);
+      in_order();
+    };
+    load_keys(0);
+    f32x16 s0 = Base::products(kf, q), s1;
+    load_keys(32);
+    if (masked) Base::mask(s0, j0, see, sinks, lane, gone0);
+    Base::follow(s0, scale2, [] {});
+    s1 = Base::products(kf, q);
+    load_values(vf[0], 0);
+    Base::probabilities(s0, scale2, w0);
+    asm volatile("" ::"v"(w0[0]), "v"(w0[1]));
+    if (masked) Base::mask(s1, j0 + 32, see, sinks, lane, gone1);
+    Base::follow(s1, scale2, [&] {
+      values(rd, vs, 0, w0);
+      w0[0] = w0[1] = Frag{};
+    });
+    load_values(vf[1], 16);
+    Base::weigh(vf[0], w0[0]);
+    load_values(vf[0], 32);
+    Base::weigh(vf[1], w0[1]);
+    load_values(vf[1], 48);
+    Base::probabilities(s1, scale2, w1);
+    Base::weigh(vf[0], w1[0]);
+    Base::weigh(vf[1], w1[1]);
   }
 };
 
@@ -259,6 +468,8 @@ __device__ __forceinline__ int64_t uniform64(int64_t x) {
   return (int64_t)uniform((int)(x >> 32)) << 32 | (uint32_t)uniform((int)x);
 }
 
+__device__ __forceinline__ int most_rows(const CacheCall &a) { return a.sh.max_rows > 0 ? a.sh.max_rows : a.t.N; }
+
 // A workgroup's range of the line: it begins `at` work into sequence b.
 struct Range {
   int id, b;
@@ -269,9 +480,12 @@ struct RangeScratch {
   int b;
 };
 template <bool FEW, int NT>
-__device__ __forceinline__ Range find_range(const dconv_cache &c, const dconv_cache_attend_shape &sh, const Batch &t,
-                                            const CachePtrs &p, const CacheTile &ct, int most, RangeScratch &lds) {
-  const int tid = threadIdx.x, G = sh.Hq / c.Hkv;
+__device__ __forceinline__ Range find_range(const CacheCall &a, RangeScratch &lds) {
+  const dconv_cache &c = a.c;
+  const dconv_cache_attend_shape &sh = a.sh;
+  const Batch &t = a.t;
+  const CachePtrs &p = a.p.cache;
+  const int tid = threadIdx.x, G = sh.Hq / c.Hkv, most = most_rows(a);
   const int per = (t.B + NT - 1) / NT, b0 = min(tid * per, t.B), b1 = min(b0 + per, t.B);
   auto work = [&](int b) {
     const Work<FEW> w(sh, G, rows_of(t, p, b), most);
@@ -295,8 +509,8 @@ __device__ __forceinline__ Range find_range(const dconv_cache &c, const dconv_ca
     total += lds.wave[w];
   }
   Range r;
-  r.id = xcd_remap(blockIdx.x, ct.groups);
-  r.share = max((total + ct.groups - 1) / ct.groups, (int64_t)ct.least);
+  r.id = xcd_remap(blockIdx.x, a.ct.groups);
+  r.share = max((total + a.ct.groups - 1) / a.ct.groups, (int64_t)a.ct.least);
   r.begin = r.id * r.share;
   r.end = min(r.begin + r.share, total);
   int64_t from = upto - mine;
@@ -347,14 +561,15 @@ __device__ __forceinline__ int cut(int64_t pos, int64_t work, int steps, int64_t
 }
 
 template <bool FEW, class F>
-__device__ __forceinline__ void for_segments(const dconv_cache &c, const dconv_cache_attend_shape &sh, const Batch &t,
-                                             const CachePtrs &p, const Range &r, int most, F f) {
-  const int G = sh.Hq / c.Hkv;
+__device__ __forceinline__ void for_segments(const Range &r, F f) {
   int64_t x = r.begin, at = r.at;
-  for (int b = r.b; b < t.B && x < r.end; ++b) {
-    Rows s = rows_of(t, p, b);
+  for (int b = r.b; x < r.end; ++b) {
+    const CacheCall &a = fresh();
+    if (b >= a.t.B) break;
+    const int G = a.sh.Hq / a.c.Hkv, heads = a.c.Hkv;
+    Rows s = rows_of(a.t, a.p.cache, b);
     s = {uniform(s.row), uniform(s.n), uniform(s.len)};
-    const Work<FEW> w(sh, G, s, most);
+    const Work<FEW> w(a.sh, G, s, most_rows(a));
     if (w.tiles == 0) continue;
     const int64_t head = w.before(w.tiles);
     int hk = 0, tile = 0;
@@ -364,7 +579,7 @@ __device__ __forceinline__ void for_segments(const dconv_cache &c, const dconv_c
       tile = w.at(at);
       at -= w.before(tile);
     }
-    for (; hk < c.Hkv && x < r.end; ++hk, tile = 0)
+    for (; hk < heads && x < r.end; ++hk, tile = 0)
       for (; tile < w.tiles && x < r.end; ++tile) {
         Segment g = {b, uniform(hk), uniform(tile), s, at, 0, w.of(tile), x - at};
         g.end = min(g.work, at + (r.end - x));
@@ -383,22 +598,26 @@ constexpr int cache_part() { return R * (DP + 2); }
 // 128 rows: four waves of 32 share tiles of keys
 // ---------------------------------------------------------------------------
 template <class T, int DP, int FORMAT>
-__global__ __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1) void cache_tiles(const dconv_cache c,
-                                                                                 const dconv_cache_attend_shape sh,
-                                                                                 const Batch t, const CacheAttendPtrs p,
-                                                                                 const CacheTile ct) {
+__global__ __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1) void cache_tiles(
+    const CacheCall) {
   constexpr int BN = forward_keys<T>(DP), KS = DP / 16, DT = DP / 32;
   typedef typename Mma<T>::Frag Frag;
   __shared__ __align__(16) T buf0[2 * BN * DP];
   __shared__ __align__(16) T buf1[2 * BN * DP];
   __shared__ RangeScratch scratch;
   DCONV_POISON(poison_lds(buf0, 2 * BN * DP); poison_lds(buf1, 2 * BN * DP));
-  const int wave = uniform(threadIdx.x >> 6), G = sh.Hq / c.Hkv;
-  const int most = sh.max_rows > 0 ? sh.max_rows : t.N;
-  const Range range = find_range<false, 256>(c, sh, t, p.cache, ct, most, scratch);
+  const int wave = uniform(threadIdx.x >> 6);
+  const Range range = find_range<false, 256>(fresh(), scratch);
   CacheJoin join = {0, 0, 0, 0, 0, 0};
 
-  for_segments<false>(c, sh, t, p.cache, range, most, [&](const Segment &g) {
+  for_segments<false>(range, [&](const Segment &g) {
+    const CacheCall &a = fresh();
+    const dconv_cache &c = a.c;
+    const dconv_cache_attend_shape &sh = a.sh;
+    const Batch &t = a.t;
+    const CacheAttendPtrs &p = a.p;
+    const CacheTile &ct = a.ct;
+    const int G = sh.Hq / c.Hkv;
     const int lane = again_vector(threadIdx.x & 63), D = again_scalar(c.D);
     const int rows = g.s.n * G, r0 = g.tile * kTileRows, start = g.s.start();
     const KeyRange<BN> keys(sh, g.s.len, start + r0 / G, start + (min(r0 + kTileRows, rows) - 1) / G);
@@ -433,7 +652,8 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1) void cache_tile
     const int64_t es = Finder<T, FORMAT, BN>::kBytes;
     const char *kb = static_cast<const char *>(p.cache.k) + g.hk * c.k_stride[2] * es;
     const char *vb = static_cast<const char *>(p.cache.v) + g.hk * c.v_stride[2] * es;
-    Softmax<T, DP> soft;
+    const Reader<T, DP> rd(lane);
+    CacheSoftmax<T, DP> soft;
     soft.clear();
     auto step = [&](const T *buf, int j0, uint64_t gone) {
       auto unseen = [&](int v0, int N) { return idle || v0 >= to || (v0 + N <= from && v0 >= sh.sinks); };
@@ -442,12 +662,12 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1) void cache_tile
       };
       if constexpr (BN == 64 && sizeof(T) == 2) {
         if (!unseen(j0, BN))
-          soft.add_two(buf, buf + BN * DP, q, j0, see, sh.sinks, ct.scale2, masked(j0, BN), lane, gone);
+          soft.add_two(rd, buf, buf + BN * DP, q, j0, see, sh.sinks, ct.scale2, masked(j0, BN), lane, gone);
       } else {
 #pragma unroll
         for (int k = 0; k < BN; k += 32)
           if (!unseen(j0 + k, 32))
-            soft.add(buf + k * DP, buf + (BN + k) * DP, q, j0 + k, see, sh.sinks, ct.scale2, masked(j0 + k, 32), lane,
+            soft.add(rd, buf + k * DP, buf + (BN + k) * DP, q, j0 + k, see, sh.sinks, ct.scale2, masked(j0 + k, 32), lane,
                      (uint32_t)(gone >> k));
       }
     };
@@ -484,7 +704,7 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1) void cache_tile
         }
       } else {
         const uint8_t *ksb = p.cache.k_scale + g.hk * c.k_scale_stride[2], *vsb = p.cache.v_scale + g.hk * c.v_scale_stride[2];
-        CodeTiles<T, DP, BN, 256, FORMAT> codes;
+        CodeTiles<T, DP, BN, 256, FORMAT, 2> codes;
         uint64_t next = 0;
         auto load = [&](int u) {
           const Found f = finder.find(c, asked);
@@ -565,10 +785,11 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1) void cache_tile
     // that the row does not see has made a NaN here (or it sees no page).
     for (unsigned again = redo; again; again &= again - 1) {
       const int x = r0 + 32 * wave + __ffs(again) - 1;
-      cache_attend_row<T, FORMAT>(c, sh, t, p, g.b, g.s, g.s.row + x / G, g.hk * G + x % G);
+      const CacheCall &f = fresh();
+      cache_attend_row<T, FORMAT>(f.c, f.sh, f.t, f.p, g.b, g.s, g.s.row + x / G, g.hk * G + x % G);
     }
   });
-  if (threadIdx.x == 0) ct.joins[range.id] = join;
+  if (threadIdx.x == 0) fresh().ct.joins[range.id] = join;
 }
 
 // ---------------------------------------------------------------------------
@@ -576,22 +797,28 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1) void cache_tile
 // ---------------------------------------------------------------------------
 template <class T, int DP, int FORMAT>
 __global__ __launch_bounds__(64 * split_waves<T>(DP), split_waves<T>(DP) == 4 ? 2 : 1) void cache_few(
-    const dconv_cache c, const dconv_cache_attend_shape sh, const Batch t, const CacheAttendPtrs p,
-    const CacheTile ct) {
+    const CacheCall) {
   constexpr int KS = DP / 16, DT = DP / 32, BN = 32, kTile = BN * DP, W = split_waves<T>(DP);
   typedef typename Mma<T>::Frag Frag;
+  typedef KeyCodes<T, DP, FORMAT == DCONV_CACHE_PLAIN ? DCONV_CACHE_E4M3 : FORMAT> Codes;
   __shared__ __align__(16) T kbuf[W * kTile];
   __shared__ __align__(16) T vbuf[W * kTile];
   __shared__ float ml[W][64];
   __shared__ unsigned again;
   __shared__ RangeScratch scratch;
   DCONV_POISON(poison_lds(kbuf, W * kTile); poison_lds(vbuf, W * kTile));
-  const int wave = uniform(threadIdx.x >> 6), G = sh.Hq / c.Hkv;
-  const int most = sh.max_rows > 0 ? sh.max_rows : t.N;
-  const Range range = find_range<true, 64 * W>(c, sh, t, p.cache, ct, most, scratch);
+  const int wave = uniform(threadIdx.x >> 6);
+  const Range range = find_range<true, 64 * W>(fresh(), scratch);
   CacheJoin join = {0, 0, 0, 0, 0, 0};
 
-  for_segments<true>(c, sh, t, p.cache, range, most, [&](const Segment &g) {
+  for_segments<true>(range, [&](const Segment &g) {
+    const CacheCall &a = fresh();
+    const dconv_cache &c = a.c;
+    const dconv_cache_attend_shape &sh = a.sh;
+    const Batch &t = a.t;
+    const CacheAttendPtrs &p = a.p;
+    const CacheTile &ct = a.ct;
+    const int G = sh.Hq / c.Hkv;
     const int lane = again_vector(threadIdx.x & 63), D = again_scalar(c.D);
     const int rows = g.s.n * G, start = g.s.start();
     const KeyRange<BN> keys(sh, g.s.len, start, start + g.s.n - 1);
@@ -603,24 +830,43 @@ __global__ __launch_bounds__(64 * split_waves<T>(DP), split_waves<T>(DP) == 4 ? 
     const int r = lane & 31, rr = min(r, rows - 1), row = g.s.row + rr / G, h = g.hk * G + rr % G;
     const KeySpan span = keys_seen(sh, g.s.len, start + rr / G);
     const RowKeys see = {span.lo, span.none() ? 0 : span.hi, span.none()};
+    int all_from = see.lo, all_to = see.hi;   // keys that all rows see
+#pragma unroll
+    for (int x = 16; x > 0; x >>= 1) {
+      all_from = max(all_from, __shfl_xor(all_from, x));
+      all_to = min(all_to, __shfl_xor(all_to, x));
+    }
+    all_from = uniform(all_from), all_to = uniform(all_to);
     Frag q[KS];
     const T *qrow = static_cast<const T *>(p.q) + row * sh.q_stride[0] + h * sh.q_stride[1];
 #pragma unroll
-    for (int k = 0; k < KS; ++k) q[k] = load_frag(qrow, 16 * k + 8 * (lane >> 5), D, ct.direct, ct.sign);
+    for (int k = 0; k < KS; ++k)
+      q[k] = load_frag(qrow, FORMAT == DCONV_CACHE_PLAIN ? 16 * k + 8 * (lane >> 5) : Codes::order_of(k, lane >> 5), D,
+                       ct.direct, ct.sign);
 
     const Finder<T, FORMAT, BN> finder = {p.cache.table + g.b * t.table_stride, t.page, t.pages};
     const int64_t es = Finder<T, FORMAT, BN>::kBytes;
     const char *kb = static_cast<const char *>(p.cache.k) + g.hk * c.k_stride[2] * es;
     const char *vb = static_cast<const char *>(p.cache.v) + g.hk * c.v_stride[2] * es;
-    Softmax<T, DP> soft;
+    const Reader<T, DP> reader(lane);
+    CacheSoftmax<T, DP> soft;
     soft.clear();
     T *kt = kbuf + wave * kTile, *vt = vbuf + wave * kTile;
+    // Scores to probabilities.
+    auto weigh = [&](f32x16 &s, int j0, uint32_t gone, Frag(&w)[2]) {
+      if (gone != 0 || !(j0 + BN <= all_to && (j0 >= all_from || j0 + BN <= sh.sinks)))
+        soft.mask(s, j0, see, sh.sinks, lane, gone);
+      soft.follow(s, ct.scale2, [] {});
+      soft.probabilities(s, ct.scale2, w);
+    };
     // this wave's tiles: u0 W + wave, and every W-th from there
     const int end = min(u1 * W, keys.n);
     int u = u0 * W + wave;
     if (u < end) {
       Asked asked = finder.ask(keys, keys.start(u));
       if constexpr (FORMAT == DCONV_CACHE_PLAIN) {
+        // Keys and values have a buffer each, filled again as soon as it is read: a
+        // tile is on its way through all of the other's arithmetic.
         typedef PlainTiles<T, DP, BN, 1> Tiles;
         Tiles ck, cv;
         ck.init(D, c.k_stride[1], 0, lane);
@@ -634,42 +880,63 @@ __global__ __launch_bounds__(64 * split_waves<T>(DP), split_waves<T>(DP) == 4 ? 
         for (; u < end; u += W) {
           const int j0 = keys.start(u);
           const uint32_t gone = (uint32_t)f.gone;
-          landed<Tiles::C::kCopies>();   // the values may still be on their way
-          f32x16 s = soft.scores(kt, 0, q, lane);
-          landed<Tiles::C::kCopies>();
-          if (u + W < end) {
+          const bool more = u + W < end;
+          Reader<T, DP> rd = reader;
+          rd.again();
+          landed<Tiles::C::kCopies>();   // the keys; the values may still be on their way
+          f32x16 s = soft.scores(rd, kt, 0, q);
+          landed<Tiles::C::kCopies>();   // (read)
+          if (more) {
             f = finder.find(c, asked);
             close = near && keys.whole(keys.start(u + W));
             ck.stage(kt, kb, f.k, close, ct.pieces, D, 0, lane);
           }
-          soft.mask(s, j0, see, sh.sinks, lane, gone);
-          soft.follow(s, ct.scale2, [] {});
           Frag w[2];
-          soft.probabilities(s, ct.scale2, w);
-          if (u + W < end) landed<Tiles::C::kCopies>();
+          weigh(s, j0, gone, w);
+          if (more) landed<Tiles::C::kCopies>();   // the values; not the next keys
           else landed<0>();
-          soft.values(vt, 0, w, lane);
-          if (u + W < end) {
+          soft.values(rd, vt, 0, w);
+          if (more) {
             if (u + 2 * W < end) asked = finder.ask(keys, keys.start(u + 2 * W));
-            landed<63>();
+            landed<63>();   // (read)
             cv.stage(vt, vb, f.v, close, ct.pieces, D, 0, lane);
           }
         }
       } else {
+        // Codes come into registers, kAhead tiles ahead: keys as operands, values by
+        // way of LDS, which turns them.
+        constexpr int kAhead = FORMAT == DCONV_CACHE_E2M1 ? 2 : 1;
         const uint8_t *ksb = p.cache.k_scale + g.hk * c.k_scale_stride[2], *vsb = p.cache.v_scale + g.hk * c.v_scale_stride[2];
-        CodeTiles<T, DP, BN, 64, FORMAT> codes;
-        Found f = finder.find(c, asked);
-        if (u + W < end) asked = finder.ask(keys, keys.start(u + W));
-        codes.load(kb, vb, ksb, vsb, f, D, lane);
-        for (; u < end; u += W) {
-          codes.store(kt, vt, lane);
-          const uint32_t gone = (uint32_t)f.gone;
-          if (u + W < end) {
-            f = finder.find(c, asked);
-            if (u + 2 * W < end) asked = finder.ask(keys, keys.start(u + 2 * W));
-            codes.load(kb, vb, ksb, vsb, f, D, lane);
+        Codes kc[kAhead];
+        CodeTiles<T, DP, BN, 64, FORMAT, 1> vc[kAhead];
+        uint32_t gone[kAhead];
+        auto load = [&](int i, int v) {   // tile v, whose places have been asked for
+          const Found f = finder.find(c, asked);
+          if (v + W < end) asked = finder.ask(keys, keys.start(v + W));
+          kc[i].load(kb + f.k, ksb + f.ks, D, lane >> 5);
+          vc[i].load(kb, vb, ksb, vsb, f, D, lane);
+          gone[i] = (uint32_t)f.gone;
+        };
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i)
+          if (u + i * W < end) load(i, u + i * W);
+        for (; u < end; u += kAhead * W) {
+#pragma unroll
+          for (int i = 0; i < kAhead; ++i) {
+            const int v = u + i * W;
+            if (v >= end) break;
+            Reader<T, DP> rd = reader;
+            rd.again();
+            f32x16 s = {};
+#pragma unroll
+            for (int k = 0; k < KS; ++k) s = Mma<T>::mac(kc[i].frag(k), q[k], s);
+            vc[i].store(vt, vt, lane);
+            const uint32_t now = gone[i];
+            if (v + kAhead * W < end) load(i, v + kAhead * W);
+            Frag w[2];
+            weigh(s, keys.start(v), now, w);
+            soft.values(rd, vt, 0, w);
           }
-          soft.add(kt, vt, q, keys.start(u), see, sh.sinks, ct.scale2, true, lane, gone);
         }
       }
     }
@@ -763,10 +1030,13 @@ __global__ __launch_bounds__(64 * split_waves<T>(DP), split_waves<T>(DP) == 4 ? 
     // (see cache_tiles; the stores above come first, a row's by this workgroup alone)
     const unsigned redo = again;
     for (int x = wave; x < rows; x += W)
-      if (redo >> x & 1) cache_attend_row<T, FORMAT>(c, sh, t, p, g.b, g.s, g.s.row + x / G, g.hk * G + x % G);
+      if (redo >> x & 1) {
+        const CacheCall &f = fresh();
+        cache_attend_row<T, FORMAT>(f.c, f.sh, f.t, f.p, g.b, g.s, g.s.row + x / G, g.hk * G + x % G);
+      }
     __syncthreads();
   });
-  if (threadIdx.x == 0) ct.joins[range.id] = join;
+  if (threadIdx.x == 0) fresh().ct.joins[range.id] = join;
 }
 
 // ---------------------------------------------------------------------------
@@ -850,9 +1120,11 @@ void launch_cache_attend(const dconv_cache &c, const dconv_cache_attend_shape &s
     constexpr int DP = decltype(dp)::value;
     tiles.partial = few.partial + (int64_t)plan.few * 2 * cache_part<kFewRows, DP>();
     if (plan.few > 0)
-      hipLaunchKernelGGL((cache_few<T, DP, FORMAT>), dim3(plan.few), dim3(64 * split_waves<T>(DP)), 0, s, c, sh, t, p, few);
+      hipLaunchKernelGGL((cache_few<T, DP, FORMAT>), dim3(plan.few), dim3(64 * split_waves<T>(DP)), 0, s,
+                         CacheCall{c, sh, t, p, few});
     if (plan.tiles > 0)
-      hipLaunchKernelGGL((cache_tiles<T, DP, FORMAT>), dim3(plan.tiles), dim3(256), 0, s, c, sh, t, p, tiles);
+      hipLaunchKernelGGL((cache_tiles<T, DP, FORMAT>), dim3(plan.tiles), dim3(256), 0, s,
+                         CacheCall{c, sh, t, p, tiles});
     hipLaunchKernelGGL((cache_join<T, DP, FORMAT>), dim3(plan.few + plan.tiles, plan.tiles > 0 ? 8 : 2), dim3(256), 0, s,
                        c, sh, t, p, few, tiles);
   });
