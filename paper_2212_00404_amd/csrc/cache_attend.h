@@ -108,6 +108,7 @@ struct CachePlan {
   bool direct, pieces, near;    // as in CacheTile
   int few, tiles;               // workgroups
   int few_least, tiles_least;   // least work of one, in keys
+  int few_whole, tiles_whole;   // items of a sequence's key head, if every workgroup takes one; 0: by work
   int64_t joins_bytes, workspace;
 };
 

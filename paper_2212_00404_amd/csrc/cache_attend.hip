@@ -1,5 +1,6 @@
 // Attention of new tokens over a cache in pages (dconv_cache_attend): validation
 // and launch.
+#include <algorithm>
 #include <climits>
 #include <cmath>
 
@@ -37,12 +38,13 @@ bool whole_pieces(const void *p, int D, int es, std::initializer_list<long long>
 
 int padded_head(int D) { return D <= 32 ? 32 : D <= 64 ? 64 : D <= 96 ? 96 : D <= 128 ? 128 : 256; }
 
-CachePlan plan_attend(const dconv_cache &c, const dconv_cache_attend_shape &sh) {
+// `even`: every sequence has max_rows rows.
+CachePlan plan_attend(const dconv_cache &c, const dconv_cache_attend_shape &sh, bool even) {
   CachePlan f = {};
   f.dp = padded_head(c.D);
   const int es = element_size(sh.dtype), G = sh.Hq / c.Hkv;
-  const int64_t rows = (int64_t)(sh.max_rows > 0 ? sh.max_rows : sh.N) * G;
-  const int64_t keys = (int64_t)sh.table_width * c.page_size + 64;
+  const int64_t rows = (int64_t)(sh.max_rows > 0 ? sh.max_rows : sh.N) * G, heads = (int64_t)sh.B * c.Hkv;
+  const int64_t keys = (int64_t)sh.table_width * c.page_size;
   // Two workgroups per compute unit, where LDS and registers hold them; no more than
   // there is work for.
   auto groups = [](int64_t most, int64_t work, int least) {
@@ -51,13 +53,20 @@ CachePlan plan_attend(const dconv_cache &c, const dconv_cache_attend_shape &sh) 
   };
   f.few_least = 256;
   f.tiles_least = 512;
-  f.few = groups(f.dp * es <= 256 ? 512 : 256, (int64_t)sh.B * c.Hkv * keys, f.few_least);
+  if (!even || rows <= 32) {
+    f.few = groups(f.dp * es <= 256 ? 512 : 256, heads * (keys + 64), f.few_least);
+    // tables of a few steps of a workgroup: nothing is divided, and nothing joined
+    if (keys <= 512 && heads < (1 << 20)) f.few_whole = 1, f.few = (int)heads;
+  }
   if (rows > 32) {
     const int64_t tiles = ((int64_t)sh.N * G / 128 + sh.B) * c.Hkv;
-    f.tiles = groups(f.dp * es <= 256 ? 512 : 256, tiles * keys, f.tiles_least);
+    f.tiles = groups(f.dp * es <= 256 ? 512 : 256, tiles * (keys + 64), f.tiles_least);
+    const int64_t each = (rows + 127) / 128;
+    if (even && keys <= 512 && heads * each < (1 << 20)) f.tiles_whole = (int)each, f.tiles = (int)(heads * each);
   }
-  f.joins_bytes = ((int64_t)(f.few + f.tiles) * (int64_t)sizeof(CacheJoin) + 15) / 16 * 16;
-  f.workspace = f.joins_bytes + ((int64_t)f.few * 32 + (int64_t)f.tiles * 128) * 2 * (f.dp + 2) * 4;
+  const int64_t few = f.few_whole ? 0 : f.few, tiles = f.tiles_whole ? 0 : f.tiles;
+  f.joins_bytes = ((few + tiles) * (int64_t)sizeof(CacheJoin) + 15) / 16 * 16;
+  f.workspace = f.joins_bytes + (few * 32 + tiles * 128) * 2 * (f.dp + 2) * 4;
   return f;
 }
 
@@ -69,9 +78,12 @@ int launch(const dconv_cache &c, const dconv_cache_attend_shape &sh, const Batch
   if (c.format == DCONV_CACHE_PLAIN) {
     plan.pieces = whole_pieces(p.cache.k, c.D, es, {c.k_stride[0], c.k_stride[1], c.k_stride[2]}) &&
                   whole_pieces(p.cache.v, c.D, es, {c.v_stride[0], c.v_stride[1], c.v_stride[2]});
-    const long long far = (1ll << 31) / es / 64 - c.D;   // (a copy has 16 rows at most)
-    plan.near = plan.pieces && c.k_stride[1] >= 0 && c.k_stride[1] < far && c.v_stride[1] >= 0 && c.v_stride[1] < far;
   }
+  // as many slots as a tile has keys (64) span less than 2^31 bytes
+  plan.near = c.format != DCONV_CACHE_PLAIN || plan.pieces;
+  const long long far = (1ll << 31) / (c.format == DCONV_CACHE_PLAIN ? es : 1) / 64 - c.D;
+  for (long long s : {c.k_stride[1], c.v_stride[1], c.k_scale_stride[1], c.v_scale_stride[1]})
+    plan.near = plan.near && s >= 0 && s < far;
   (void)hipGetLastError();  // report this launch only
   by_type(sh.dtype, [&](auto *type) {
     by_format(c.format, [&](auto format) {
@@ -89,7 +101,8 @@ DCONV_EXPORT int dconv_cache_attend_workspace(const dconv_cache *cache, const dc
                                               long long *bytes) {
   if (!cache || !shape || !bytes) return DCONV_ENULL;
   const int rc = dconv::validate(*cache, *shape);
-  if (rc == DCONV_OK) *bytes = shape->B == 0 || shape->N == 0 ? 0 : dconv::plan_attend(*cache, *shape).workspace;
+  if (rc == DCONV_OK) *bytes = shape->B == 0 || shape->N == 0 ? 0 : std::max(dconv::plan_attend(*cache, *shape, false).workspace,
+                                        dconv::plan_attend(*cache, *shape, true).workspace);
   return rc;
 }
 
@@ -113,10 +126,9 @@ DCONV_EXPORT int dconv_cache_attend(const dconv_cache *cache, const dconv_cache_
   const Batch t = batch_of(*cache, shape->B, shape->N, shape->table_width, shape->table_stride, offsets);
   dconv_cache_attend_shape sh = *shape;
   if (!offsets) sh.max_rows = t.each;
-  CachePlan plan = plan_attend(*cache, sh);
+  CachePlan plan = plan_attend(*cache, sh, !offsets);
   if (plan.workspace > 0 && !workspace) return DCONV_ENULL;
   if (workspace_bytes < plan.workspace) return DCONV_EWORKSPACE;
   if ((uintptr_t)workspace % 16 != 0) return DCONV_EINVAL;
-  if (!offsets && plan.tiles > 0) plan.few = 0;   // all sequences are alike
   return launch(*cache, sh, t, p, plan, workspace, stream);
 }

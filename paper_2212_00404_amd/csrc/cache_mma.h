@@ -14,6 +14,7 @@ struct CacheTile {
   bool direct;          // queries and results in 16-byte pieces
   bool pieces, near;    // rows of a plain cache too; and those of one copy span less than 2^31 bytes
   int groups, least;    // workgroups, the least work of one
+  int whole;            // tiles per sequence and key head, one for each workgroup; 0: by work
   float *partial;       // two parts of each workgroup's
   CacheJoin *joins;     // one of each workgroup's
 };
@@ -57,17 +58,20 @@ struct KeyRange {
     n = front + max(hi > lo ? (hi + BN - 1) / BN - from : 0, 0);
   }
   __device__ __forceinline__ int start(int u) const { return (u < front ? u : u - front + from) * BN; }
-  // j, or where no row sees it a key that one sees.
-  __device__ __forceinline__ int key(int j) const {
+  // Key j of the tile from j0 on, or where no row sees it one of the tile that is seen.
+  __device__ __forceinline__ int key(int j0, int j) const {
     if (j < first) return j;
-    if (j < lo) return first > 0 ? first - 1 : lo;
+    if (j < lo) return lo < j0 + BN ? lo : first - 1;
     return min(j, hi - 1);
   }
   __device__ __forceinline__ bool whole(int j0) const { return (j0 >= lo && j0 + BN <= hi) || j0 + BN <= first; }
 };
 
-// Where the keys of a tile are, key l of it in lane l (and l + 32 for 32 keys): asked
-// for a tile ahead, as the table's entry comes from memory.
+// Where the keys of a tile are, asked for a tile ahead, as the table's entry comes
+// from memory.  ONE: a tile lies within a page, and is found by scalar arithmetic: the
+// place of its first key.  Else key l of it in lane l (and l + 32 for 32 keys): the
+// places are handed to the lanes that load by exchanges, 75 vector instructions for a
+// wave and tile of 64 keys beside some 300 of its arithmetic.
 struct Asked {
   int page, slot;
 };
@@ -75,20 +79,21 @@ struct Found {
   int64_t k, v, ks, vs;   // bytes from the head's base
   uint64_t gone;          // keys without a page, whose places are the first page's
 };
-template <class T, int FORMAT, int BN>
+template <class T, int FORMAT, int BN, bool ONE>
 struct Finder {
   static constexpr int64_t kBytes = FORMAT == DCONV_CACHE_PLAIN ? sizeof(T) : 1;
   const int *table;
   FastDiv page;
   int pages;
   __device__ __forceinline__ Asked ask(const KeyRange<BN> &keys, int j0) const {
-    const uint32_t j = (uint32_t)keys.key(j0 + (int)(threadIdx.x & (BN - 1)));
+    const uint32_t j = (uint32_t)(ONE ? j0 : keys.key(j0, j0 + (int)(threadIdx.x & (BN - 1))));
     const uint32_t at = page.div(j);
     return {table[at], (int)(j - at * page.d)};
   }
   __device__ __forceinline__ Found find(const dconv_cache &c, const Asked &a) const {
-    const bool there = a.page >= 0 && a.page < pages;
-    const int64_t p = there ? a.page : 0;
+    const int entry = ONE ? uniform(a.page) : a.page;
+    const bool there = entry >= 0 && entry < pages;
+    const int64_t p = there ? entry : 0;
     Found f;
     f.k = (p * c.k_stride[0] + a.slot * c.k_stride[1]) * kBytes;
     f.v = (p * c.v_stride[0] + a.slot * c.v_stride[1]) * kBytes;
@@ -97,7 +102,7 @@ struct Finder {
       f.ks = p * c.k_scale_stride[0] + a.slot * c.k_scale_stride[1];
       f.vs = p * c.v_scale_stride[0] + a.slot * c.v_scale_stride[1];
     }
-    f.gone = __ballot(!there);
+    f.gone = ONE ? (there ? 0 : ~(uint64_t)0) : __ballot(!there);
     return f;
   }
 };
@@ -114,31 +119,35 @@ __device__ __forceinline__ int64_t from_uniform_lane(int64_t x, int lane) {
 // ---------------------------------------------------------------------------
 // Tiles of a plain cache: copied into LDS
 // ---------------------------------------------------------------------------
-template <class T, int DP, int BN, int NW>
+template <class T, int DP, int BN, int NW, bool ONE>
 struct PlainTiles {
   typedef Copy<T, DP, BN, NW> C;
-  static constexpr int kRows = 64 / C::kPieces;           // of one copy of a wave, where they are whole
+  static constexpr int kRows = C::kPieces < 64 ? 64 / C::kPieces : 1;   // of one copy of a wave, where they are whole
   static constexpr bool kWhole = 64 % C::kPieces == 0;
-  uint32_t offset[C::kStep ? 1 : C::kCopies];             // of the lane's pieces from the copy's first row
+  C copy;             // offsets of the lane's pieces: from the tile's first row, or (not ONE) from the copy's
+  int64_t stride;     // of slots, in elements
 
   __device__ __forceinline__ void init(int D, int64_t slot_stride, int wave, int lane) {
-    if constexpr (kWhole) {
-#pragma unroll
-      for (int i = 0; i < (C::kStep ? 1 : C::kCopies); ++i)
-        offset[i] = (uint32_t)(C::row(i, wave, lane) % kRows) * (uint32_t)slot_stride * (uint32_t)sizeof(T) +
-                    C::element(i, wave, lane, D) * (uint32_t)sizeof(T);
-    }
+    stride = slot_stride;
+    if constexpr (ONE || kWhole)
+      copy.init(D, wave, lane, [&](int r) {
+        return (uint32_t)(ONE ? r : r % kRows) * (uint32_t)slot_stride * (uint32_t)sizeof(T);
+      });
   }
-  // The tile whose rows' places the lanes hold in `at`.  `close`: the rows of a copy
-  // stand in one page: a scalar base and a 32-bit offset each.
-  __device__ __forceinline__ void stage(T *lds, const char *base, int64_t at, bool close, bool pieces, int D, int wave,
-                                        int lane) const {
-    if constexpr (kWhole) {
-      if (close) {
+  // The tile from key j0 on, whose place is `at` (of its first key, or of the keys in
+  // the lanes).  `close`: the rows of a copy stand in one page, and all are seen: a
+  // scalar base and a 32-bit offset each.
+  __device__ __forceinline__ void stage(T *lds, const char *base, int64_t at, const KeyRange<BN> &keys, int j0,
+                                        bool close, bool pieces, int D, int wave, int lane) const {
+    if (close) {
+      if constexpr (ONE) {
+        copy.tile(lds, reinterpret_cast<const T *>(base + at), C::kStep * stride * (int64_t)sizeof(T), wave);
+        return;
+      } else if constexpr (kWhole) {
 #pragma unroll
         for (int i = 0; i < C::kCopies; ++i) {
           if (!C::has(i, wave)) break;
-          uint32_t o = offset[C::kStep ? 0 : i];
+          uint32_t o = copy.offset[C::kStep ? 0 : i];
           asm volatile("" : "+v"(o));
           const char *row = base + from_uniform_lane(at, (i * C::kThreads + 64 * wave) / C::kPieces);
           __builtin_amdgcn_global_load_lds(row + o, (lds_ptr)C::to(lds, i, wave), 16, 0, 0);
@@ -146,7 +155,12 @@ struct PlainTiles {
         return;
       }
     }
-    auto row = [&](int r) { return reinterpret_cast<const T *>(base + from_lane(at, r)); };
+    auto row = [&](int r) {
+      if constexpr (ONE)
+        return reinterpret_cast<const T *>(base + at) + (keys.key(j0, j0 + r) - j0) * stride;
+      else
+        return reinterpret_cast<const T *>(base + from_lane(at, r));
+    };
     if (pieces) {
       C::rows(lds, D, wave, lane, row);
       return;
@@ -170,7 +184,7 @@ template <int WORDS>
 struct __attribute__((packed, aligned(1))) RawCodes {
   uint32_t w[WORDS];
 };
-template <class T, int DP, int BN, int NT, int FORMAT, int TENSORS>
+template <class T, int DP, int BN, int NT, int FORMAT, int TENSORS, bool ONE>
 struct CodeTiles {
   static constexpr int kBlocks = DP / kBlock, kTensor = BN * kBlocks, kAll = TENSORS * kTensor;
   static constexpr int kPer = (kAll + NT - 1) / NT, kWords = kBlock / codes_per_word<FORMAT>();
@@ -180,28 +194,38 @@ struct CodeTiles {
   static __device__ __forceinline__ bool has(int u) { return kAll % NT == 0 || u < kAll; }
   static __device__ __forceinline__ int row_of(int u) { return (u & 15) + u % kTensor / (16 * kBlocks) * 16; }
   static __device__ __forceinline__ int block_of(int u) { return (u >> 4) % kBlocks; }
-  __device__ __forceinline__ void load(const char *k, const char *v, const uint8_t *ks, const uint8_t *vs,
-                                       const Found &f, int D, int thread) {
+  // k, v, ks, vs: the head's bases.
+  __device__ __forceinline__ void load(const dconv_cache &c, const char *k, const char *v, const uint8_t *ks,
+                                       const uint8_t *vs, const Found &f, const KeyRange<BN> &keys, int j0, int D,
+                                       int thread) {
+    const bool whole = ONE && keys.whole(j0);
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
       const int u = i * NT + thread, row = row_of(u), blk = block_of(u);
-      int64_t at, sat;
       bool value = TENSORS == 1 || u >= kTensor;
-      if constexpr (TENSORS == 1 || kTensor % 64 == 0) {
-        value = uniform(value);   // a wave's are of one tensor
-        at = from_lane(value ? f.v : f.k, row);
-        sat = from_lane(value ? f.vs : f.ks, row);
+      if constexpr (TENSORS == 1 || kTensor % 64 == 0) value = uniform(value);   // a wave's are of one tensor
+      const char *from;
+      const uint8_t *sfrom;
+      if constexpr (ONE) {
+        const int r = whole ? row : keys.key(j0, j0 + row) - j0;
+        const int rs = (int)(value ? c.v_stride[1] : c.k_stride[1]);
+        const int ss = (int)(value ? c.v_scale_stride[1] : c.k_scale_stride[1]);
+        from = (value ? v + f.v : k + f.k) + (uint32_t)(r * rs + blk * (kWords * 4));
+        sfrom = (value ? vs + f.vs : ks + f.ks) + (uint32_t)(r * ss + blk);
+      } else if constexpr (TENSORS == 1 || kTensor % 64 == 0) {
+        from = (value ? v : k) + from_lane(value ? f.v : f.k, row) + blk * (kWords * 4);
+        sfrom = (value ? vs : ks) + from_lane(value ? f.vs : f.ks, row) + blk;
       } else {
         const int64_t ak = from_lane(f.k, row), av = from_lane(f.v, row), sk = from_lane(f.ks, row),
                       sv = from_lane(f.vs, row);
-        at = value ? av : ak;
-        sat = value ? sv : sk;
+        from = (value ? v + av : k + ak) + blk * (kWords * 4);
+        sfrom = (value ? vs + sv : ks + sk) + blk;
       }
       raw[i] = {};
       scale[i] = 0;
       if (has(u) && blk * kBlock < D) {
-        raw[i] = *reinterpret_cast<const RawCodes<kWords> *>((value ? v : k) + at + blk * (kWords * 4));
-        scale[i] = (value ? vs : ks)[sat + blk];
+        raw[i] = *reinterpret_cast<const RawCodes<kWords> *>(from);
+        scale[i] = *sfrom;
       }
     }
   }
@@ -486,6 +510,12 @@ __device__ __forceinline__ Range find_range(const CacheCall &a, RangeScratch &ld
   const Batch &t = a.t;
   const CachePtrs &p = a.p.cache;
   const int tid = threadIdx.x, G = sh.Hq / c.Hkv, most = most_rows(a);
+  if (a.ct.whole > 0) {   // an item
+    Range r = {};
+    r.id = xcd_remap(blockIdx.x, a.ct.groups);
+    r.b = r.id / (c.Hkv * a.ct.whole);
+    return r;
+  }
   const int per = (t.B + NT - 1) / NT, b0 = min(tid * per, t.B), b1 = min(b0 + per, t.B);
   auto work = [&](int b) {
     const Work<FEW> w(sh, G, rows_of(t, p, b), most);
@@ -562,6 +592,15 @@ __device__ __forceinline__ int cut(int64_t pos, int64_t work, int steps, int64_t
 
 template <bool FEW, class F>
 __device__ __forceinline__ void for_segments(const Range &r, F f) {
+  if (fresh().ct.whole > 0) {
+    const CacheCall &a = fresh();
+    Rows s = rows_of(a.t, a.p.cache, r.b);
+    s = {uniform(s.row), uniform(s.n), uniform(s.len)};
+    const Work<FEW> w(a.sh, a.sh.Hq / a.c.Hkv, s, most_rows(a));
+    const int tile = r.id % a.ct.whole;
+    if (tile < w.tiles) f(Segment{r.b, r.id / a.ct.whole % a.c.Hkv, tile, s, 0, 1, 1, 0});
+    return;
+  }
   int64_t x = r.begin, at = r.at;
   for (int b = r.b; x < r.end; ++b) {
     const CacheCall &a = fresh();
@@ -597,7 +636,7 @@ constexpr int cache_part() { return R * (DP + 2); }
 // ---------------------------------------------------------------------------
 // 128 rows: four waves of 32 share tiles of keys
 // ---------------------------------------------------------------------------
-template <class T, int DP, int FORMAT>
+template <class T, int DP, int FORMAT, bool ONE>
 __global__ __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1) void cache_tiles(
     const CacheCall) {
   constexpr int BN = forward_keys<T>(DP), KS = DP / 16, DT = DP / 32;
@@ -648,8 +687,8 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1) void cache_tile
 #pragma unroll
     for (int k = 0; k < KS; ++k) q[k] = load_frag(qrow, 16 * k + 8 * (lane >> 5), D, ct.direct, ct.sign);
 
-    const Finder<T, FORMAT, BN> finder = {p.cache.table + g.b * t.table_stride, t.page, t.pages};
-    const int64_t es = Finder<T, FORMAT, BN>::kBytes;
+    const Finder<T, FORMAT, BN, ONE> finder = {p.cache.table + g.b * t.table_stride, t.page, t.pages};
+    const int64_t es = Finder<T, FORMAT, BN, ONE>::kBytes;
     const char *kb = static_cast<const char *>(p.cache.k) + g.hk * c.k_stride[2] * es;
     const char *vb = static_cast<const char *>(p.cache.v) + g.hk * c.v_stride[2] * es;
     const Reader<T, DP> rd(lane);
@@ -675,16 +714,18 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1) void cache_tile
     if (u0 < u1) {
       Asked asked = finder.ask(keys, keys.start(u0));
       if constexpr (FORMAT == DCONV_CACHE_PLAIN) {
-        PlainTiles<T, DP, BN, 4> kt, vt;
+        typedef PlainTiles<T, DP, BN, 4, ONE> Tiles;
+        Tiles kt, vt;
         kt.init(D, c.k_stride[1], wave, lane);
         vt.init(D, c.v_stride[1], wave, lane);
-        const bool near = ct.near && t.page.d % PlainTiles<T, DP, BN, 4>::kRows == 0;
+        const bool near = ct.near && (ONE || (Tiles::kWhole && t.page.d % Tiles::kRows == 0));
         // stages tile u and asks for the one after it
         auto stage = [&](T *buf, int u) {
+          const int j0 = keys.start(u);
           const Found f = finder.find(c, asked);
-          const bool close = near && keys.whole(keys.start(u));
-          kt.stage(buf, kb, f.k, close, ct.pieces, D, wave, lane);
-          vt.stage(buf + BN * DP, vb, f.v, close, ct.pieces, D, wave, lane);
+          const bool close = near && keys.whole(j0);
+          kt.stage(buf, kb, f.k, keys, j0, close, ct.pieces, D, wave, lane);
+          vt.stage(buf + BN * DP, vb, f.v, keys, j0, close, ct.pieces, D, wave, lane);
           if (u + 1 < u1) asked = finder.ask(keys, keys.start(u + 1));
           return f.gone;
         };
@@ -704,11 +745,11 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1) void cache_tile
         }
       } else {
         const uint8_t *ksb = p.cache.k_scale + g.hk * c.k_scale_stride[2], *vsb = p.cache.v_scale + g.hk * c.v_scale_stride[2];
-        CodeTiles<T, DP, BN, 256, FORMAT, 2> codes;
+        CodeTiles<T, DP, BN, 256, FORMAT, 2, ONE> codes;
         uint64_t next = 0;
         auto load = [&](int u) {
           const Found f = finder.find(c, asked);
-          codes.load(kb, vb, ksb, vsb, f, D, threadIdx.x);
+          codes.load(c, kb, vb, ksb, vsb, f, keys, keys.start(u), D, threadIdx.x);
           next = f.gone;
           if (u + 1 < u1) asked = finder.ask(keys, keys.start(u + 1));
         };
@@ -789,13 +830,13 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1) void cache_tile
       cache_attend_row<T, FORMAT>(f.c, f.sh, f.t, f.p, g.b, g.s, g.s.row + x / G, g.hk * G + x % G);
     }
   });
-  if (threadIdx.x == 0) fresh().ct.joins[range.id] = join;
+  if (threadIdx.x == 0 && fresh().ct.whole == 0) fresh().ct.joins[range.id] = join;
 }
 
 // ---------------------------------------------------------------------------
 // Up to 32 rows: each wave takes tiles of 32 keys by itself
 // ---------------------------------------------------------------------------
-template <class T, int DP, int FORMAT>
+template <class T, int DP, int FORMAT, bool ONE>
 __global__ __launch_bounds__(64 * split_waves<T>(DP), split_waves<T>(DP) == 4 ? 2 : 1) void cache_few(
     const CacheCall) {
   constexpr int KS = DP / 16, DT = DP / 32, BN = 32, kTile = BN * DP, W = split_waves<T>(DP);
@@ -844,8 +885,8 @@ __global__ __launch_bounds__(64 * split_waves<T>(DP), split_waves<T>(DP) == 4 ? 
       q[k] = load_frag(qrow, FORMAT == DCONV_CACHE_PLAIN ? 16 * k + 8 * (lane >> 5) : Codes::order_of(k, lane >> 5), D,
                        ct.direct, ct.sign);
 
-    const Finder<T, FORMAT, BN> finder = {p.cache.table + g.b * t.table_stride, t.page, t.pages};
-    const int64_t es = Finder<T, FORMAT, BN>::kBytes;
+    const Finder<T, FORMAT, BN, ONE> finder = {p.cache.table + g.b * t.table_stride, t.page, t.pages};
+    const int64_t es = Finder<T, FORMAT, BN, ONE>::kBytes;
     const char *kb = static_cast<const char *>(p.cache.k) + g.hk * c.k_stride[2] * es;
     const char *vb = static_cast<const char *>(p.cache.v) + g.hk * c.v_stride[2] * es;
     const Reader<T, DP> reader(lane);
@@ -867,18 +908,24 @@ __global__ __launch_bounds__(64 * split_waves<T>(DP), split_waves<T>(DP) == 4 ? 
       if constexpr (FORMAT == DCONV_CACHE_PLAIN) {
         // Keys and values have a buffer each, filled again as soon as it is read: a
         // tile is on its way through all of the other's arithmetic.
-        typedef PlainTiles<T, DP, BN, 1> Tiles;
+        typedef PlainTiles<T, DP, BN, 1, ONE> Tiles;
         Tiles ck, cv;
         ck.init(D, c.k_stride[1], 0, lane);
         cv.init(D, c.v_stride[1], 0, lane);
-        const bool near = ct.near && t.page.d % Tiles::kRows == 0;
+        const bool near = ct.near && (ONE || (Tiles::kWhole && t.page.d % Tiles::kRows == 0));
         Found f = finder.find(c, asked);
-        bool close = near && keys.whole(keys.start(u));
-        ck.stage(kt, kb, f.k, close, ct.pieces, D, 0, lane);
+        auto stage_keys = [&](int v) {
+          const int j0 = keys.start(v);
+          ck.stage(kt, kb, f.k, keys, j0, near && keys.whole(j0), ct.pieces, D, 0, lane);
+        };
+        auto stage_values = [&](int v) {
+          const int j0 = keys.start(v);
+          cv.stage(vt, vb, f.v, keys, j0, near && keys.whole(j0), ct.pieces, D, 0, lane);
+        };
+        stage_keys(u);
         if (u + W < end) asked = finder.ask(keys, keys.start(u + W));
-        cv.stage(vt, vb, f.v, close, ct.pieces, D, 0, lane);
+        stage_values(u);
         for (; u < end; u += W) {
-          const int j0 = keys.start(u);
           const uint32_t gone = (uint32_t)f.gone;
           const bool more = u + W < end;
           Reader<T, DP> rd = reader;
@@ -888,18 +935,17 @@ __global__ __launch_bounds__(64 * split_waves<T>(DP), split_waves<T>(DP) == 4 ? 
           landed<Tiles::C::kCopies>();   // (read)
           if (more) {
             f = finder.find(c, asked);
-            close = near && keys.whole(keys.start(u + W));
-            ck.stage(kt, kb, f.k, close, ct.pieces, D, 0, lane);
+            stage_keys(u + W);
           }
           Frag w[2];
-          weigh(s, j0, gone, w);
+          weigh(s, keys.start(u), gone, w);
           if (more) landed<Tiles::C::kCopies>();   // the values; not the next keys
           else landed<0>();
           soft.values(rd, vt, 0, w);
           if (more) {
             if (u + 2 * W < end) asked = finder.ask(keys, keys.start(u + 2 * W));
             landed<63>();   // (read)
-            cv.stage(vt, vb, f.v, close, ct.pieces, D, 0, lane);
+            stage_values(u + W);
           }
         }
       } else {
@@ -908,13 +954,15 @@ __global__ __launch_bounds__(64 * split_waves<T>(DP), split_waves<T>(DP) == 4 ? 
         constexpr int kAhead = FORMAT == DCONV_CACHE_E2M1 ? 2 : 1;
         const uint8_t *ksb = p.cache.k_scale + g.hk * c.k_scale_stride[2], *vsb = p.cache.v_scale + g.hk * c.v_scale_stride[2];
         Codes kc[kAhead];
-        CodeTiles<T, DP, BN, 64, FORMAT, 1> vc[kAhead];
+        CodeTiles<T, DP, BN, 64, FORMAT, 1, ONE> vc[kAhead];
         uint32_t gone[kAhead];
         auto load = [&](int i, int v) {   // tile v, whose places have been asked for
           const Found f = finder.find(c, asked);
           if (v + W < end) asked = finder.ask(keys, keys.start(v + W));
-          kc[i].load(kb + f.k, ksb + f.ks, D, lane >> 5);
-          vc[i].load(kb, vb, ksb, vsb, f, D, lane);
+          const int j0 = keys.start(v), r = lane & 31;
+          const uint32_t key = ONE ? keys.whole(j0) ? r : keys.key(j0, j0 + r) - j0 : 0;   // (else its place is the lane's)
+          kc[i].load(kb + f.k + key * (uint32_t)c.k_stride[1], ksb + f.ks + key * (uint32_t)c.k_scale_stride[1], D, lane >> 5);
+          vc[i].load(c, kb, vb, ksb, vsb, f, keys, j0, D, lane);
           gone[i] = (uint32_t)f.gone;
         };
 #pragma unroll
@@ -1036,48 +1084,65 @@ __global__ __launch_bounds__(64 * split_waves<T>(DP), split_waves<T>(DP) == 4 ? 
       }
     __syncthreads();
   });
-  if (threadIdx.x == 0) fresh().ct.joins[range.id] = join;
+  if (threadIdx.x == 0 && fresh().ct.whole == 0) fresh().ct.joins[range.id] = join;
 }
 
 // ---------------------------------------------------------------------------
-// Parts joined: a wave per row
+// Parts joined
 // ---------------------------------------------------------------------------
+// A row by one wave, or, of more than four parts, by four that take every fourth part
+// each: a sum over 64 parts is a chain of 16 loads that miss, in two batches.
 template <class T, int DP, int FORMAT, int R>
 __device__ __forceinline__ void join_rows(const dconv_cache &c, const dconv_cache_attend_shape &sh, const Batch &t,
-                                          const CacheAttendPtrs &p, const CacheTile &ct, int id) {
+                                          const CacheAttendPtrs &p, const CacheTile &ct, int id, float (&lds)[4][DP + 1]) {
   const CacheJoin j = ct.joins[id];
   if (j.parts == 0) return;
-  const int lane = threadIdx.x & 63, G = sh.Hq / c.Hkv;
+  constexpr int E = (DP + 63) / 64;
+  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), G = sh.Hq / c.Hkv;
   const Rows s = rows_of(t, p.cache, j.b);
   // the first part is its workgroup's second one
   auto part = [&](int i) { return ct.partial + ((int64_t)(j.first + i) * 2 + (i == 0)) * cache_part<R, DP>(); };
-  for (int x = blockIdx.y * 4 + (threadIdx.x >> 6); x < j.rows; x += 4 * gridDim.y) {
+  const bool shared = j.parts > 4;
+  const int first = shared ? wave : 0, step = shared ? 4 : 1;
+  for (int x = shared ? blockIdx.y : blockIdx.y * 4 + wave; x < j.rows; x += (shared ? 1 : 4) * gridDim.y) {
     const int r = j.r0 + x, row = s.row + r / G, h = j.hk * G + r % G;
     const bool none = keys_seen(sh, s.len, s.start() + r / G).none();
-    // bases and totals, a part per lane
-    float m = -INFINITY;
+    float m = -INFINITY;   // the largest base, parts in the lanes
     for (int i = lane; i < j.parts; i += 64) m = fmaxf(m, part(i)[R * DP + x]);
     m = lanes_max<64>(m);
     const float base = m == -INFINITY ? 0.0f : m;
-    float l = 0.0f, acc[kLaneParts] = {};
-    for (int i0 = 0; i0 < j.parts; i0 += 64) {
-      const int i = i0 + lane;
-      float w = 0.0f;
-      if (i < j.parts) w = exp2f(part(i)[R * DP + x] - base);
-      if (w != 0.0f) l += w * part(i)[R * (DP + 1) + x];
-#pragma unroll 4
-      for (int k = 0; k < 64 && i0 + k < j.parts; ++k) {
-        const float f = __shfl(w, k);
-        const float *y = part(i0 + k) + x * DP;
+    float l = 0.0f, acc[E] = {};
+#pragma unroll 8
+    for (int i = first; i < j.parts; i += step) {
+      const float *from = part(i);
+      const float w = exp2f(from[R * DP + x] - base);
+      l += w * from[R * (DP + 1) + x];
 #pragma unroll
-        for (int e = 0; e < (DP + 63) / 64; ++e)
-          if (lane + 64 * e < c.D) acc[e] = fmaf(f, y[lane + 64 * e], acc[e]);
-      }
+      for (int e = 0; e < E; ++e)
+        if (lane + 64 * e < DP) acc[e] = fmaf(w, from[x * DP + lane + 64 * e], acc[e]);
     }
-    l = lanes_sum<64>(l);
+    if (shared) {   // by the first wave, in the waves' order
+#pragma unroll
+      for (int e = 0; e < E; ++e)
+        if (lane + 64 * e < DP) lds[wave][lane + 64 * e] = acc[e];
+      if (lane == 0) lds[wave][DP] = l;
+      __syncthreads();
+      l = 0.0f;
+#pragma unroll
+      for (int e = 0; e < E; ++e) acc[e] = 0.0f;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        l += lds[w][DP];
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+          if (lane + 64 * e < DP) acc[e] += lds[w][lane + 64 * e];
+      }
+      __syncthreads();
+      if (wave > 0) continue;
+    }
     bool bad = false;
 #pragma unroll
-    for (int e = 0; e < (DP + 63) / 64; ++e) {
+    for (int e = 0; e < E; ++e) {
       acc[e] = none ? 0.0f : acc[e] / l;
       bad |= lane + 64 * e < c.D && !(fabsf(acc[e]) < INFINITY);
     }
@@ -1087,18 +1152,20 @@ __device__ __forceinline__ void join_rows(const dconv_cache &c, const dconv_cach
     }
     T *o = static_cast<T *>(p.out) + row * sh.out_stride[0] + h * sh.out_stride[1];
 #pragma unroll
-    for (int e = 0; e < (DP + 63) / 64; ++e)
+    for (int e = 0; e < E; ++e)
       if (lane + 64 * e < c.D) o[lane + 64 * e] = from_f32<T>(acc[e]);
     if (p.lse && lane == 0) p.lse[(int64_t)row * sh.Hq + h] = none ? -INFINITY : log_sum(m, l);
   }
 }
 
-// The workgroups of both kernels, those of few rows first.
+// The workgroups of both kernels, those of few rows first (as far as they divide items).
 template <class T, int DP, int FORMAT>
 __global__ __launch_bounds__(256) void cache_join(const dconv_cache c, const dconv_cache_attend_shape sh, const Batch t,
                                                   const CacheAttendPtrs p, const CacheTile few, const CacheTile tiles) {
-  if ((int)blockIdx.x < few.groups) join_rows<T, DP, FORMAT, kFewRows>(c, sh, t, p, few, blockIdx.x);
-  else join_rows<T, DP, FORMAT, kTileRows>(c, sh, t, p, tiles, blockIdx.x - few.groups);
+  __shared__ float lds[4][DP + 1];
+  const int n = few.whole ? 0 : few.groups;
+  if ((int)blockIdx.x < n) join_rows<T, DP, FORMAT, kFewRows>(c, sh, t, p, few, blockIdx.x, lds);
+  else join_rows<T, DP, FORMAT, kTileRows>(c, sh, t, p, tiles, blockIdx.x - n, lds);
 }
 
 template <class T, int FORMAT>
@@ -1109,24 +1176,37 @@ void launch_cache_attend(const dconv_cache &c, const dconv_cache_attend_shape &s
     a.scale = sh.scale;
     return attend_tile(a, false, false);
   }();
-  CacheTile few = {scale.scale2, scale.sign, plan.direct, plan.pieces, plan.near, plan.few, plan.few_least, nullptr, nullptr};
+  CacheTile few = {scale.scale2, scale.sign, plan.direct, plan.pieces, plan.near, plan.few, plan.few_least,
+                   plan.few_whole, nullptr, nullptr};
   CacheTile tiles = few;
   tiles.groups = plan.tiles;
   tiles.least = plan.tiles_least;
+  tiles.whole = plan.tiles_whole;
+  const int few_joins = plan.few_whole ? 0 : plan.few, tile_joins = plan.tiles_whole ? 0 : plan.tiles;
   few.joins = reinterpret_cast<CacheJoin *>(workspace);
-  tiles.joins = few.joins + plan.few;
+  tiles.joins = few.joins + few_joins;
   few.partial = reinterpret_cast<float *>(workspace + plan.joins_bytes);
   by_width(plan.dp, [&](auto dp) {
     constexpr int DP = decltype(dp)::value;
-    tiles.partial = few.partial + (int64_t)plan.few * 2 * cache_part<kFewRows, DP>();
-    if (plan.few > 0)
-      hipLaunchKernelGGL((cache_few<T, DP, FORMAT>), dim3(plan.few), dim3(64 * split_waves<T>(DP)), 0, s,
-                         CacheCall{c, sh, t, p, few});
-    if (plan.tiles > 0)
-      hipLaunchKernelGGL((cache_tiles<T, DP, FORMAT>), dim3(plan.tiles), dim3(256), 0, s,
-                         CacheCall{c, sh, t, p, tiles});
-    hipLaunchKernelGGL((cache_join<T, DP, FORMAT>), dim3(plan.few + plan.tiles, plan.tiles > 0 ? 8 : 2), dim3(256), 0, s,
-                       c, sh, t, p, few, tiles);
+    tiles.partial = few.partial + (int64_t)few_joins * 2 * cache_part<kFewRows, DP>();
+    if (plan.few > 0) {
+      const CacheCall call = {c, sh, t, p, few};
+      const dim3 block(64 * split_waves<T>(DP));
+      if (plan.near && c.page_size % 32 == 0)
+        hipLaunchKernelGGL((cache_few<T, DP, FORMAT, true>), dim3(plan.few), block, 0, s, call);
+      else
+        hipLaunchKernelGGL((cache_few<T, DP, FORMAT, false>), dim3(plan.few), block, 0, s, call);
+    }
+    if (plan.tiles > 0) {
+      const CacheCall call = {c, sh, t, p, tiles};
+      if (plan.near && c.page_size % forward_keys<T>(DP) == 0)
+        hipLaunchKernelGGL((cache_tiles<T, DP, FORMAT, true>), dim3(plan.tiles), dim3(256), 0, s, call);
+      else
+        hipLaunchKernelGGL((cache_tiles<T, DP, FORMAT, false>), dim3(plan.tiles), dim3(256), 0, s, call);
+    }
+    if (few_joins + tile_joins > 0)
+      hipLaunchKernelGGL((cache_join<T, DP, FORMAT>), dim3(few_joins + tile_joins, tile_joins > 0 ? 16 : 8), dim3(256), 0,
+                         s, c, sh, t, p, few, tiles);
   });
 }
 
