@@ -385,23 +385,6 @@ struct CacheSoftmax : Softmax<T, DP> {
     const uint32_t gone0 = (uint32_t)gone, gone1 = (uint32_t)(gone >> 32);
     Frag w0[2], w1[2];
     rd.again();
-    if constexpr (DP > 96) {
-      f32x16 s0 = scores(rd, ks, 0, q);
-      if (masked) Base::mask(s0, j0, see, sinks, lane, gone0);
-      Base::follow(s0, scale2, [] {});
-      f32x16 s1 = scores(rd, ks, 32, q);
-      Base::probabilities(s0, scale2, w0);
-      asm volatile("" ::"v"(w0[0]), "v"(w0[1]));   // here, not after the next branch
-      if (masked) Base::mask(s1, j0 + 32, see, sinks, lane, gone1);
-      Base::follow(s1, scale2, [&] {
-        values(rd, vs, 0, w0);
-        w0[0] = w0[1] = Frag{};
-      });
-      values(rd, vs, 0, w0);
-      Base::probabilities(s1, scale2, w1);
-      values(rd, vs, 32, w1);
-      return;
-    }
     Frag kf[KS], vf[2][DT];
     auto load_keys = [&](int k0) {
 #pragma unroll
@@ -699,10 +682,12 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1) void cache_tile
       auto masked = [&](int v0, int N) {
         return gone != 0 || !(v0 + N <= all_to && (v0 >= all_from || v0 + N <= sh.sinks));
       };
-      if constexpr (BN == 64 && sizeof(T) == 2) {
+      if constexpr (BN == 64 && sizeof(T) == 2 && DP <= 96) {
         if (!unseen(j0, BN))
           soft.add_two(rd, buf, buf + BN * DP, q, j0, see, sh.sinks, ct.scale2, masked(j0, BN), lane, gone);
       } else {
+        // (registers: the scores of a second 32 keys would push out those that copies
+        // and codes of the next tile are on their way to)
 #pragma unroll
         for (int k = 0; k < BN; k += 32)
           if (!unseen(j0 + k, 32))
