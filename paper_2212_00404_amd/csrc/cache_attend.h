@@ -98,7 +98,8 @@ __device__ void cache_attend_row(const dconv_cache &c, const dconv_cache_attend_
 // workgroups from `first` on have left.
 struct CacheJoin {
   int parts, first;
-  int b, hk, r0, rows;
+  int b, hk, r0, rows;   // rows r0 .. of the key head's
+  Rows s;
 };
 
 // How a call runs: workgroups for sequences of up to 32 rows of a key head

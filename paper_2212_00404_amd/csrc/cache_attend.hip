@@ -64,6 +64,11 @@ CachePlan plan_attend(const dconv_cache &c, const dconv_cache_attend_shape &sh, 
     const int64_t each = (rows + 127) / 128;
     if (even && keys <= 512 && heads * each < (1 << 20)) f.tiles_whole = (int)each, f.tiles = (int)(heads * each);
   }
+  // one launch for both kinds (cache_tiles): as many workgroups, and shares of both
+  if (f.few > 0 && f.tiles > 0 && f.dp * es <= 256) {
+    f.few_whole = 0;
+    f.few = f.tiles = std::max(std::min(f.few, 512), f.tiles);
+  }
   const int64_t few = f.few_whole ? 0 : f.few, tiles = f.tiles_whole ? 0 : f.tiles;
   f.joins_bytes = ((few + tiles) * (int64_t)sizeof(CacheJoin) + 15) / 16 * 16;
   f.workspace = f.joins_bytes + (few * 32 + tiles * 128) * 2 * (f.dp + 2) * 4;

@@ -27,7 +27,11 @@ struct CacheCall {
   dconv_cache_attend_shape sh;
   Batch t;
   CacheAttendPtrs p;
-  CacheTile ct;
+  CacheTile few, tiles;
+  template <bool FEW>
+  __device__ __forceinline__ const CacheTile &tile() const {
+    return FEW ? few : tiles;
+  }
 };
 __device__ __forceinline__ const CacheCall &fresh() {
   typedef const __attribute__((address_space(4))) CacheCall *Arg;
@@ -366,11 +370,35 @@ struct CacheSoftmax : Softmax<T, DP> {
 #pragma unroll
       for (int c = 0; c < DT; ++c) o[c] = Mma<T>::mac(rd.column(vs, k0 + 16 * k, c), w[k], o[c]);
   }
+  static __device__ __forceinline__ void load_keys(const Reader<T, DP> &rd, Frag (&f)[KS], const T *ks, int k0) {
+#pragma unroll
+    for (int k = 0; k < KS; ++k) f[k] = rd.row(ks, k0, k);
+    in_order();
+  }
+  static __device__ __forceinline__ void load_values(const Reader<T, DP> &rd, Frag (&f)[DT], const T *vs, int k0) {
+#pragma unroll
+    for (int c = 0; c < DT; ++c) f[c] = rd.column(vs, k0, c);
+    in_order();
+  }
   // Adds 32 keys, j0 .., of the tiles ks, vs.
   __device__ __forceinline__ void add(Reader<T, DP> rd, const T *ks, const T *vs, const Frag (&q)[KS], int j0,
                                       const RowKeys &see, int sinks, float scale2, bool masked, int lane,
                                       uint32_t gone) {
     rd.again();
+    if constexpr (KS * sizeof(Frag) <= 128) {   // operands are read well before their products
+      Frag kf[KS], vf[2][DT];
+      load_keys(rd, kf, ks, 0);
+      f32x16 s = Base::products(kf, q);
+      load_values(rd, vf[0], vs, 0);
+      if (masked) Base::mask(s, j0, see, sinks, lane, gone);
+      Base::follow(s, scale2, [] {});
+      Frag w[2];
+      Base::probabilities(s, scale2, w);
+      load_values(rd, vf[1], vs, 16);
+      Base::weigh(vf[0], w[0]);
+      Base::weigh(vf[1], w[1]);
+      return;
+    }
     f32x16 s = scores(rd, ks, 0, q);
     if (masked) Base::mask(s, j0, see, sinks, lane, gone);
     Base::follow(s, scale2, [] {});
@@ -386,23 +414,13 @@ struct CacheSoftmax : Softmax<T, DP> {
     Frag w0[2], w1[2];
     rd.again();
     Frag kf[KS], vf[2][DT];
-    auto load_keys = [&](int k0) {
-#pragma unroll
-      for (int k = 0; k < KS; ++k) kf[k] = rd.row(ks, k0, k);
-      in_order();
-    };
-    auto load_values = [&](Frag(&f)[DT], int k0) {
-#pragma unroll
-      for (int c = 0; c < DT; ++c) f[c] = rd.column(vs, k0, c);
-      in_order();
-    };
-    load_keys(0);
+    load_keys(rd, kf, ks, 0);
     f32x16 s0 = Base::products(kf, q), s1;
-    load_keys(32);
+    load_keys(rd, kf, ks, 32);
     if (masked) Base::mask(s0, j0, see, sinks, lane, gone0);
     Base::follow(s0, scale2, [] {});
     s1 = Base::products(kf, q);
-    load_values(vf[0], 0);
+    load_values(rd, vf[0], vs, 0);
     Base::probabilities(s0, scale2, w0);
     asm volatile("" ::"v"(w0[0]), "v"(w0[1]));
     if (masked) Base::mask(s1, j0 + 32, see, sinks, lane, gone1);
@@ -410,11 +428,11 @@ struct CacheSoftmax : Softmax<T, DP> {
       values(rd, vs, 0, w0);
       w0[0] = w0[1] = Frag{};
     });
-    load_values(vf[1], 16);
+    load_values(rd, vf[1], vs, 16);
     Base::weigh(vf[0], w0[0]);
-    load_values(vf[0], 32);
+    load_values(rd, vf[0], vs, 32);
     Base::weigh(vf[1], w0[1]);
-    load_values(vf[1], 48);
+    load_values(rd, vf[1], vs, 48);
     Base::probabilities(s1, scale2, w1);
     Base::weigh(vf[0], w1[0]);
     Base::weigh(vf[1], w1[1]);
@@ -489,14 +507,15 @@ struct RangeScratch {
 template <bool FEW, int NT>
 __device__ __forceinline__ Range find_range(const CacheCall &a, RangeScratch &lds) {
   const dconv_cache &c = a.c;
+  const CacheTile &ct = a.tile<FEW>();
   const dconv_cache_attend_shape &sh = a.sh;
   const Batch &t = a.t;
   const CachePtrs &p = a.p.cache;
   const int tid = threadIdx.x, G = sh.Hq / c.Hkv, most = most_rows(a);
-  if (a.ct.whole > 0) {   // an item
+  if (ct.whole > 0) {   // an item
     Range r = {};
-    r.id = xcd_remap(blockIdx.x, a.ct.groups);
-    r.b = r.id / (c.Hkv * a.ct.whole);
+    r.id = xcd_remap(blockIdx.x, ct.groups);
+    r.b = r.id / (c.Hkv * ct.whole);
     return r;
   }
   const int per = (t.B + NT - 1) / NT, b0 = min(tid * per, t.B), b1 = min(b0 + per, t.B);
@@ -522,8 +541,8 @@ __device__ __forceinline__ Range find_range(const CacheCall &a, RangeScratch &ld
     total += lds.wave[w];
   }
   Range r;
-  r.id = xcd_remap(blockIdx.x, a.ct.groups);
-  r.share = max((total + a.ct.groups - 1) / a.ct.groups, (int64_t)a.ct.least);
+  r.id = xcd_remap(blockIdx.x, ct.groups);
+  r.share = max((total + ct.groups - 1) / ct.groups, (int64_t)ct.least);
   r.begin = r.id * r.share;
   r.end = min(r.begin + r.share, total);
   int64_t from = upto - mine;
@@ -575,13 +594,14 @@ __device__ __forceinline__ int cut(int64_t pos, int64_t work, int steps, int64_t
 
 template <bool FEW, class F>
 __device__ __forceinline__ void for_segments(const Range &r, F f) {
-  if (fresh().ct.whole > 0) {
+  if (fresh().tile<FEW>().whole > 0) {
     const CacheCall &a = fresh();
+    const int whole = a.tile<FEW>().whole;
     Rows s = rows_of(a.t, a.p.cache, r.b);
     s = {uniform(s.row), uniform(s.n), uniform(s.len)};
     const Work<FEW> w(a.sh, a.sh.Hq / a.c.Hkv, s, most_rows(a));
-    const int tile = r.id % a.ct.whole;
-    if (tile < w.tiles) f(Segment{r.b, r.id / a.ct.whole % a.c.Hkv, tile, s, 0, 1, 1, 0});
+    const int tile = r.id % whole;
+    if (tile < w.tiles) f(Segment{r.b, r.id / whole % a.c.Hkv, tile, s, 0, 1, 1, 0});
     return;
   }
   int64_t x = r.begin, at = r.at;
@@ -619,18 +639,14 @@ constexpr int cache_part() { return R * (DP + 2); }
 // ---------------------------------------------------------------------------
 // 128 rows: four waves of 32 share tiles of keys
 // ---------------------------------------------------------------------------
-template <class T, int DP, int FORMAT, bool ONE>
-__global__ __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1) void cache_tiles(
-    const CacheCall) {
+template <class T, int DP, int FORMAT, bool ONE, int LEN>
+__device__ __forceinline__ void tiles_body(T (&buf0)[LEN], T (&buf1)[LEN], RangeScratch &scratch) {
   constexpr int BN = forward_keys<T>(DP), KS = DP / 16, DT = DP / 32;
   typedef typename Mma<T>::Frag Frag;
-  __shared__ __align__(16) T buf0[2 * BN * DP];
-  __shared__ __align__(16) T buf1[2 * BN * DP];
-  __shared__ RangeScratch scratch;
-  DCONV_POISON(poison_lds(buf0, 2 * BN * DP); poison_lds(buf1, 2 * BN * DP));
+  static_assert(2 * BN * DP <= LEN, "a tile's keys and values");
   const int wave = uniform(threadIdx.x >> 6);
   const Range range = find_range<false, 256>(fresh(), scratch);
-  CacheJoin join = {0, 0, 0, 0, 0, 0};
+  CacheJoin join = {};
 
   for_segments<false>(range, [&](const Segment &g) {
     const CacheCall &a = fresh();
@@ -638,8 +654,9 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1) void cache_tile
     const dconv_cache_attend_shape &sh = a.sh;
     const Batch &t = a.t;
     const CacheAttendPtrs &p = a.p;
-    const CacheTile &ct = a.ct;
-    const int G = sh.Hq / c.Hkv;
+    const CacheTile &ct = a.tile<false>();
+    const int G = sh.Hq / c.Hkv, sinks = again_scalar(sh.sinks);
+    const float scale2 = __int_as_float(again_scalar(__float_as_int(ct.scale2)));
     const int lane = again_vector(threadIdx.x & 63), D = again_scalar(c.D);
     const int rows = g.s.n * G, r0 = g.tile * kTileRows, start = g.s.start();
     const KeyRange<BN> keys(sh, g.s.len, start + r0 / G, start + (min(r0 + kTileRows, rows) - 1) / G);
@@ -678,20 +695,20 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1) void cache_tile
     CacheSoftmax<T, DP> soft;
     soft.clear();
     auto step = [&](const T *buf, int j0, uint64_t gone) {
-      auto unseen = [&](int v0, int N) { return idle || v0 >= to || (v0 + N <= from && v0 >= sh.sinks); };
+      auto unseen = [&](int v0, int N) { return idle || v0 >= to || (v0 + N <= from && v0 >= sinks); };
       auto masked = [&](int v0, int N) {
-        return gone != 0 || !(v0 + N <= all_to && (v0 >= all_from || v0 + N <= sh.sinks));
+        return gone != 0 || !(v0 + N <= all_to && (v0 >= all_from || v0 + N <= sinks));
       };
-      if constexpr (BN == 64 && sizeof(T) == 2 && DP <= 96) {
+      if constexpr (BN == 64 && sizeof(T) == 2 && (FORMAT == DCONV_CACHE_PLAIN || DP <= 64)) {
         if (!unseen(j0, BN))
-          soft.add_two(rd, buf, buf + BN * DP, q, j0, see, sh.sinks, ct.scale2, masked(j0, BN), lane, gone);
+          soft.add_two(rd, buf, buf + BN * DP, q, j0, see, sinks, scale2, masked(j0, BN), lane, gone);
       } else {
-        // (registers: the scores of a second 32 keys would push out those that copies
-        // and codes of the next tile are on their way to)
+        // (codes of the next tile are on their way to registers: the scores of a second
+        // 32 keys would not fit beside them)
 #pragma unroll
         for (int k = 0; k < BN; k += 32)
           if (!unseen(j0 + k, 32))
-            soft.add(rd, buf + k * DP, buf + (BN + k) * DP, q, j0 + k, see, sh.sinks, ct.scale2, masked(j0 + k, 32), lane,
+            soft.add(rd, buf + k * DP, buf + (BN + k) * DP, q, j0 + k, see, sinks, scale2, masked(j0 + k, 32), lane,
                      (uint32_t)(gone >> k));
       }
     };
@@ -772,7 +789,7 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1) void cache_tile
       }
       if (u0 == 0)
         join = {(int)((g.item + g.work - 1) / range.share) - range.id + 1, range.id, g.b, g.hk, r0,
-                min(kTileRows, rows - r0)};
+                min(kTileRows, rows - r0), g.s};
       return;
     }
     const float inv = see.none ? 0.0f : 1.0f / l;
@@ -815,27 +832,28 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1) void cache_tile
       cache_attend_row<T, FORMAT>(f.c, f.sh, f.t, f.p, g.b, g.s, g.s.row + x / G, g.hk * G + x % G);
     }
   });
-  if (threadIdx.x == 0 && fresh().ct.whole == 0) fresh().ct.joins[range.id] = join;
+  if (threadIdx.x == 0 && fresh().tiles.whole == 0) fresh().tiles.joins[range.id] = join;
 }
 
 // ---------------------------------------------------------------------------
 // Up to 32 rows: each wave takes tiles of 32 keys by itself
 // ---------------------------------------------------------------------------
-template <class T, int DP, int FORMAT, bool ONE>
-__global__ __launch_bounds__(64 * split_waves<T>(DP), split_waves<T>(DP) == 4 ? 2 : 1) void cache_few(
-    const CacheCall) {
+template <class T, int DP>
+struct FewScratch {
+  float ml[split_waves<T>(DP)][64];
+  unsigned again;
+};
+template <class T, int DP, int FORMAT, bool ONE, int LEN>
+__device__ __forceinline__ void few_body(T (&kbuf)[LEN], T (&vbuf)[LEN], RangeScratch &scratch, FewScratch<T, DP> &fs) {
   constexpr int KS = DP / 16, DT = DP / 32, BN = 32, kTile = BN * DP, W = split_waves<T>(DP);
   typedef typename Mma<T>::Frag Frag;
   typedef KeyCodes<T, DP, FORMAT == DCONV_CACHE_PLAIN ? DCONV_CACHE_E4M3 : FORMAT> Codes;
-  __shared__ __align__(16) T kbuf[W * kTile];
-  __shared__ __align__(16) T vbuf[W * kTile];
-  __shared__ float ml[W][64];
-  __shared__ unsigned again;
-  __shared__ RangeScratch scratch;
-  DCONV_POISON(poison_lds(kbuf, W * kTile); poison_lds(vbuf, W * kTile));
+  static_assert(W * kTile <= LEN, "a tile of each wave");
+  float(&ml)[W][64] = fs.ml;
+  unsigned &again = fs.again;
   const int wave = uniform(threadIdx.x >> 6);
   const Range range = find_range<true, 64 * W>(fresh(), scratch);
-  CacheJoin join = {0, 0, 0, 0, 0, 0};
+  CacheJoin join = {};
 
   for_segments<true>(range, [&](const Segment &g) {
     const CacheCall &a = fresh();
@@ -843,8 +861,9 @@ __global__ __launch_bounds__(64 * split_waves<T>(DP), split_waves<T>(DP) == 4 ? 
     const dconv_cache_attend_shape &sh = a.sh;
     const Batch &t = a.t;
     const CacheAttendPtrs &p = a.p;
-    const CacheTile &ct = a.ct;
-    const int G = sh.Hq / c.Hkv;
+    const CacheTile &ct = a.tile<true>();
+    const int G = sh.Hq / c.Hkv, sinks = again_scalar(sh.sinks);
+    const float scale2 = __int_as_float(again_scalar(__float_as_int(ct.scale2)));
     const int lane = again_vector(threadIdx.x & 63), D = again_scalar(c.D);
     const int rows = g.s.n * G, start = g.s.start();
     const KeyRange<BN> keys(sh, g.s.len, start, start + g.s.n - 1);
@@ -880,10 +899,10 @@ __global__ __launch_bounds__(64 * split_waves<T>(DP), split_waves<T>(DP) == 4 ? 
     T *kt = kbuf + wave * kTile, *vt = vbuf + wave * kTile;
     // Scores to probabilities.
     auto weigh = [&](f32x16 &s, int j0, uint32_t gone, Frag(&w)[2]) {
-      if (gone != 0 || !(j0 + BN <= all_to && (j0 >= all_from || j0 + BN <= sh.sinks)))
-        soft.mask(s, j0, see, sh.sinks, lane, gone);
-      soft.follow(s, ct.scale2, [] {});
-      soft.probabilities(s, ct.scale2, w);
+      if (gone != 0 || !(j0 + BN <= all_to && (j0 >= all_from || j0 + BN <= sinks)))
+        soft.mask(s, j0, see, sinks, lane, gone);
+      soft.follow(s, scale2, [] {});
+      soft.probabilities(s, scale2, w);
     };
     // this wave's tiles: u0 W + wave, and every W-th from there
     const int end = min(u1 * W, keys.n);
@@ -936,7 +955,7 @@ __global__ __launch_bounds__(64 * split_waves<T>(DP), split_waves<T>(DP) == 4 ? 
       } else {
         // Codes come into registers, kAhead tiles ahead: keys as operands, values by
         // way of LDS, which turns them.
-        constexpr int kAhead = FORMAT == DCONV_CACHE_E2M1 ? 2 : 1;
+        constexpr int kAhead = FORMAT == DCONV_CACHE_E2M1 && DP <= 128 ? 2 : 1;
         const uint8_t *ksb = p.cache.k_scale + g.hk * c.k_scale_stride[2], *vsb = p.cache.v_scale + g.hk * c.v_scale_stride[2];
         Codes kc[kAhead];
         CodeTiles<T, DP, BN, 64, FORMAT, 1, ONE> vc[kAhead];
@@ -1051,7 +1070,8 @@ __global__ __launch_bounds__(64 * split_waves<T>(DP), split_waves<T>(DP) == 4 ? 
         part[kFewRows * (DP + 1) + lane] = l;
       }
       if (u0 == 0)
-        join = {(int)((g.item + g.work - 1) / range.share) - range.id + 1, range.id, g.b, g.hk, 0, rows};
+        join = {(int)((g.item + g.work - 1) / range.share) - range.id + 1, range.id, g.b, g.hk, 0, rows,
+                g.s};
       __syncthreads();
       return;
     }
@@ -1069,77 +1089,149 @@ __global__ __launch_bounds__(64 * split_waves<T>(DP), split_waves<T>(DP) == 4 ? 
       }
     __syncthreads();
   });
-  if (threadIdx.x == 0 && fresh().ct.whole == 0) fresh().ct.joins[range.id] = join;
+  if (threadIdx.x == 0 && fresh().few.whole == 0) fresh().few.joins[range.id] = join;
+}
+
+// ---------------------------------------------------------------------------
+// The kernels
+// ---------------------------------------------------------------------------
+template <class T, int DP, int FORMAT, bool ONE>
+__global__ __launch_bounds__(64 * split_waves<T>(DP), split_waves<T>(DP) == 4 ? 2 : 1) void cache_few(const CacheCall) {
+  constexpr int N = split_waves<T>(DP) * 32 * DP;
+  __shared__ __align__(16) T buf0[N];
+  __shared__ __align__(16) T buf1[N];
+  __shared__ RangeScratch scratch;
+  __shared__ FewScratch<T, DP> fs;
+  DCONV_POISON(poison_lds(buf0, N); poison_lds(buf1, N));
+  few_body<T, DP, FORMAT, ONE>(buf0, buf1, scratch, fs);
+}
+
+// Both kinds of sequences by the same workgroups, where they have as many waves: a
+// share of the chunks, then one of the single tokens, which alone would be a launch
+// of 21 us for 24 items that take 3 us of each workgroup's time here.
+template <class T, int DP, int FORMAT, bool ONE>
+__global__ __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1) void cache_tiles(const CacheCall) {
+  constexpr int N = 2 * forward_keys<T>(DP) * DP;
+  __shared__ __align__(16) T buf0[N];
+  __shared__ __align__(16) T buf1[N];
+  __shared__ RangeScratch scratch;
+  DCONV_POISON(poison_lds(buf0, N); poison_lds(buf1, N));
+  tiles_body<T, DP, FORMAT, ONE>(buf0, buf1, scratch);
+  if constexpr (split_waves<T>(DP) == 4) {
+    __shared__ FewScratch<T, DP> fs;
+    if (fresh().few.groups == 0) return;
+    __syncthreads();   // the tiles are through with the buffers
+    few_body<T, DP, FORMAT, ONE>(buf0, buf1, scratch, fs);
+  }
 }
 
 // ---------------------------------------------------------------------------
 // Parts joined
 // ---------------------------------------------------------------------------
-// A row by one wave, or, of more than four parts, by four that take every fourth part
-// each: a sum over 64 parts is a chain of 16 loads that miss, in two batches.
+// A row by as many lanes as it has pieces of four floats (or a power of two), so that
+// a wave joins several; and of more than four parts by four waves, each every fourth
+// part.  Four parts are on their way at a time: what it waits for is memory, 84 MB of
+// parts for a call that divides 460 items of 128 rows.
+template <int DP>
+struct JoinLds {
+  float4 o[4][64];
+  float ml[4][64][2];
+};
+template <int DP>
+constexpr int join_lanes() { return DP <= 32 ? 8 : DP <= 64 ? 16 : DP <= 128 ? 32 : 64; }
 template <class T, int DP, int FORMAT, int R>
 __device__ __forceinline__ void join_rows(const dconv_cache &c, const dconv_cache_attend_shape &sh, const Batch &t,
-                                          const CacheAttendPtrs &p, const CacheTile &ct, int id, float (&lds)[4][DP + 1]) {
+                                          const CacheAttendPtrs &p, const CacheTile &ct, int id, JoinLds<DP> &lds) {
   const CacheJoin j = ct.joins[id];
   if (j.parts == 0) return;
-  constexpr int E = (DP + 63) / 64;
-  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), G = sh.Hq / c.Hkv;
-  const Rows s = rows_of(t, p.cache, j.b);
-  // the first part is its workgroup's second one
-  auto part = [&](int i) { return ct.partial + ((int64_t)(j.first + i) * 2 + (i == 0)) * cache_part<R, DP>(); };
-  const bool shared = j.parts > 4;
-  const int first = shared ? wave : 0, step = shared ? 4 : 1;
-  for (int x = shared ? blockIdx.y : blockIdx.y * 4 + wave; x < j.rows; x += (shared ? 1 : 4) * gridDim.y) {
-    const int r = j.r0 + x, row = s.row + r / G, h = j.hk * G + r % G;
-    const bool none = keys_seen(sh, s.len, s.start() + r / G).none();
-    float m = -INFINITY;   // the largest base, parts in the lanes
-    for (int i = lane; i < j.parts; i += 64) m = fmaxf(m, part(i)[R * DP + x]);
-    m = lanes_max<64>(m);
-    const float base = m == -INFINITY ? 0.0f : m;
-    float l = 0.0f, acc[E] = {};
-#pragma unroll 8
-    for (int i = first; i < j.parts; i += step) {
-      const float *from = part(i);
-      const float w = exp2f(from[R * DP + x] - base);
-      l += w * from[R * (DP + 1) + x];
+  constexpr int L = join_lanes<DP>(), kRows = 64 / L;
+  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), G = sh.Hq / c.Hkv, d = lane % L * 4;
+  const bool shared = j.parts > 4, in = d < DP;
+  const int first = shared ? wave : 0, step = shared ? 4 : 1, rows = shared ? kRows : 4 * kRows;
+  for (int x0 = blockIdx.y * rows; x0 < j.rows; x0 += rows * gridDim.y) {
+    const int y = x0 + (shared ? 0 : wave * kRows) + lane / L, x = min(y, j.rows - 1);
+    float m = -INFINITY, l = 0.0f;
+    float4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int i0 = first; i0 < j.parts; i0 += 4 * step) {
+      float pm[4], pl[4];
+      float4 po[4];
 #pragma unroll
-      for (int e = 0; e < E; ++e)
-        if (lane + 64 * e < DP) acc[e] = fmaf(w, from[x * DP + lane + 64 * e], acc[e]);
+      for (int k = 0; k < 4; ++k) {
+        // the first part is its workgroup's second one
+        const int i = min(i0 + k * step, j.parts - 1);
+        const float *part = ct.partial + ((int64_t)(j.first + i) * 2 + (i == 0)) * cache_part<R, DP>();
+        pm[k] = part[R * DP + x];
+        pl[k] = part[R * (DP + 1) + x];
+        po[k] = in ? *reinterpret_cast<const float4 *>(part + x * DP + d) : float4{};
+      }
+      float top = m;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        if (i0 + k * step >= j.parts) pm[k] = -INFINITY, po[k] = float4{}, pl[k] = 0.0f;
+        top = fmaxf(top, pm[k]);
+      }
+      const float base = top == -INFINITY ? 0.0f : top, keep = exp2f(m - base);
+      m = top;
+      l *= keep;
+      acc = {acc.x * keep, acc.y * keep, acc.z * keep, acc.w * keep};
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float w = exp2f(pm[k] - base);
+        l = fmaf(w, pl[k], l);
+        acc = {fmaf(w, po[k].x, acc.x), fmaf(w, po[k].y, acc.y), fmaf(w, po[k].z, acc.z), fmaf(w, po[k].w, acc.w)};
+      }
     }
     if (shared) {   // by the first wave, in the waves' order
-#pragma unroll
-      for (int e = 0; e < E; ++e)
-        if (lane + 64 * e < DP) lds[wave][lane + 64 * e] = acc[e];
-      if (lane == 0) lds[wave][DP] = l;
+      lds.o[wave][lane] = acc;
+      lds.ml[wave][lane][0] = m;
+      lds.ml[wave][lane][1] = l;
       __syncthreads();
-      l = 0.0f;
+      float top = -INFINITY;
 #pragma unroll
-      for (int e = 0; e < E; ++e) acc[e] = 0.0f;
+      for (int w = 0; w < 4; ++w) top = fmaxf(top, lds.ml[w][lane][0]);
+      const float base = top == -INFINITY ? 0.0f : top;
+      m = top;
+      l = 0.0f;
+      acc = float4{};
 #pragma unroll
       for (int w = 0; w < 4; ++w) {
-        l += lds[w][DP];
-#pragma unroll
-        for (int e = 0; e < E; ++e)
-          if (lane + 64 * e < DP) acc[e] += lds[w][lane + 64 * e];
+        const float f = exp2f(lds.ml[w][lane][0] - base);
+        const float4 o = lds.o[w][lane];
+        l = fmaf(f, lds.ml[w][lane][1], l);
+        acc = {fmaf(f, o.x, acc.x), fmaf(f, o.y, acc.y), fmaf(f, o.z, acc.z), fmaf(f, o.w, acc.w)};
       }
       __syncthreads();
       if (wave > 0) continue;
     }
+    const int r = j.r0 + x, row = j.s.row + r / G, h = j.hk * G + r % G;
+    const bool none = keys_seen(sh, j.s.len, j.s.start() + r / G).none();
+    const float o[4] = {acc.x, acc.y, acc.z, acc.w};
+    T out[4];
     bool bad = false;
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-      acc[e] = none ? 0.0f : acc[e] / l;
-      bad |= lane + 64 * e < c.D && !(fabsf(acc[e]) < INFINITY);
+    for (int e = 0; e < 4; ++e) {
+      const float z = none ? 0.0f : o[e] / l;
+      bad |= y < j.rows && d + e < c.D && !(fabsf(z) < INFINITY);
+      out[e] = from_f32<T>(z);
     }
-    if (kSumAgain && __any(bad)) {
-      cache_attend_row<T, FORMAT>(c, sh, t, p, j.b, s, row, h);
-      continue;
-    }
-    T *o = static_cast<T *>(p.out) + row * sh.out_stride[0] + h * sh.out_stride[1];
+    const unsigned long long any = kSumAgain ? __ballot(bad) : 0ull;
+    const bool redo = any >> (lane / L * L) & (L == 64 ? ~0ull : (1ull << (L & 63)) - 1);
+    if (y < j.rows && !redo) {
+      T *to = static_cast<T *>(p.out) + row * sh.out_stride[0] + h * sh.out_stride[1];
+      if (ct.direct && d + 4 <= c.D) {
+        __builtin_memcpy(__builtin_assume_aligned(to + d, 4), out, sizeof(out));
+      } else {
 #pragma unroll
-    for (int e = 0; e < E; ++e)
-      if (lane + 64 * e < c.D) o[lane + 64 * e] = from_f32<T>(acc[e]);
-    if (p.lse && lane == 0) p.lse[(int64_t)row * sh.Hq + h] = none ? -INFINITY : log_sum(m, l);
+        for (int e = 0; e < 4; ++e)
+          if (d + e < c.D) to[d + e] = out[e];
+      }
+      if (p.lse && d == 0) p.lse[(int64_t)row * sh.Hq + h] = none ? -INFINITY : log_sum(m, l);
+    }
+    for (int k = 0; any && k < kRows; ++k) {   // (not finite: see cache_tiles)
+      if (!(any >> (k * L) & (L == 64 ? ~0ull : (1ull << (L & 63)) - 1))) continue;
+      const int z = j.r0 + x0 + (shared ? 0 : wave * kRows) + k;
+      cache_attend_row<T, FORMAT>(c, sh, t, p, j.b, j.s, j.s.row + z / G, j.hk * G + z % G);
+    }
   }
 }
 
@@ -1147,7 +1239,7 @@ __device__ __forceinline__ void join_rows(const dconv_cache &c, const dconv_cach
 template <class T, int DP, int FORMAT>
 __global__ __launch_bounds__(256) void cache_join(const dconv_cache c, const dconv_cache_attend_shape sh, const Batch t,
                                                   const CacheAttendPtrs p, const CacheTile few, const CacheTile tiles) {
-  __shared__ float lds[4][DP + 1];
+  __shared__ JoinLds<DP> lds;
   const int n = few.whole ? 0 : few.groups;
   if ((int)blockIdx.x < n) join_rows<T, DP, FORMAT, kFewRows>(c, sh, t, p, few, blockIdx.x, lds);
   else join_rows<T, DP, FORMAT, kTileRows>(c, sh, t, p, tiles, blockIdx.x - n, lds);
@@ -1174,8 +1266,9 @@ void launch_cache_attend(const dconv_cache &c, const dconv_cache_attend_shape &s
   by_width(plan.dp, [&](auto dp) {
     constexpr int DP = decltype(dp)::value;
     tiles.partial = few.partial + (int64_t)few_joins * 2 * cache_part<kFewRows, DP>();
-    if (plan.few > 0) {
-      const CacheCall call = {c, sh, t, p, few};
+    const CacheCall call = {c, sh, t, p, few, tiles};
+    const bool together = plan.few > 0 && plan.tiles > 0 && split_waves<T>(DP) == 4;
+    if (plan.few > 0 && !together) {
       const dim3 block(64 * split_waves<T>(DP));
       if (plan.near && c.page_size % 32 == 0)
         hipLaunchKernelGGL((cache_few<T, DP, FORMAT, true>), dim3(plan.few), block, 0, s, call);
@@ -1183,14 +1276,19 @@ void launch_cache_attend(const dconv_cache &c, const dconv_cache_attend_shape &s
         hipLaunchKernelGGL((cache_few<T, DP, FORMAT, false>), dim3(plan.few), block, 0, s, call);
     }
     if (plan.tiles > 0) {
-      const CacheCall call = {c, sh, t, p, tiles};
+      CacheCall both = call;
+      if (!together) both.few.groups = 0;
       if (plan.near && c.page_size % forward_keys<T>(DP) == 0)
-        hipLaunchKernelGGL((cache_tiles<T, DP, FORMAT, true>), dim3(plan.tiles), dim3(256), 0, s, call);
+        hipLaunchKernelGGL((cache_tiles<T, DP, FORMAT, true>), dim3(plan.tiles), dim3(256), 0, s, both);
       else
-        hipLaunchKernelGGL((cache_tiles<T, DP, FORMAT, false>), dim3(plan.tiles), dim3(256), 0, s, call);
+        hipLaunchKernelGGL((cache_tiles<T, DP, FORMAT, false>), dim3(plan.tiles), dim3(256), 0, s, both);
     }
+    // rows of an item, by steps of a workgroup
+    const int step = 64 / join_lanes<DP>(), G = sh.Hq / c.Hkv;
+    const int rows = plan.tiles > 0 ? kTileRows : sh.max_rows > 0 && sh.max_rows < kFewRows / G ? sh.max_rows * G : kFewRows;
+    const int steps = plan.tiles > 0 ? rows / (4 * step) : (rows + step - 1) / step;
     if (few_joins + tile_joins > 0)
-      hipLaunchKernelGGL((cache_join<T, DP, FORMAT>), dim3(few_joins + tile_joins, tile_joins > 0 ? 16 : 8), dim3(256), 0,
+      hipLaunchKernelGGL((cache_join<T, DP, FORMAT>), dim3(few_joins + tile_joins, steps < 16 ? steps : 16), dim3(256), 0,
                          s, c, sh, t, p, few, tiles);
   });
 }
