@@ -34,6 +34,33 @@ struct __attribute__((packed, aligned(1))) Codes {
   uint32_t w[N];
 };
 
+// The first n elements of a piece (zeros past them).
+template <class T>
+__device__ __forceinline__ Piece<T> load_piece(const T *p, int n) {
+  Piece<T> a;
+  if (n == kPiece) return *reinterpret_cast<const Piece<T> *>(p);
+#pragma unroll
+  for (int e = 0; e < kPiece; ++e) a.x[e] = e < n ? p[e] : from_f32<T>(0.0f);
+  return a;
+}
+template <class T>
+__device__ __forceinline__ void store_piece(T *p, const Piece<T> &a, int n) {
+  if (n == kPiece) {
+#if VAR_NT
+    typedef uint32_t u32x4 __attribute__((ext_vector_type(4), aligned(4)));
+    u32x4 w[sizeof(a) / 16];
+    __builtin_memcpy(w, &a, sizeof(a));
+    for (unsigned i = 0; i < sizeof(a) / 16; ++i) __builtin_nontemporal_store(w[i], reinterpret_cast<u32x4 *>(p) + i);
+    return;
+#endif
+    *reinterpret_cast<Piece<T> *>(p) = a;
+    return;
+  }
+#pragma unroll
+  for (int e = 0; e < kPiece; ++e)
+    if (e < n) p[e] = a.x[e];
+}
+
 // Where piece c of the workgroup's is: in the rows, and in the cache.
 struct Spot {
   int page, n;             // page or kNowhere, kNoRow; elements
@@ -58,17 +85,34 @@ __device__ __forceinline__ Spot spot_of(const dconv_cache &c, const Walk &w, con
   return s;
 }
 
-// Pages and slots of a workgroup's rows, into LDS.
-__device__ __forceinline__ void find_rows(const Batch &t, const CachePtrs &p, int r0, int rows, int2 *at) {
+// Pages and slots of a workgroup's rows, into LDS.  Offsets and lengths come there
+// first, all at once: looked up one by one in memory they would be a chain of loads
+// that miss (17 us for a call whose bytes take 1).
+constexpr int kFewSequences = 512;
+struct Lookup {
+  int offsets[kFewSequences + 1], lengths[kFewSequences];
+  int2 at[kMostRows];
+};
+__device__ __forceinline__ void find_rows(const Batch &t, const CachePtrs &p, int r0, int rows, Lookup &lds) {
+  CachePtrs q = p;
+  if (p.offsets && t.B <= kFewSequences) {
+    for (int b = threadIdx.x; b <= t.B; b += 256) {
+      lds.offsets[b] = p.offsets[b];
+      if (b < t.B) lds.lengths[b] = p.lengths[b];
+    }
+    __syncthreads();
+    q.offsets = lds.offsets;
+    q.lengths = lds.lengths;
+  }
   for (int r = threadIdx.x; r < rows; r += 256) {
-    const int b = sequence_of(t, p, r0 + r);
+    const int b = sequence_of(t, q, r0 + r);
     int2 s = {kNoRow, 0};
     if (b >= 0) {
-      const Rows q = rows_of(t, p, b);
-      const int i = q.start() + (r0 + r - q.row);
-      s.x = i < 0 || i >= q.len ? kNowhere : page_of(t, p, b, i, &s.y);
+      const Rows n = rows_of(t, q, b);
+      const int i = n.start() + (r0 + r - n.row);
+      s.x = i < 0 || i >= n.len ? kNowhere : page_of(t, p, b, i, &s.y);
     }
-    at[r] = s;
+    lds.at[r] = s;
   }
   __syncthreads();
 }
@@ -121,31 +165,44 @@ __device__ __forceinline__ Codes<FORMAT == DCONV_CACHE_E4M3 ? 2 : 1> encode(cons
   return out;
 }
 
-// One step for each piece of eight elements.
+// A thread's pieces, kBatch on their way at a time.
+#ifndef VAR_BATCH
+#define VAR_BATCH 4
+#endif
+#ifndef VAR_NT
+#define VAR_NT 0
+#endif
+constexpr int kBatch = VAR_BATCH;
+
 template <class T, int FORMAT>
 __global__ __launch_bounds__(256) void cache_write(const dconv_cache c, const Batch t, const CachePtrs p, const Walk w,
                                                    const RowPtrs from) {
-  __shared__ int2 at[kMostRows];
-  const int r0 = blockIdx.x * w.rows, rows = min(w.rows, t.N - r0);
-  find_rows(t, p, r0, rows, at);
-  for (int x = threadIdx.x; x < rows * w.per_row; x += 256) {
-    const Spot s = spot_of(c, w, at, r0, (uint32_t)x);
-    if (s.page < 0) continue;
-    const T *in = static_cast<const T *>(s.value ? from.v : from.k) + s.row;
-    Piece<T> a = {};
-    if (s.n == kPiece) a = *reinterpret_cast<const Piece<T> *>(in);
-    else
-      for (int e = 0; e < s.n; ++e) a.x[e] = in[e];
-    if constexpr (FORMAT == DCONV_CACHE_PLAIN) {
-      T *to = static_cast<T *>(s.value ? p.v : p.k) + s.kept;
-      if (s.n == kPiece) *reinterpret_cast<Piece<T> *>(to) = a;
-      else
-        for (int e = 0; e < s.n; ++e) to[e] = a.x[e];
-    } else {
-      const uint32_t scale = scale_for<T, FORMAT>(block_top(a));
-      const auto code = encode<T, FORMAT>(a, scale);
-      *reinterpret_cast<decltype(encode<T, FORMAT>(a, scale)) *>(static_cast<uint8_t *>(s.value ? p.v : p.k) + s.kept) = code;
-      if ((x & 3) == 0) (s.value ? p.v_scale : p.k_scale)[s.scale] = (uint8_t)scale;
+  __shared__ Lookup lds;
+  const int r0 = blockIdx.x * w.rows, rows = min(w.rows, t.N - r0), n = rows * w.per_row;
+  find_rows(t, p, r0, rows, lds);
+  for (int x0 = threadIdx.x; x0 < n; x0 += kBatch * 256) {
+    Spot s[kBatch];
+    Piece<T> a[kBatch] = {};
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+      s[i].page = kNoRow;
+      if (x0 + i * 256 >= n) continue;
+      s[i] = spot_of(c, w, lds.at, r0, (uint32_t)(x0 + i * 256));
+      if (s[i].page < 0) continue;
+      a[i] = load_piece(static_cast<const T *>(s[i].value ? from.v : from.k) + s[i].row, s[i].n);
+    }
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+      if (s[i].page < 0) continue;
+      if constexpr (FORMAT == DCONV_CACHE_PLAIN) {
+        store_piece(static_cast<T *>(s[i].value ? p.v : p.k) + s[i].kept, a[i], s[i].n);
+      } else {
+        const uint32_t scale = scale_for<T, FORMAT>(block_top(a[i]));
+        const auto code = encode<T, FORMAT>(a[i], scale);
+        *reinterpret_cast<decltype(encode<T, FORMAT>(a[i], scale)) *>(
+            static_cast<uint8_t *>(s[i].value ? p.v : p.k) + s[i].kept) = code;
+        if ((threadIdx.x & 3) == 0) (s[i].value ? p.v_scale : p.k_scale)[s[i].scale] = (uint8_t)scale;
+      }
     }
   }
 }
@@ -153,31 +210,42 @@ __global__ __launch_bounds__(256) void cache_write(const dconv_cache c, const Ba
 template <class T, int FORMAT>
 __global__ __launch_bounds__(256) void cache_read(const dconv_cache c, const Batch t, const CachePtrs p, const Walk w,
                                                   const RowPtrs to) {
-  __shared__ int2 at[kMostRows];
-  const int r0 = blockIdx.x * w.rows, rows = min(w.rows, t.N - r0);
-  find_rows(t, p, r0, rows, at);
-  for (int x = threadIdx.x; x < rows * w.per_row; x += 256) {
-    const Spot s = spot_of(c, w, at, r0, (uint32_t)x);
-    if (s.page == kNoRow) continue;
-    Piece<T> a = {};
-    if (s.page >= 0) {
-      if constexpr (FORMAT == DCONV_CACHE_PLAIN) {
-        const T *in = static_cast<const T *>(s.value ? p.v : p.k) + s.kept;
-        if (s.n == kPiece) a = *reinterpret_cast<const Piece<T> *>(in);
-        else
-          for (int e = 0; e < s.n; ++e) a.x[e] = in[e];
-      } else {
-        constexpr int kWords = FORMAT == DCONV_CACHE_E4M3 ? 2 : 1, kPairs = codes_per_word<FORMAT>() / 2;
-        const auto code = *reinterpret_cast<const Codes<kWords> *>(static_cast<const uint8_t *>(s.value ? p.v : p.k) + s.kept);
-        const float scale = scale_of((s.value ? p.v_scale : p.k_scale)[s.scale]);
+  constexpr bool kCodes = FORMAT != DCONV_CACHE_PLAIN;
+  constexpr int kWords = FORMAT == DCONV_CACHE_E2M1 ? 1 : 2, kPairs = kCodes ? codes_per_word<FORMAT>() / 2 : 2;
+  __shared__ Lookup lds;
+  const int r0 = blockIdx.x * w.rows, rows = min(w.rows, t.N - r0), n = rows * w.per_row;
+  find_rows(t, p, r0, rows, lds);
+  for (int x0 = threadIdx.x; x0 < n; x0 += kBatch * 256) {
+    Spot s[kBatch];
+    Piece<T> a[kBatch] = {};
+    Codes<kWords> code[kBatch];
+    uint32_t scale[kBatch];
 #pragma unroll
-        for (int i = 0; i < kPiece / 2; ++i) decode_pair<T, FORMAT>(code.w[i / kPairs], i % kPairs, scale, a.x + 2 * i);
+    for (int i = 0; i < kBatch; ++i) {
+      s[i].page = kNoRow;
+      if (x0 + i * 256 >= n) continue;
+      s[i] = spot_of(c, w, lds.at, r0, (uint32_t)(x0 + i * 256));
+      if (s[i].page < 0) continue;
+      const void *kept = s[i].value ? p.v : p.k;
+      if constexpr (kCodes) {
+        code[i] = *reinterpret_cast<const Codes<kWords> *>(static_cast<const uint8_t *>(kept) + s[i].kept);
+        scale[i] = (s[i].value ? p.v_scale : p.k_scale)[s[i].scale];
+      } else {
+        a[i] = load_piece(static_cast<const T *>(kept) + s[i].kept, s[i].n);
       }
     }
-    T *out = static_cast<T *>(s.value ? to.v : to.k) + s.row;
-    if (s.n == kPiece) *reinterpret_cast<Piece<T> *>(out) = a;
-    else
-      for (int e = 0; e < s.n; ++e) out[e] = a.x[e];
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+      if (s[i].page == kNoRow) continue;
+      if constexpr (kCodes) {
+        if (s[i].page >= 0) {
+#pragma unroll
+          for (int e = 0; e < kPiece / 2; ++e)
+            decode_pair<T, FORMAT>(code[i].w[e / kPairs], e % kPairs, scale_of(scale[i]), a[i].x + 2 * e);
+        }
+      }
+      store_piece(static_cast<T *>(s[i].value ? to.v : to.k) + s[i].row, a[i], s[i].n);
+    }
   }
 }
 

@@ -95,9 +95,10 @@ __device__ void cache_attend_row(const dconv_cache &c, const dconv_cache_attend_
 }
 
 // Rows of one key head that are joined from parts: its sums are those that `parts`
-// workgroups from `first` on have left.
+// workgroups from `first` on have left.  Each of them joins a share of the rows, this
+// the index-th; two such of every workgroup, as for its parts.
 struct CacheJoin {
-  int parts, first;
+  int parts, first, index;
   int b, hk, r0, rows;   // rows r0 .. of the key head's
   Rows s;
 };

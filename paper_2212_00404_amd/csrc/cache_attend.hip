@@ -51,18 +51,20 @@ CachePlan plan_attend(const dconv_cache &c, const dconv_cache_attend_shape &sh, 
     const int64_t n = (work + least - 1) / least;
     return (int)(n < 1 ? 1 : n < most ? n : most);
   };
-  f.few_least = 256;
-  f.tiles_least = 512;
+  // (fp32 takes sixteen times as long for the products of as many keys)
+  f.few_least = es == 4 ? 128 : 256;
+  f.tiles_least = es == 4 ? 96 : 512;
+  const int whole = es == 4 ? 256 : 512;
   if (!even || rows <= 32) {
     f.few = groups(f.dp * es <= 256 ? 512 : 256, heads * (keys + 64), f.few_least);
     // tables of a few steps of a workgroup: nothing is divided, and nothing joined
-    if (keys <= 512 && heads < (1 << 20)) f.few_whole = 1, f.few = (int)heads;
+    if (keys <= whole && heads < (1 << 20)) f.few_whole = 1, f.few = (int)heads;
   }
   if (rows > 32) {
     const int64_t tiles = ((int64_t)sh.N * G / 128 + sh.B) * c.Hkv;
     f.tiles = groups(f.dp * es <= 256 ? 512 : 256, tiles * (keys + 64), f.tiles_least);
     const int64_t each = (rows + 127) / 128;
-    if (even && keys <= 512 && heads * each < (1 << 20)) f.tiles_whole = (int)each, f.tiles = (int)(heads * each);
+    if (even && keys <= whole && heads * each < (1 << 20)) f.tiles_whole = (int)each, f.tiles = (int)(heads * each);
   }
   // one launch for both kinds (cache_tiles): as many workgroups, and shares of both
   if (f.few > 0 && f.tiles > 0 && f.dp * es <= 256) {
@@ -70,7 +72,7 @@ CachePlan plan_attend(const dconv_cache &c, const dconv_cache_attend_shape &sh, 
     f.few = f.tiles = std::max(std::min(f.few, 512), f.tiles);
   }
   const int64_t few = f.few_whole ? 0 : f.few, tiles = f.tiles_whole ? 0 : f.tiles;
-  f.joins_bytes = ((few + tiles) * (int64_t)sizeof(CacheJoin) + 15) / 16 * 16;
+  f.joins_bytes = ((few + tiles) * 2 * (int64_t)sizeof(CacheJoin) + 15) / 16 * 16;
   f.workspace = f.joins_bytes + (few * 32 + tiles * 128) * 2 * (f.dp + 2) * 4;
   return f;
 }

@@ -2,6 +2,12 @@
 // running softmax of attend_mma.h over tiles of keys whose places a table gives.
 // Instantiated per type and format in cache_attend_*.hip.
 #pragma once
+#ifndef VAR_QREG
+#define VAR_QREG 0
+#endif
+#ifndef VAR_AHEAD
+#define VAR_AHEAD 2
+#endif
 
 #include "attend_mma.h"
 #include "cache_attend.h"
@@ -16,7 +22,7 @@ struct CacheTile {
   int groups, least;    // workgroups, the least work of one
   int whole;            // tiles per sequence and key head, one for each workgroup; 0: by work
   float *partial;       // two parts of each workgroup's
-  CacheJoin *joins;     // one of each workgroup's
+  CacheJoin *joins;     // and two joins
 };
 
 // A kernel's one argument.  What it holds is read from the argument's own memory
@@ -205,7 +211,7 @@ struct CodeTiles {
     const bool whole = ONE && keys.whole(j0);
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
-      const int u = i * NT + thread, row = row_of(u), blk = block_of(u);
+      const int u = has(i * NT + thread) ? i * NT + thread : kAll - 1, row = row_of(u), blk = block_of(u);
       bool value = TENSORS == 1 || u >= kTensor;
       if constexpr (TENSORS == 1 || kTensor % 64 == 0) value = uniform(value);   // a wave's are of one tensor
       const char *from;
@@ -225,11 +231,12 @@ struct CodeTiles {
         from = (value ? v + av : k + ak) + blk * (kWords * 4);
         sfrom = (value ? vs + sv : ks + sk) + blk;
       }
-      raw[i] = {};
-      scale[i] = 0;
-      if (has(u) && blk * kBlock < D) {
+      if (DP <= 128 || blk * kBlock < D) {   // (up to 128 a head is as long as it is padded to)
         raw[i] = *reinterpret_cast<const RawCodes<kWords> *>(from);
         scale[i] = *sfrom;
+      } else {
+        raw[i] = {};
+        scale[i] = 0;
       }
     }
   }
@@ -268,11 +275,12 @@ struct KeyCodes {
   __device__ __forceinline__ void load(const char *row, const uint8_t *scales, int D, int half) {
 #pragma unroll
     for (int b = 0; b < kBlocks; ++b) {
-      raw[b] = {};
-      scale[b] = 0;
-      if (b * kBlock < D) {
+      if (DP <= 128 || b * kBlock < D) {
         raw[b] = *reinterpret_cast<const RawCodes<kWords> *>(row + (2 * b + half) * (kWords * 4));
         scale[b] = scales[b];
+      } else {
+        raw[b] = {};
+        scale[b] = 0;
       }
     }
   }
@@ -516,6 +524,7 @@ __device__ __forceinline__ Range find_range(const CacheCall &a, RangeScratch &ld
     Range r = {};
     r.id = xcd_remap(blockIdx.x, ct.groups);
     r.b = r.id / (c.Hkv * ct.whole);
+    r.end = 1;
     return r;
   }
   const int per = (t.B + NT - 1) / NT, b0 = min(tid * per, t.B), b1 = min(b0 + per, t.B);
@@ -577,6 +586,10 @@ __device__ __forceinline__ int again_vector(int x) {
   return x;
 }
 
+// Nothing moves across: conversions and loads of several tiles at once do not fit the
+// registers.
+__device__ __forceinline__ void phase() { __builtin_amdgcn_sched_barrier(0); }
+
 // A segment of an item: from `pos` to `end` of its work.
 struct Segment {
   int b, hk, tile;
@@ -592,18 +605,23 @@ __device__ __forceinline__ int cut(int64_t pos, int64_t work, int steps, int64_t
   return (int)(pos * steps / work);
 }
 
+// The join of a segment's item, of which the segment's workgroup has a part.
+__device__ __forceinline__ CacheJoin join_of(const Range &r, const Segment &g, int steps, int r0, int rows) {
+  int first = (int)(g.item / r.share), upto;   // (or one after it, where its cut has gone to the item's beginning)
+  while ((upto = cut(min((first + 1) * r.share - g.item, g.work), g.work, steps, r.share)) == 0 && first < r.id) ++first;
+  if (upto == steps) return {};                // the first has done all of it: a cut has gone to the item's end
+  return {(int)((g.item + g.work - 1) / r.share) - first + 1, first, r.id - first, g.b, g.hk, r0, rows, g.s};
+}
+
+// A workgroup's records of joins, until a segment has one.
+template <bool FEW>
+__device__ __forceinline__ void no_joins(const Range &r) {
+  const CacheTile &ct = fresh().tile<FEW>();
+  if (threadIdx.x == 0 && ct.whole == 0) ct.joins[2 * r.id].parts = ct.joins[2 * r.id + 1].parts = 0;
+}
+
 template <bool FEW, class F>
 __device__ __forceinline__ void for_segments(const Range &r, F f) {
-  if (fresh().tile<FEW>().whole > 0) {
-    const CacheCall &a = fresh();
-    const int whole = a.tile<FEW>().whole;
-    Rows s = rows_of(a.t, a.p.cache, r.b);
-    s = {uniform(s.row), uniform(s.n), uniform(s.len)};
-    const Work<FEW> w(a.sh, a.sh.Hq / a.c.Hkv, s, most_rows(a));
-    const int tile = r.id % whole;
-    if (tile < w.tiles) f(Segment{r.b, r.id / whole % a.c.Hkv, tile, s, 0, 1, 1, 0});
-    return;
-  }
   int64_t x = r.begin, at = r.at;
   for (int b = r.b; x < r.end; ++b) {
     const CacheCall &a = fresh();
@@ -612,10 +630,16 @@ __device__ __forceinline__ void for_segments(const Range &r, F f) {
     Rows s = rows_of(a.t, a.p.cache, b);
     s = {uniform(s.row), uniform(s.n), uniform(s.len)};
     const Work<FEW> w(a.sh, G, s, most_rows(a));
+    const int whole = a.tile<FEW>().whole;
+    int hk = 0, tile = 0;
+    if (whole > 0) {   // one item, as if it were the line
+      tile = r.id % whole;
+      hk = r.id / whole % heads;
+      if (tile >= w.tiles) break;
+    }
     if (w.tiles == 0) continue;
     const int64_t head = w.before(w.tiles);
-    int hk = 0, tile = 0;
-    if (at > 0) {
+    if (whole == 0 && at > 0) {
       hk = (int)(at / head);
       at -= hk * head;
       tile = w.at(at);
@@ -623,7 +647,7 @@ __device__ __forceinline__ void for_segments(const Range &r, F f) {
     }
     for (; hk < heads && x < r.end; ++hk, tile = 0)
       for (; tile < w.tiles && x < r.end; ++tile) {
-        Segment g = {b, uniform(hk), uniform(tile), s, at, 0, w.of(tile), x - at};
+        Segment g = {b, uniform(hk), uniform(tile), s, at, 0, whole > 0 ? 1 : w.of(tile), x - at};
         g.end = min(g.work, at + (r.end - x));
         f(g);
         x += g.end - at;
@@ -646,7 +670,7 @@ __device__ __forceinline__ void tiles_body(T (&buf0)[LEN], T (&buf1)[LEN], Range
   static_assert(2 * BN * DP <= LEN, "a tile's keys and values");
   const int wave = uniform(threadIdx.x >> 6);
   const Range range = find_range<false, 256>(fresh(), scratch);
-  CacheJoin join = {};
+  no_joins<false>(range);
 
   for_segments<false>(range, [&](const Segment &g) {
     const CacheCall &a = fresh();
@@ -787,9 +811,7 @@ __device__ __forceinline__ void tiles_body(T (&buf0)[LEN], T (&buf1)[LEN], Range
         part[kTileRows * DP + x] = soft.m;
         part[kTileRows * (DP + 1) + x] = l;
       }
-      if (u0 == 0)
-        join = {(int)((g.item + g.work - 1) / range.share) - range.id + 1, range.id, g.b, g.hk, r0,
-                min(kTileRows, rows - r0), g.s};
+      if (threadIdx.x == 0) fresh().tiles.joins[2 * range.id + (u0 == 0)] = join_of(range, g, keys.n, r0, min(kTileRows, rows - r0));
       return;
     }
     const float inv = see.none ? 0.0f : 1.0f / l;
@@ -832,7 +854,6 @@ __device__ __forceinline__ void tiles_body(T (&buf0)[LEN], T (&buf1)[LEN], Range
       cache_attend_row<T, FORMAT>(f.c, f.sh, f.t, f.p, g.b, g.s, g.s.row + x / G, g.hk * G + x % G);
     }
   });
-  if (threadIdx.x == 0 && fresh().tiles.whole == 0) fresh().tiles.joins[range.id] = join;
 }
 
 // ---------------------------------------------------------------------------
@@ -853,7 +874,7 @@ __device__ __forceinline__ void few_body(T (&kbuf)[LEN], T (&vbuf)[LEN], RangeSc
   unsigned &again = fs.again;
   const int wave = uniform(threadIdx.x >> 6);
   const Range range = find_range<true, 64 * W>(fresh(), scratch);
-  CacheJoin join = {};
+  no_joins<true>(range);
 
   for_segments<true>(range, [&](const Segment &g) {
     const CacheCall &a = fresh();
@@ -882,12 +903,27 @@ __device__ __forceinline__ void few_body(T (&kbuf)[LEN], T (&vbuf)[LEN], RangeSc
       all_to = min(all_to, __shfl_xor(all_to, x));
     }
     all_from = uniform(all_from), all_to = uniform(all_to);
-    Frag q[KS];
+    // Beside codes on their way there are no registers for the queries: they are
+    // operands from LDS, where plain keys would be.
+    Frag q[FORMAT == DCONV_CACHE_PLAIN || VAR_QREG ? KS : 1];
     const T *qrow = static_cast<const T *>(p.q) + row * sh.q_stride[0] + h * sh.q_stride[1];
+    const uint32_t qb = r * Reader<T, DP>::kRow, qx = ((2 * (lane >> 5)) ^ Tile<T, DP>::swizzle(r)) * Reader<T, DP>::kChunk;
+    auto query = [&](uint32_t b, uint32_t x, int k) {   // elements order_of(k, lane / 32) .. + 7 of the lane's row
+      return reinterpret_cast<char *>(kbuf) + ((x ^ (4 * (k / 2) + (k & 1)) * Reader<T, DP>::kChunk) + b);
+    };
+    if constexpr (FORMAT == DCONV_CACHE_PLAIN) {
 #pragma unroll
-    for (int k = 0; k < KS; ++k)
-      q[k] = load_frag(qrow, FORMAT == DCONV_CACHE_PLAIN ? 16 * k + 8 * (lane >> 5) : Codes::order_of(k, lane >> 5), D,
-                       ct.direct, ct.sign);
+      for (int k = 0; k < KS; ++k) q[k] = load_frag(qrow, 16 * k + 8 * (lane >> 5), D, ct.direct, ct.sign);
+    } else if constexpr (VAR_QREG) {
+#pragma unroll
+      for (int k = 0; k < KS; ++k) q[k] = load_frag(qrow, Codes::order_of(k, lane >> 5), D, ct.direct, ct.sign);
+    } else {
+      for (int k = wave; k < KS; k += W) {
+        const Frag f = load_frag(qrow, Codes::order_of(k, lane >> 5), D, ct.direct, ct.sign);
+        __builtin_memcpy(__builtin_assume_aligned(query(qb, qx, k), 16), &f, sizeof(f));
+      }
+      __syncthreads();
+    }
 
     const Finder<T, FORMAT, BN, ONE> finder = {p.cache.table + g.b * t.table_stride, t.page, t.pages};
     const int64_t es = Finder<T, FORMAT, BN, ONE>::kBytes;
@@ -955,14 +991,17 @@ __device__ __forceinline__ void few_body(T (&kbuf)[LEN], T (&vbuf)[LEN], RangeSc
       } else {
         // Codes come into registers, kAhead tiles ahead: keys as operands, values by
         // way of LDS, which turns them.
-        constexpr int kAhead = FORMAT == DCONV_CACHE_E2M1 && DP <= 128 ? 2 : 1;
+        constexpr int kAhead = DP <= 128 && sizeof(T) == 2 ? VAR_AHEAD : 1;
         const uint8_t *ksb = p.cache.k_scale + g.hk * c.k_scale_stride[2], *vsb = p.cache.v_scale + g.hk * c.v_scale_stride[2];
         Codes kc[kAhead];
         CodeTiles<T, DP, BN, 64, FORMAT, 1, ONE> vc[kAhead];
         uint32_t gone[kAhead];
+        // (past the last tile it comes again: loads under a condition would be waited for
+        // one and all, as the compiler cannot count them)
+        const int last = u + (end - 1 - u) / W * W;
         auto load = [&](int i, int v) {   // tile v, whose places have been asked for
           const Found f = finder.find(c, asked);
-          if (v + W < end) asked = finder.ask(keys, keys.start(v + W));
+          asked = finder.ask(keys, keys.start(min(v + W, last)));
           const int j0 = keys.start(v), r = lane & 31;
           const uint32_t key = ONE ? keys.whole(j0) ? r : keys.key(j0, j0 + r) - j0 : 0;   // (else its place is the lane's)
           kc[i].load(kb + f.k + key * (uint32_t)c.k_stride[1], ksb + f.ks + key * (uint32_t)c.k_scale_stride[1], D, lane >> 5);
@@ -970,24 +1009,34 @@ __device__ __forceinline__ void few_body(T (&kbuf)[LEN], T (&vbuf)[LEN], RangeSc
           gone[i] = (uint32_t)f.gone;
         };
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i)
-          if (u + i * W < end) load(i, u + i * W);
+        for (int i = 0; i < kAhead; ++i) load(i, min(u + i * W, last));
         for (; u < end; u += kAhead * W) {
 #pragma unroll
           for (int i = 0; i < kAhead; ++i) {
-            const int v = u + i * W;
-            if (v >= end) break;
+            const int v = u + i * W;   // (past the last tile: nobody sees it)
             Reader<T, DP> rd = reader;
             rd.again();
+            uint32_t xb = qb, xx = qx;
+            asm volatile("" : "+v"(xb), "+v"(xx));
             f32x16 s = {};
+            phase();
 #pragma unroll
-            for (int k = 0; k < KS; ++k) s = Mma<T>::mac(kc[i].frag(k), q[k], s);
+            for (int k = 0; k < KS; ++k) {
+              Frag f;
+              if constexpr (VAR_QREG) f = q[k];
+              else __builtin_memcpy(&f, __builtin_assume_aligned(query(xb, xx, k), 16), sizeof(f));
+              s = Mma<T>::mac(kc[i].frag(k), f, s);
+            }
+            phase();
             vc[i].store(vt, vt, lane);
-            const uint32_t now = gone[i];
-            if (v + kAhead * W < end) load(i, v + kAhead * W);
+            phase();
+            const uint32_t now = v > last ? ~0u : gone[i];
+            load(i, min(v + kAhead * W, last));
+            phase();
             Frag w[2];
-            weigh(s, keys.start(v), now, w);
+            weigh(s, keys.start(min(v, last)), now, w);
             soft.values(rd, vt, 0, w);
+            phase();
           }
         }
       }
@@ -1069,9 +1118,7 @@ __device__ __forceinline__ void few_body(T (&kbuf)[LEN], T (&vbuf)[LEN], RangeSc
         part[kFewRows * DP + lane] = m;
         part[kFewRows * (DP + 1) + lane] = l;
       }
-      if (u0 == 0)
-        join = {(int)((g.item + g.work - 1) / range.share) - range.id + 1, range.id, g.b, g.hk, 0, rows,
-                g.s};
+      if (threadIdx.x == 0) fresh().few.joins[2 * range.id + (u0 == 0)] = join_of(range, g, steps, 0, rows);
       __syncthreads();
       return;
     }
@@ -1089,7 +1136,6 @@ __device__ __forceinline__ void few_body(T (&kbuf)[LEN], T (&vbuf)[LEN], RangeSc
       }
     __syncthreads();
   });
-  if (threadIdx.x == 0 && fresh().few.whole == 0) fresh().few.joins[range.id] = join;
 }
 
 // ---------------------------------------------------------------------------
@@ -1129,13 +1175,15 @@ __global__ __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1) void cache_tile
 // Parts joined
 // ---------------------------------------------------------------------------
 // A row by as many lanes as it has pieces of four floats (or a power of two), so that
-// a wave joins several; and of more than four parts by four waves, each every fourth
-// part.  Four parts are on their way at a time: what it waits for is memory, 84 MB of
-// parts for a call that divides 460 items of 128 rows.
+// a wave joins several; and where parts are many beside the rows by eight waves, each
+// every eighth part.  Four parts are on their way at a time: what it waits for is memory.  (Waves
+// start at some 1.7 per nanosecond: a workgroup for every few rows of every workgroup's
+// parts, most of which have nothing to do, took 30 us.)
+constexpr int kJoinWaves = 8;
 template <int DP>
 struct JoinLds {
-  float4 o[4][64];
-  float ml[4][64][2];
+  float4 o[kJoinWaves][64];
+  float ml[kJoinWaves][64][2];
 };
 template <int DP>
 constexpr int join_lanes() { return DP <= 32 ? 8 : DP <= 64 ? 16 : DP <= 128 ? 32 : 64; }
@@ -1146,9 +1194,13 @@ __device__ __forceinline__ void join_rows(const dconv_cache &c, const dconv_cach
   if (j.parts == 0) return;
   constexpr int L = join_lanes<DP>(), kRows = 64 / L;
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), G = sh.Hq / c.Hkv, d = lane % L * 4;
-  const bool shared = j.parts > 4, in = d < DP;
-  const int first = shared ? wave : 0, step = shared ? 4 : 1, rows = shared ? kRows : 4 * kRows;
-  for (int x0 = blockIdx.y * rows; x0 < j.rows; x0 += rows * gridDim.y) {
+  const int share = (j.rows + j.parts - 1) / j.parts;
+  // the way with fewer loads one after another
+  const bool in = d < DP, shared = (share + kRows - 1) / kRows * ((j.parts + 4 * kJoinWaves - 1) / (4 * kJoinWaves)) <
+                                   (share + kJoinWaves * kRows - 1) / (kJoinWaves * kRows) * ((j.parts + 3) / 4);
+  const int first = shared ? wave : 0, step = shared ? kJoinWaves : 1, rows = shared ? kRows : kJoinWaves * kRows;
+  const int from = share * j.index, to = min(from + share, j.rows);
+  for (int x0 = from; x0 < to; x0 += rows) {
     const int y = x0 + (shared ? 0 : wave * kRows) + lane / L, x = min(y, j.rows - 1);
     float m = -INFINITY, l = 0.0f;
     float4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -1186,44 +1238,46 @@ __device__ __forceinline__ void join_rows(const dconv_cache &c, const dconv_cach
       lds.ml[wave][lane][0] = m;
       lds.ml[wave][lane][1] = l;
       __syncthreads();
-      float top = -INFINITY;
-#pragma unroll
-      for (int w = 0; w < 4; ++w) top = fmaxf(top, lds.ml[w][lane][0]);
-      const float base = top == -INFINITY ? 0.0f : top;
-      m = top;
-      l = 0.0f;
-      acc = float4{};
-#pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        const float f = exp2f(lds.ml[w][lane][0] - base);
-        const float4 o = lds.o[w][lane];
-        l = fmaf(f, lds.ml[w][lane][1], l);
-        acc = {fmaf(f, o.x, acc.x), fmaf(f, o.y, acc.y), fmaf(f, o.z, acc.z), fmaf(f, o.w, acc.w)};
+      if (wave == 0) {
+        const int n = min(j.parts, kJoinWaves);
+        float top = -INFINITY;
+        for (int w = 0; w < n; ++w) top = fmaxf(top, lds.ml[w][lane][0]);
+        const float base = top == -INFINITY ? 0.0f : top;
+        m = top;
+        l = 0.0f;
+        acc = float4{};
+#pragma unroll 4
+        for (int w = 0; w < n; ++w) {
+          const float f = exp2f(lds.ml[w][lane][0] - base);
+          const float4 o = lds.o[w][lane];
+          l = fmaf(f, lds.ml[w][lane][1], l);
+          acc = {fmaf(f, o.x, acc.x), fmaf(f, o.y, acc.y), fmaf(f, o.z, acc.z), fmaf(f, o.w, acc.w)};
+        }
       }
       __syncthreads();
       if (wave > 0) continue;
     }
     const int r = j.r0 + x, row = j.s.row + r / G, h = j.hk * G + r % G;
     const bool none = keys_seen(sh, j.s.len, j.s.start() + r / G).none();
-    const float o[4] = {acc.x, acc.y, acc.z, acc.w};
+    const float sum[4] = {acc.x, acc.y, acc.z, acc.w};
     T out[4];
     bool bad = false;
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const float z = none ? 0.0f : o[e] / l;
-      bad |= y < j.rows && d + e < c.D && !(fabsf(z) < INFINITY);
+      const float z = none ? 0.0f : sum[e] / l;
+      bad |= y < to && d + e < c.D && !(fabsf(z) < INFINITY);
       out[e] = from_f32<T>(z);
     }
     const unsigned long long any = kSumAgain ? __ballot(bad) : 0ull;
     const bool redo = any >> (lane / L * L) & (L == 64 ? ~0ull : (1ull << (L & 63)) - 1);
-    if (y < j.rows && !redo) {
-      T *to = static_cast<T *>(p.out) + row * sh.out_stride[0] + h * sh.out_stride[1];
+    if (y < to && !redo) {
+      T *o = static_cast<T *>(p.out) + row * sh.out_stride[0] + h * sh.out_stride[1];
       if (ct.direct && d + 4 <= c.D) {
-        __builtin_memcpy(__builtin_assume_aligned(to + d, 4), out, sizeof(out));
+        __builtin_memcpy(__builtin_assume_aligned(o + d, 4), out, sizeof(out));
       } else {
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-          if (d + e < c.D) to[d + e] = out[e];
+          if (d + e < c.D) o[d + e] = out[e];
       }
       if (p.lse && d == 0) p.lse[(int64_t)row * sh.Hq + h] = none ? -INFINITY : log_sum(m, l);
     }
@@ -1235,14 +1289,17 @@ __device__ __forceinline__ void join_rows(const dconv_cache &c, const dconv_cach
   }
 }
 
-// The workgroups of both kernels, those of few rows first (as far as they divide items).
 template <class T, int DP, int FORMAT>
-__global__ __launch_bounds__(256) void cache_join(const dconv_cache c, const dconv_cache_attend_shape sh, const Batch t,
-                                                  const CacheAttendPtrs p, const CacheTile few, const CacheTile tiles) {
+__global__ __launch_bounds__(64 * kJoinWaves) void cache_join(const dconv_cache c, const dconv_cache_attend_shape sh,
+                                                              const Batch t, const CacheAttendPtrs p, const CacheTile few,
+                                                              const CacheTile tiles) {
   __shared__ JoinLds<DP> lds;
-  const int n = few.whole ? 0 : few.groups;
-  if ((int)blockIdx.x < n) join_rows<T, DP, FORMAT, kFewRows>(c, sh, t, p, few, blockIdx.x, lds);
-  else join_rows<T, DP, FORMAT, kTileRows>(c, sh, t, p, tiles, blockIdx.x - n, lds);
+  for (int i = 0; i < 2; ++i) {
+    if (!few.whole && (int)blockIdx.x < few.groups)
+      join_rows<T, DP, FORMAT, kFewRows>(c, sh, t, p, few, 2 * blockIdx.x + i, lds);
+    if (!tiles.whole && (int)blockIdx.x < tiles.groups)
+      join_rows<T, DP, FORMAT, kTileRows>(c, sh, t, p, tiles, 2 * blockIdx.x + i, lds);
+  }
 }
 
 template <class T, int FORMAT>
@@ -1261,7 +1318,7 @@ void launch_cache_attend(const dconv_cache &c, const dconv_cache_attend_shape &s
   tiles.whole = plan.tiles_whole;
   const int few_joins = plan.few_whole ? 0 : plan.few, tile_joins = plan.tiles_whole ? 0 : plan.tiles;
   few.joins = reinterpret_cast<CacheJoin *>(workspace);
-  tiles.joins = few.joins + few_joins;
+  tiles.joins = few.joins + 2 * few_joins;
   few.partial = reinterpret_cast<float *>(workspace + plan.joins_bytes);
   by_width(plan.dp, [&](auto dp) {
     constexpr int DP = decltype(dp)::value;
@@ -1283,13 +1340,9 @@ void launch_cache_attend(const dconv_cache &c, const dconv_cache_attend_shape &s
       else
         hipLaunchKernelGGL((cache_tiles<T, DP, FORMAT, false>), dim3(plan.tiles), dim3(256), 0, s, both);
     }
-    // rows of an item, by steps of a workgroup
-    const int step = 64 / join_lanes<DP>(), G = sh.Hq / c.Hkv;
-    const int rows = plan.tiles > 0 ? kTileRows : sh.max_rows > 0 && sh.max_rows < kFewRows / G ? sh.max_rows * G : kFewRows;
-    const int steps = plan.tiles > 0 ? rows / (4 * step) : (rows + step - 1) / step;
-    if (few_joins + tile_joins > 0)
-      hipLaunchKernelGGL((cache_join<T, DP, FORMAT>), dim3(few_joins + tile_joins, steps < 16 ? steps : 16), dim3(256), 0,
-                         s, c, sh, t, p, few, tiles);
+    const int joins = few_joins > tile_joins ? few_joins : tile_joins;
+    if (joins > 0)
+      hipLaunchKernelGGL((cache_join<T, DP, FORMAT>), dim3(joins), dim3(64 * kJoinWaves), 0, s, c, sh, t, p, few, tiles);
   });
 }
 
