@@ -85,6 +85,8 @@ int launch(const dconv_cache &c, const dconv_cache_attend_shape &sh, const Batch
   if (c.format == DCONV_CACHE_PLAIN) {
     plan.pieces = whole_pieces(p.cache.k, c.D, es, {c.k_stride[0], c.k_stride[1], c.k_stride[2]}) &&
                   whole_pieces(p.cache.v, c.D, es, {c.v_stride[0], c.v_stride[1], c.v_stride[2]});
+  } else {
+    plan.pieces = whole_pieces(p.cache.k, c.D, 1, {c.k_stride[0], c.k_stride[1], c.k_stride[2]});
   }
   // as many slots as a tile has keys (64) span less than 2^31 bytes
   plan.near = c.format != DCONV_CACHE_PLAIN || plan.pieces;

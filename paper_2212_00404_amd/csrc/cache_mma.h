@@ -2,12 +2,6 @@
 // running softmax of attend_mma.h over tiles of keys whose places a table gives.
 // Instantiated per type and format in cache_attend_*.hip.
 #pragma once
-#ifndef VAR_QREG
-#define VAR_QREG 0
-#endif
-#ifndef VAR_AHEAD
-#define VAR_AHEAD 2
-#endif
 
 #include "attend_mma.h"
 #include "cache_attend.h"
@@ -18,7 +12,7 @@ namespace dconv {
 struct CacheTile {
   float scale2, sign;   // as in AttendTile
   bool direct;          // queries and results in 16-byte pieces
-  bool pieces, near;    // rows of a plain cache too; and those of one copy span less than 2^31 bytes
+  bool pieces, near;    // rows of a plain cache too (codes: on 4-byte boundaries); a tile's slots span less than 2^31 bytes
   int groups, least;    // workgroups, the least work of one
   int whole;            // tiles per sequence and key head, one for each workgroup; 0: by work
   float *partial;       // two parts of each workgroup's
@@ -262,40 +256,67 @@ struct CodeTiles {
   }
 };
 
-// The codes of one key's half row as row operands, straight from memory: the lane of
-// key l % 32 takes elements 32 b + 16 (l / 32) .. + 15 of every block b, and the
-// queries are taken in the same order (order_of), as the inner index has none.
+// The codes of 32 keys, copied into LDS as they are (32 rows by rows' lanes straight
+// into registers would touch every row's line with each load) and read as row operands:
+// the lane of key l % 32 takes elements 32 b + 16 (l / 32) .. + 15 of every block b, and
+// the queries are taken in the same order (order_of), as the inner index has none.
 template <class T, int DP, int FORMAT>
 struct KeyCodes {
   typedef typename Mma<T>::Frag Frag;
   static constexpr int kBlocks = DP / kBlock, kWords = 16 / codes_per_word<FORMAT>();
-  RawCodes<kWords> raw[kBlocks];
+  static constexpr int kRow = DP / kBlock * kWords * 8, kPieces = kRow / 16, kAll = 32 * kPieces;
   uint32_t scale[kBlocks];
   static __device__ __forceinline__ int order_of(int k, int half) { return 32 * (k / 2) + 16 * half + 8 * (k & 1); }
-  __device__ __forceinline__ void load(const char *row, const uint8_t *scales, int D, int half) {
+  // Pieces are permuted within a row so that sixteen rows' lie on different banks.
+  static __device__ __forceinline__ int swizzle(int row) {
+    return kPieces == 16 ? row & 15 : kPieces == 8 ? row >> 1 & 7 : kPieces == 4 ? row >> 2 & 3 : kPieces == 2 ? row >> 3 & 1 : 0;
+  }
+  // row(r): where row r is; scales: those of the lane's row.  `pieces`: rows begin on
+  // 4-byte boundaries, which copies into LDS need.
+  template <class F>
+  __device__ __forceinline__ void load(char *lds, const uint8_t *scales, int D, int lane, bool pieces, F row) {
 #pragma unroll
-    for (int b = 0; b < kBlocks; ++b) {
-      if (DP <= 128 || b * kBlock < D) {
-        raw[b] = *reinterpret_cast<const RawCodes<kWords> *>(row + (2 * b + half) * (kWords * 4));
-        scale[b] = scales[b];
+    for (int i = 0; i < (kAll + 63) / 64; ++i) {
+      const int x = min(i * 64 + lane, kAll - 1), r = x / kPieces;
+      int piece = x % kPieces ^ swizzle(r);
+      if (DP > 128 && piece * (kBlock * 16) >= D * kWords * 8) piece = 0;   // (meets queries that are zeros)
+      const char *from = row(r) + piece * 16;
+      if (pieces) {
+        if (kAll % 64 == 0 || i * 64 + lane < kAll)
+          __builtin_amdgcn_global_load_lds(from, (lds_ptr)(lds + i * 1024), 16, 0, 0);
       } else {
-        raw[b] = {};
-        scale[b] = 0;
+        const RawCodes<4> w = *reinterpret_cast<const RawCodes<4> *>(from);
+        __builtin_memcpy(__builtin_assume_aligned(lds + x * 16, 16), &w, 16);
       }
     }
+    if constexpr (kBlocks == 4) {
+      const uint32_t w = reinterpret_cast<const RawCodes<1> *>(scales)->w[0];
+#pragma unroll
+      for (int b = 0; b < 4; ++b) scale[b] = w >> 8 * b & 255;
+    } else {
+#pragma unroll
+      for (int b = 0; b < kBlocks; ++b) scale[b] = DP <= 128 || b * kBlock < D ? scales[b] : 0;
+    }
   }
-  __device__ __forceinline__ Frag frag(int k) const {
-    struct alignas(16) {
-      T x[8];
-    } y;
+  // Operands 2 b and 2 b + 1.
+  __device__ __forceinline__ void frags(const char *lds, int b, int lane, Frag (&f)[2]) const {
+    const int row = lane & 31, half = lane >> 5;
+    RawCodes<kWords> raw;
+    if constexpr (FORMAT == DCONV_CACHE_E4M3)
+      __builtin_memcpy(&raw, __builtin_assume_aligned(lds + row * kRow + ((2 * b + half) ^ swizzle(row)) * 16, 16), 16);
+    else
+      __builtin_memcpy(&raw, __builtin_assume_aligned(lds + row * kRow + (b ^ swizzle(row)) * 16 + half * 8, 8), 8);
     constexpr int kPairs = codes_per_word<FORMAT>() / 2;
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
-      decode_pair<T, FORMAT>(raw[k / 2].w[(4 * (k & 1) + e) / kPairs], (4 * (k & 1) + e) % kPairs,
-                             scale_of(scale[k / 2]), y.x + 2 * e);
-    Frag f;
-    __builtin_memcpy(&f, &y, sizeof(f));
-    return f;
+    for (int k = 0; k < 2; ++k) {
+      struct alignas(16) {
+        T x[8];
+      } y;
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        decode_pair<T, FORMAT>(raw.w[(4 * k + e) / kPairs], (4 * k + e) % kPairs, scale_of(scale[b]), y.x + 2 * e);
+      __builtin_memcpy(&f[k], &y, sizeof(f[k]));
+    }
   }
 };
 
@@ -585,10 +606,6 @@ __device__ __forceinline__ int again_vector(int x) {
   asm volatile("" : "+v"(x));
   return x;
 }
-
-// Nothing moves across: conversions and loads of several tiles at once do not fit the
-// registers.
-__device__ __forceinline__ void phase() { __builtin_amdgcn_sched_barrier(0); }
 
 // A segment of an item: from `pos` to `end` of its work.
 struct Segment {
@@ -903,27 +920,12 @@ __device__ __forceinline__ void few_body(T (&kbuf)[LEN], T (&vbuf)[LEN], RangeSc
       all_to = min(all_to, __shfl_xor(all_to, x));
     }
     all_from = uniform(all_from), all_to = uniform(all_to);
-    // Beside codes on their way there are no registers for the queries: they are
-    // operands from LDS, where plain keys would be.
-    Frag q[FORMAT == DCONV_CACHE_PLAIN || VAR_QREG ? KS : 1];
+    Frag q[KS];
     const T *qrow = static_cast<const T *>(p.q) + row * sh.q_stride[0] + h * sh.q_stride[1];
-    const uint32_t qb = r * Reader<T, DP>::kRow, qx = ((2 * (lane >> 5)) ^ Tile<T, DP>::swizzle(r)) * Reader<T, DP>::kChunk;
-    auto query = [&](uint32_t b, uint32_t x, int k) {   // elements order_of(k, lane / 32) .. + 7 of the lane's row
-      return reinterpret_cast<char *>(kbuf) + ((x ^ (4 * (k / 2) + (k & 1)) * Reader<T, DP>::kChunk) + b);
-    };
-    if constexpr (FORMAT == DCONV_CACHE_PLAIN) {
 #pragma unroll
-      for (int k = 0; k < KS; ++k) q[k] = load_frag(qrow, 16 * k + 8 * (lane >> 5), D, ct.direct, ct.sign);
-    } else if constexpr (VAR_QREG) {
-#pragma unroll
-      for (int k = 0; k < KS; ++k) q[k] = load_frag(qrow, Codes::order_of(k, lane >> 5), D, ct.direct, ct.sign);
-    } else {
-      for (int k = wave; k < KS; k += W) {
-        const Frag f = load_frag(qrow, Codes::order_of(k, lane >> 5), D, ct.direct, ct.sign);
-        __builtin_memcpy(__builtin_assume_aligned(query(qb, qx, k), 16), &f, sizeof(f));
-      }
-      __syncthreads();
-    }
+    for (int k = 0; k < KS; ++k)
+      q[k] = load_frag(qrow, FORMAT == DCONV_CACHE_PLAIN ? 16 * k + 8 * (lane >> 5) : Codes::order_of(k, lane >> 5), D,
+                       ct.direct, ct.sign);
 
     const Finder<T, FORMAT, BN, ONE> finder = {p.cache.table + g.b * t.table_stride, t.page, t.pages};
     const int64_t es = Finder<T, FORMAT, BN, ONE>::kBytes;
@@ -989,56 +991,52 @@ __device__ __forceinline__ void few_body(T (&kbuf)[LEN], T (&vbuf)[LEN], RangeSc
           }
         }
       } else {
-        // Codes come into registers, kAhead tiles ahead: keys as operands, values by
-        // way of LDS, which turns them.
-        constexpr int kAhead = DP <= 128 && sizeof(T) == 2 ? VAR_AHEAD : 1;
+        // Codes come a tile ahead: keys into LDS, values into registers and from there,
+        // converted, into LDS, which turns them.
         const uint8_t *ksb = p.cache.k_scale + g.hk * c.k_scale_stride[2], *vsb = p.cache.v_scale + g.hk * c.v_scale_stride[2];
-        Codes kc[kAhead];
-        CodeTiles<T, DP, BN, 64, FORMAT, 1, ONE> vc[kAhead];
-        uint32_t gone[kAhead];
+        Codes kc;
+        CodeTiles<T, DP, BN, 64, FORMAT, 1, ONE> vc;
+        char *kl = reinterpret_cast<char *>(kt);
+        static_assert(32 * Codes::kRow <= kTile * (int)sizeof(T), "the codes of a tile of keys");
+        uint32_t next = 0;
         // (past the last tile it comes again: loads under a condition would be waited for
         // one and all, as the compiler cannot count them)
         const int last = u + (end - 1 - u) / W * W;
-        auto load = [&](int i, int v) {   // tile v, whose places have been asked for
+        auto load = [&](int v) {   // tile v, whose places have been asked for
           const Found f = finder.find(c, asked);
           asked = finder.ask(keys, keys.start(min(v + W, last)));
-          const int j0 = keys.start(v), r = lane & 31;
-          const uint32_t key = ONE ? keys.whole(j0) ? r : keys.key(j0, j0 + r) - j0 : 0;   // (else its place is the lane's)
-          kc[i].load(kb + f.k + key * (uint32_t)c.k_stride[1], ksb + f.ks + key * (uint32_t)c.k_scale_stride[1], D, lane >> 5);
-          vc[i].load(c, kb, vb, ksb, vsb, f, keys, j0, D, lane);
-          gone[i] = (uint32_t)f.gone;
+          const int j0 = keys.start(v);
+          const bool whole = keys.whole(j0);
+          auto slot = [&](int r) { return (uint32_t)(whole ? r : keys.key(j0, j0 + r) - j0); };
+          const uint32_t ks = (uint32_t)c.k_stride[1];
+          auto krow = [&](int r) { return ONE ? kb + f.k + slot(r) * ks : kb + from_lane(f.k, r); };
+          kc.load(kl, ksb + f.ks + (ONE ? slot(lane & 31) * (uint32_t)c.k_scale_stride[1] : 0), D, lane, ct.pieces, krow);
+          vc.load(c, kb, vb, ksb, vsb, f, keys, j0, D, lane);
+          next = (uint32_t)f.gone;
         };
+        load(u);
+        for (; u < end; u += W) {
+          Reader<T, DP> rd = reader;
+          rd.again();
+          const int seen_from = again_vector(lane);
+          landed<0>();
+          f32x16 s = {};
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) load(i, min(u + i * W, last));
-        for (; u < end; u += kAhead * W) {
-#pragma unroll
-          for (int i = 0; i < kAhead; ++i) {
-            const int v = u + i * W;   // (past the last tile: nobody sees it)
-            Reader<T, DP> rd = reader;
-            rd.again();
-            uint32_t xb = qb, xx = qx;
-            asm volatile("" : "+v"(xb), "+v"(xx));
-            f32x16 s = {};
-            phase();
-#pragma unroll
-            for (int k = 0; k < KS; ++k) {
-              Frag f;
-              if constexpr (VAR_QREG) f = q[k];
-              else __builtin_memcpy(&f, __builtin_assume_aligned(query(xb, xx, k), 16), sizeof(f));
-              s = Mma<T>::mac(kc[i].frag(k), f, s);
-            }
-            phase();
-            vc[i].store(vt, vt, lane);
-            phase();
-            const uint32_t now = v > last ? ~0u : gone[i];
-            load(i, min(v + kAhead * W, last));
-            phase();
-            Frag w[2];
-            weigh(s, keys.start(min(v, last)), now, w);
-            soft.values(rd, vt, 0, w);
-            phase();
+          for (int k = 0; k < KS; k += 2) {
+            Frag f[2];
+            kc.frags(kl, k / 2, seen_from, f);
+            s = Mma<T>::mac(f[0], q[k], s);
+            s = Mma<T>::mac(f[1], q[k + 1], s);
           }
+          vc.store(vt, vt, lane);
+          const uint32_t gone = next;
+          landed<0>();   // (read)
+          load(min(u + W, last));
+          Frag w[2];
+          weigh(s, keys.start(u), gone, w);
+          soft.values(rd, vt, 0, w);
         }
+        landed<0>();   // the last copies, of no use
       }
     }
 

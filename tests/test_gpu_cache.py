@@ -448,6 +448,24 @@ def test_strides_and_alignment():
             check(out, None, pool.reference(q))
 
 
+@pytest.mark.parametrize("kind", ["e4m3", "e2m1"])
+def test_codes_that_begin_anywhere(kind):
+    """Pools of bytes that begin between two words, with rows as far apart."""
+    for rows in ([1, 2], [80, 33]):
+        for D, page in ((64, 16), (128, 64), (96, 32)):
+            pool = Pool(52, torch.bfloat16, kind, rows, [100, 333], 2, D, page)
+            q = pool.queries(53, 4)
+            want = dc.attend_cache(q, pool.cache, *pool.where)
+
+            def odd(t):
+                last = t.shape[-1]
+                raw = torch.zeros((pool.pages, page, 2, last + 3), dtype=torch.uint8, device=DEV)[..., 1:1 + last]
+                raw.copy_(t.view(torch.uint8))
+                return raw.view(t.dtype)
+            cache = dc.Cache(*(odd(t) for t in (pool.k, pool.v, pool.ks, pool.vs)))
+            assert torch.equal(want, dc.attend_cache(q, cache, *pool.where))
+
+
 def test_rows_behind_the_last_and_longer_sequences_than_said():
     pool = Pool(34, torch.bfloat16, "e4m3", [2, 0, 40, 1], [50, 7, 60, 20], 2, 64, 16)
     q = pool.queries(35, 4, tail=9)
