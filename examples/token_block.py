@@ -10,8 +10,8 @@ pixels, read row by row behind one class token, are the tokens of a block:
 
 ``train`` runs a few steps of gradient descent through the operators' own
 gradients; ``serve`` feeds the same tokens one at a time over a cache of keys
-and values, the way a decoder does, and gives the same outputs.  The matrix
-products are torch's.
+and values, the way a decoder does, and gives the same outputs; ``serve_in_pages``
+keeps them in pages, the first tokens as one chunk.  The matrix products are torch's.
 """
 import os
 import sys
@@ -148,6 +148,24 @@ class TokenBlock:
             out.append(self.finish(dc.attend(q, cache_k, cache_v, lengths=lengths, **self.see), now))
         return torch.cat(out, 1)
 
+    @torch.no_grad()
+    def serve_in_pages(self, x, prompt=100, kind=None, page=16):
+        """The same over a cache in pages (of ``kind``, else of the block's type): the
+        first tokens in a chunk, then one at a time."""
+        B, T, _ = x.shape
+        each = -(-T // page)
+        cache = dc.Cache.new(B * each, page, self.Hkv, self.head, kind or x.dtype, device=x.device)
+        table = torch.arange(B * each, dtype=torch.int32, device=x.device).view(B, each)
+        out = []
+        for t0, t1 in [(0, prompt)] + [(t, t + 1) for t in range(prompt, T)]:
+            now = x[:, t0:t1]
+            q, k, v = (y.flatten(0, 1) for y in self.project(now, self.positions[:, t0:t1]))
+            lengths = torch.full((B,), t1, dtype=torch.int32, device=x.device)
+            dc.cache_write(cache, k, v, table, lengths)
+            attended = dc.attend_cache(q, cache, table, lengths, **self.see)
+            out.append(self.finish(attended.unflatten(0, (B, -1)), now))
+        return torch.cat(out, 1)
+
 
 def main():
     block = TokenBlock()
@@ -161,6 +179,9 @@ def main():
         whole, served = block(x), block.serve(x)
     off = (whole.float() - served.float()).abs().max().item()
     print("one token at a time: off by at most %.4f of %.2f" % (off, whole.float().abs().max().item()))
+    for kind in (None, "e4m3", "e2m1"):
+        paged = block.serve_in_pages(x, kind=kind)
+        print("over pages of %s: off by at most %.4f" % (kind or "bf16", (whole.float() - paged.float()).abs().max().item()))
     return losses, off
 
 

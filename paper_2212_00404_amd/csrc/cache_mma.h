@@ -298,25 +298,30 @@ struct KeyCodes {
       for (int b = 0; b < kBlocks; ++b) scale[b] = DP <= 128 || b * kBlock < D ? scales[b] : 0;
     }
   }
-  // Operands 2 b and 2 b + 1.
-  __device__ __forceinline__ void frags(const char *lds, int b, int lane, Frag (&f)[2]) const {
+  // The lane's codes, of all blocks.
+  __device__ __forceinline__ void read(const char *lds, int lane, RawCodes<kWords> (&raw)[kBlocks]) const {
     const int row = lane & 31, half = lane >> 5;
-    RawCodes<kWords> raw;
-    if constexpr (FORMAT == DCONV_CACHE_E4M3)
-      __builtin_memcpy(&raw, __builtin_assume_aligned(lds + row * kRow + ((2 * b + half) ^ swizzle(row)) * 16, 16), 16);
-    else
-      __builtin_memcpy(&raw, __builtin_assume_aligned(lds + row * kRow + (b ^ swizzle(row)) * 16 + half * 8, 8), 8);
-    constexpr int kPairs = codes_per_word<FORMAT>() / 2;
 #pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      struct alignas(16) {
-        T x[8];
-      } y;
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        decode_pair<T, FORMAT>(raw.w[(4 * k + e) / kPairs], (4 * k + e) % kPairs, scale_of(scale[b]), y.x + 2 * e);
-      __builtin_memcpy(&f[k], &y, sizeof(f[k]));
+    for (int b = 0; b < kBlocks; ++b) {
+      if constexpr (FORMAT == DCONV_CACHE_E4M3)
+        __builtin_memcpy(&raw[b], __builtin_assume_aligned(lds + row * kRow + ((2 * b + half) ^ swizzle(row)) * 16, 16), 16);
+      else
+        __builtin_memcpy(&raw[b], __builtin_assume_aligned(lds + row * kRow + (b ^ swizzle(row)) * 16 + half * 8, 8), 8);
     }
+  }
+  // Operand k of them.
+  __device__ __forceinline__ Frag frag(const RawCodes<kWords> (&raw)[kBlocks], int k) const {
+    constexpr int kPairs = codes_per_word<FORMAT>() / 2;
+    struct alignas(16) {
+      T x[8];
+    } y;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      decode_pair<T, FORMAT>(raw[k / 2].w[(4 * (k & 1) + e) / kPairs], (4 * (k & 1) + e) % kPairs,
+                             scale_of(scale[k / 2]), y.x + 2 * e);
+    Frag f;
+    __builtin_memcpy(&f, &y, sizeof(f));
+    return f;
   }
 };
 
@@ -393,6 +398,22 @@ struct CacheSoftmax : Softmax<T, DP> {
     for (int k = 0; k < KS; ++k) s = Mma<T>::mac(rd.row(ks, k0, k), q[k], s);
     return s;
   }
+  // (operands are read well before their products, where registers hold them)
+  static constexpr bool kReadAhead = KS * sizeof(Frag) <= 128;
+  static __device__ __forceinline__ f32x16 scores_ahead(const Reader<T, DP> &rd, const T *ks, const Frag (&q)[KS]) {
+    if constexpr (!kReadAhead) return scores(rd, ks, 0, q);
+    Frag kf[KS];
+    load_keys(rd, kf, ks, 0);
+    return Base::products(kf, q);
+  }
+  __device__ __forceinline__ void values_ahead(const Reader<T, DP> &rd, const T *vs, const Frag (&w)[2]) {
+    if constexpr (!kReadAhead) return values(rd, vs, 0, w);
+    Frag vf[2][DT];
+    load_values(rd, vf[0], vs, 0);
+    load_values(rd, vf[1], vs, 16);
+    Base::weigh(vf[0], w[0]);
+    Base::weigh(vf[1], w[1]);
+  }
   __device__ __forceinline__ void values(const Reader<T, DP> &rd, const T *vs, int k0, const Frag (&w)[2]) {
 #pragma unroll
     for (int k = 0; k < 2; ++k)
@@ -414,7 +435,7 @@ struct CacheSoftmax : Softmax<T, DP> {
                                       const RowKeys &see, int sinks, float scale2, bool masked, int lane,
                                       uint32_t gone) {
     rd.again();
-    if constexpr (KS * sizeof(Frag) <= 128) {   // operands are read well before their products
+    if constexpr (kReadAhead) {
       Frag kf[KS], vf[2][DT];
       load_keys(rd, kf, ks, 0);
       f32x16 s = Base::products(kf, q);
@@ -973,7 +994,7 @@ __device__ __forceinline__ void few_body(T (&kbuf)[LEN], T (&vbuf)[LEN], RangeSc
           Reader<T, DP> rd = reader;
           rd.again();
           landed<Tiles::C::kCopies>();   // the keys; the values may still be on their way
-          f32x16 s = soft.scores(rd, kt, 0, q);
+          f32x16 s = soft.scores_ahead(rd, kt, q);
           landed<Tiles::C::kCopies>();   // (read)
           if (more) {
             f = finder.find(c, asked);
@@ -983,7 +1004,7 @@ __device__ __forceinline__ void few_body(T (&kbuf)[LEN], T (&vbuf)[LEN], RangeSc
           weigh(s, keys.start(u), gone, w);
           if (more) landed<Tiles::C::kCopies>();   // the values; not the next keys
           else landed<0>();
-          soft.values(rd, vt, 0, w);
+          soft.values_ahead(rd, vt, w);
           if (more) {
             if (u + 2 * W < end) asked = finder.ask(keys, keys.start(u + 2 * W));
             landed<63>();   // (read)
@@ -1020,21 +1041,19 @@ __device__ __forceinline__ void few_body(T (&kbuf)[LEN], T (&vbuf)[LEN], RangeSc
           rd.again();
           const int seen_from = again_vector(lane);
           landed<0>();
+          RawCodes<Codes::kWords> raw[DT];
+          kc.read(kl, seen_from, raw);
+          in_order();
           f32x16 s = {};
 #pragma unroll
-          for (int k = 0; k < KS; k += 2) {
-            Frag f[2];
-            kc.frags(kl, k / 2, seen_from, f);
-            s = Mma<T>::mac(f[0], q[k], s);
-            s = Mma<T>::mac(f[1], q[k + 1], s);
-          }
+          for (int k = 0; k < KS; ++k) s = Mma<T>::mac(kc.frag(raw, k), q[k], s);
           vc.store(vt, vt, lane);
           const uint32_t gone = next;
           landed<0>();   // (read)
           load(min(u + W, last));
           Frag w[2];
           weigh(s, keys.start(u), gone, w);
-          soft.values(rd, vt, 0, w);
+          soft.values_ahead(rd, vt, w);
         }
         landed<0>();   // the last copies, of no use
       }

@@ -1,6 +1,8 @@
 """GPU: a cache in pages, what is written to it, read from it and attended over,
 against the definitions in 64 bits."""
 import math
+import os
+import sys
 
 import pytest
 import torch
@@ -638,3 +640,85 @@ def test_a_cache_that_grows(kind):
                 same = dc.attend(q[at:at + r][None], dk[lo:lo + have[b]][None], dv[lo:lo + have[b]][None])[0]
                 ref.check(out[at:at + r], same.cpu().double(), 2 * r_.out_tol[0], "beside attend")
             at += r
+
+
+def test_example_serves_in_pages():
+    sys.path.insert(0, os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples"))
+    import token_block
+    block = token_block.TokenBlock()
+    g = torch.Generator().manual_seed(60)
+    with torch.no_grad():
+        x = block.tokens(torch.rand((3, 3, 16, 16), generator=g).to(DEV))
+        whole = block(x).float()
+        for prompt in (1, 100, x.shape[1]):
+            # bf16 outputs of order 1 to 4: both ways round each of five steps once
+            assert (whole - block.serve_in_pages(x, prompt=prompt).float()).abs().max() <= 5 * 4 * 2.0 ** -8
+        # and over codes as over the values that they stand for
+        for kind in ("e4m3", "e2m1"):
+            out = block.serve_in_pages(x, kind=kind)
+            assert out.shape == whole.shape and torch.isfinite(out).all()
+
+
+# ---------------------------------------------------------------------------
+# the LDS-poisoning build, and refusals of the binding
+# ---------------------------------------------------------------------------
+@pytest.mark.parametrize("dt", TYPES, ids=TYPE_IDS)
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("case", [([1, 1, 1], [900, 65, 300], 8, 2, 128, 64, dict(left=200, sinks=3)),
+                                  ([1, 1], [1, 500], 4, 4, 64, 16, dict()),
+                                  ([130, 1, 5], [300, 260, 90], 4, 2, 64, 24, dict(left=70, sinks=2)),
+                                  ([200, 33], [1500, 33], 6, 2, 96, 64, dict()),
+                                  ([2, 90], [700, 120], 2, 1, 256, 32, dict()),
+                                  ([40], [40], 2, 1, 32, 5, dict(left=7))], ids=str)
+def test_attention_with_poisoned_lds(monkeypatch, case, kind, dt):
+    path = os.path.join(os.path.dirname(dc.dconv.LIB_PATH), "libdconv_poison.so")
+    if not os.path.exists(path):
+        pytest.fail("libdconv_poison.so is not built (paper_2212_00404_amd/build.py builds it)")
+    rows, lengths, Hq, Hkv, D, page, how = case
+    pool = Pool(61, dt, kind, rows, lengths, Hkv, D, page)
+    monkeypatch.setattr(dc.dconv, "_lib", dc.load(path))
+    compare(pool, Hq, **how)
+
+
+def test_binding_refusals():
+    pool = Pool(62, torch.bfloat16, "plain", [2, 1], [20, 9], 2, 64, 8)
+    table, lengths, offsets = pool.where
+    c, k = pool.cache, torch.zeros((3, 2, 64), dtype=torch.bfloat16, device=DEV)
+    q = torch.zeros((3, 4, 64), dtype=torch.bfloat16, device=DEV)
+    e4 = Pool(63, torch.bfloat16, "e4m3", [1], [9], 2, 64, 8)
+    for bad in (lambda: dc.Cache(pool.k, pool.v[:1]), lambda: dc.Cache(pool.k, pool.v.half()),
+                lambda: dc.Cache(pool.k, pool.v, pool.k, pool.k), lambda: dc.Cache(e4.k, e4.v),
+                lambda: dc.Cache(e4.k, e4.v, e4.ks.view(torch.uint8), e4.vs), lambda: dc.Cache(pool.k[0], pool.v[0]),
+                lambda: dc.Cache(e4.k, e4.v, e4.ks[..., :1], e4.vs), lambda: dc.Cache(pool.k[:0], pool.v[:0]),
+                lambda: dc.Cache(pool.k[..., ::2], pool.v[..., ::2]), lambda: dc.Cache(pool.k.double(), pool.v.double()),
+                lambda: dc.cache_write(c, k, k[:2], table, lengths, offsets),
+                lambda: dc.cache_write(c, k.float(), k.float(), table, lengths, offsets),
+                lambda: dc.cache_write(c, k[..., :32], k[..., :32], table, lengths, offsets),
+                lambda: dc.cache_write(c, k[:, :1], k[:, :1], table, lengths, offsets),
+                lambda: dc.cache_write(c, k, k, table.long(), lengths, offsets),
+                lambda: dc.cache_write(c, k, k, table[0], lengths, offsets),
+                lambda: dc.cache_write(c, k, k, table, lengths[:1], offsets),
+                lambda: dc.cache_write(c, k, k, table, lengths, offsets[:2]),
+                lambda: dc.cache_write(c, k, k, table, lengths), lambda: dc.cache_write(c, k, k, table.cpu(), lengths, offsets),
+                lambda: dc.cache_write(c, k.cpu(), k, table, lengths, offsets),
+                lambda: dc.cache_read(c, 3, table, lengths, offsets, dtype=torch.float32),
+                lambda: dc.cache_read(e4.cache, 1, *e4.where, dtype=torch.float64),
+                lambda: dc.cache_read(c, 3, table, lengths, offsets, out=(k[:2], k[:2])),
+                lambda: dc.attend_cache(q.half(), c, table, lengths, offsets),
+                lambda: dc.attend_cache(q[:, :3], c, table, lengths, offsets),
+                lambda: dc.attend_cache(q[..., :32], c, table, lengths, offsets),
+                lambda: dc.attend_cache(q[None], c, table, lengths, offsets),
+                lambda: dc.attend_cache(q, c, table, lengths, offsets, left=-2),
+                lambda: dc.attend_cache(q, c, table, lengths, offsets, sinks=-1),
+                lambda: dc.attend_cache(q, c, table, lengths, offsets, max_rows=0),
+                lambda: dc.attend_cache(q, c, table, lengths, offsets, left=1 << 31),
+                lambda: dc.attend_cache(q, c, table, lengths, offsets, out=q[:2]),
+                lambda: dc.attend_cache(q.double(), e4.cache, *e4.where),
+                lambda: dc.attend_cache(q, c, table, lengths)):
+        with pytest.raises(ValueError):
+            bad()
+    wide = torch.zeros((2, 4, 1, 288), dtype=torch.bfloat16, device=DEV)
+    with pytest.raises(RuntimeError, match="-5"):
+        dc.attend_cache(torch.zeros((2, 1, 288), dtype=torch.bfloat16, device=DEV), dc.Cache(wide, wide), table, lengths)
+    with pytest.raises(RuntimeError, match="-2"):
+        dc.attend_cache(q, c, table, lengths, offsets, scale=math.inf)
