@@ -548,6 +548,9 @@ typedef struct dconv_cache_rows {
  * 2^-127 on by which no element exceeds M, and each element is rounded once, to
  * nearest even.  A block that holds an infinity or NaN reads back as NaN.
  * What a slot holds that one call writes twice is not defined.
+ * 1 <= D <= 256, Hkv to 4096, B to 2^20, table_width * page_size and N below
+ * 2^31 - 2^16, and what a launch can hold (2^24 workgroups of 64 rows, or of fewer:
+ * some 2048 pieces of eight elements), else DCONV_EUNSUPPORTED or DCONV_ERANGE.
  */
 int dconv_cache_write(const dconv_cache *cache, const dconv_cache_rows *rows, const void *k,
                       const void *v, void *cache_k, void *cache_v, void *k_scale, void *v_scale,

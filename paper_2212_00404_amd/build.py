@@ -121,12 +121,15 @@ def build(verbose: bool = False) -> str:
     os.makedirs(poison_dir, exist_ok=True)
     os.makedirs(trace_dir, exist_ok=True)
     srcs = sorted(glob.glob(os.path.join(CSRC, "*.hip")))
+    # the stage trace is in the multi-channel kernels and in its registration; the
+    # trace twin's other objects are the library's
+    traced = [os.path.basename(s).startswith(("multi", "api")) for s in srcs]
     jobs = ([(s, BUILD, ()) for s in srcs] + [(PEAKS_SRC, BUILD, ())] +
             [(s, poison_dir, ("-DDCONV_POISON_LDS",)) for s in srcs] +
-            [(s, trace_dir, ("-DDCONV_STAGE_TRACE",)) for s in srcs])
+            [(s, trace_dir, ("-DDCONV_STAGE_TRACE",)) for s, t in zip(srcs, traced) if t])
     workers = min(len(jobs), max(1, min(8, os.cpu_count() or 1)))
     # the matrix-core kernel units take longest: start them first
-    order = sorted(range(len(jobs)), key=lambda i: "multi_mfma" not in jobs[i][0])
+    order = sorted(range(len(jobs)), key=lambda i: "multi_mfma" not in jobs[i][0] and "cache_attend_" not in jobs[i][0])
     with concurrent.futures.ThreadPoolExecutor(workers) as ex:
         futs = {i: ex.submit(_compile, *jobs[i]) for i in order}
         results = [futs[i].result() for i in range(len(jobs))]
@@ -139,7 +142,8 @@ def build(verbose: bool = False) -> str:
     _link(objs[:n], LIB)
     _link(objs[n:n + 1], PEAKS_LIB)
     _link(objs[n + 1:2 * n + 1], POISON_LIB)
-    _link(objs[2 * n + 1:], TRACE_LIB)
+    trace_objs = iter(objs[2 * n + 1:])
+    _link([next(trace_objs) if t else o for o, t in zip(objs[:n], traced)], TRACE_LIB)
     return LIB
 
 

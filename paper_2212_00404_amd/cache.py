@@ -161,6 +161,8 @@ def cache_read(cache: Cache, rows: int, table: torch.Tensor, lengths: torch.Tens
     position is negative or whose page is not one of the cache's.  Rows behind the
     last sequence are left as they were (in ``out``, else of no meaning).
     """
+    if rows < 0:
+        raise ValueError("rows must be 0 or more, got %d" % rows)
     B, width, stride = _batch(cache, table, lengths, offsets, rows)
     if dtype is None:
         dtype = cache.dtype or (out[0].dtype if out is not None else torch.bfloat16)

@@ -158,7 +158,7 @@ __device__ __forceinline__ Codes<FORMAT == DCONV_CACHE_E4M3 ? 2 : 1> encode(cons
   return out;
 }
 
-// A thread's pieces, kBatch on their way at a time.
+// A thread's pieces, a batch on their way at a time.
 // (Writing gains nothing by it: a prompt of 61096 tokens, 8 heads of 128, bf16 into
 // e4m3, 379 MB, takes 95 us by one at a time and 108 by four, which leave registers for
 // five waves per SIMD; reading 65536 back takes 107 us by four and 113 by one.)
@@ -282,7 +282,8 @@ int move(const dconv_cache *cache, const dconv_cache_rows *rows, const RowPtrs &
     return DCONV_ENULL;
   const Batch t = batch_of(*cache, rows->B, rows->N, rows->table_width, rows->table_stride, p.offsets);
   const Walk w = walk_of(*cache, *rows);
-  const unsigned grid = (unsigned)((rows->N + w.rows - 1) / w.rows);
+  const unsigned grid = (unsigned)(((int64_t)rows->N + w.rows - 1) / w.rows);
+  if (grid >= (1ll << 32) / 256) return DCONV_ERANGE;   // a launch has less than 2^32 threads
   (void)hipGetLastError();  // report this launch only
   by_type(rows->dtype, [&](auto *type) {
     using T = std::remove_pointer_t<decltype(type)>;

@@ -47,22 +47,22 @@ CachePlan plan_attend(const dconv_cache &c, const dconv_cache_attend_shape &sh, 
   const int64_t keys = (int64_t)sh.table_width * c.page_size;
   // Two workgroups per compute unit, where LDS and registers hold them; no more than
   // there is work for.
-  auto groups = [](int64_t most, int64_t work, int least) {
-    const int64_t n = (work + least - 1) / least;
-    return (int)(n < 1 ? 1 : n < most ? n : most);
+  auto groups = [](int most, double work, int least) {   // (work may pass 64 bits)
+    const double n = std::ceil(work / least);
+    return n < 1 ? 1 : n < most ? (int)n : most;
   };
   // (fp32 takes sixteen times as long for the products of as many keys)
   f.few_least = es == 4 ? 128 : 256;
   f.tiles_least = es == 4 ? 96 : 512;
   const int whole = es == 4 ? 256 : 512;
   if (!even || rows <= 32) {
-    f.few = groups(f.dp * es <= 256 ? 512 : 256, heads * (keys + 64), f.few_least);
+    f.few = groups(f.dp * es <= 256 ? 512 : 256, (double)heads * (double)(keys + 64), f.few_least);
     // tables of a few steps of a workgroup: nothing is divided, and nothing joined
     if (keys <= whole && heads < (1 << 20)) f.few_whole = 1, f.few = (int)heads;
   }
   if (rows > 32) {
     const int64_t tiles = ((int64_t)sh.N * G / 128 + sh.B) * c.Hkv;
-    f.tiles = groups(f.dp * es <= 256 ? 512 : 256, tiles * (keys + 64), f.tiles_least);
+    f.tiles = groups(f.dp * es <= 256 ? 512 : 256, (double)tiles * (double)(keys + 64), f.tiles_least);
     const int64_t each = (rows + 127) / 128;
     if (even && keys <= whole && heads * each < (1 << 20)) f.tiles_whole = (int)each, f.tiles = (int)(heads * each);
   }

@@ -701,6 +701,13 @@ constexpr int cache_part() { return R * (DP + 2); }
 // ---------------------------------------------------------------------------
 // 128 rows: four waves of 32 share tiles of keys
 // ---------------------------------------------------------------------------
+// A plain cache's tiles are copied into two LDS buffers in turn, the next while the
+// current one is used; codes come a tile ahead into registers and go into the other
+// buffer after it.  Chunks of 401 to 512 tokens over up to 8192, 32 heads of 128 over
+// 8, bf16: 168 GFLOP of seen scores in 243 us (690 TFLOP/s; matrix cores busy in 0.34 of the
+// cycles, vector instructions issuing in 0.40, waves waiting in 0.43: two waves per
+// SIMD, each a chain of operands, products and exponentials, do not fill it), and 24 us
+// for the join of rows that two or three workgroups have parts of.
 template <class T, int DP, int FORMAT, bool ONE, int LEN>
 __device__ __forceinline__ void tiles_body(T (&buf0)[LEN], T (&buf1)[LEN], RangeScratch &scratch) {
   constexpr int BN = forward_keys<T>(DP), KS = DP / 16, DT = DP / 32;
@@ -897,6 +904,12 @@ __device__ __forceinline__ void tiles_body(T (&buf0)[LEN], T (&buf1)[LEN], Range
 // ---------------------------------------------------------------------------
 // Up to 32 rows: each wave takes tiles of 32 keys by itself
 // ---------------------------------------------------------------------------
+// No barrier between tiles.  Bound by memory for a plain cache: 32 sequences of 853 to
+// 16384 tokens, 8 key heads of 128, bf16, 1125 MB in 216 us (5.2 TB/s).  A tile of
+// codes takes a wave as long for half or a quarter of the bytes: 64 sequences over 4
+// key heads in e4m3, 568 MB in 140 us (4.1 TB/s); 131072 tokens, 8 heads, five rows
+// each of 4, e2m1, 142 MB in 43 us (3.3 TB/s), the same with all pages in L2.  Reading
+// codes two or three tiles ahead gains nothing (registers: 145 to 245 us for 568 MB).
 template <class T, int DP>
 struct FewScratch {
   float ml[split_waves<T>(DP)][64];
@@ -1170,8 +1183,8 @@ __global__ __launch_bounds__(64 * split_waves<T>(DP), split_waves<T>(DP) == 4 ? 
 }
 
 // Both kinds of sequences by the same workgroups, where they have as many waves: a
-// share of the chunks, then one of the single tokens, which alone would be a launch
-// of 21 us for 24 items that take 3 us of each workgroup's time here.
+// share of the chunks, then one of the single tokens (16 sequences of both: 131 and
+// 21 us apart, 144 together, and a launch less).
 template <class T, int DP, int FORMAT, bool ONE>
 __global__ __launch_bounds__(256, DP * sizeof(T) <= 256 ? 2 : 1) void cache_tiles(const CacheCall) {
   constexpr int N = 2 * forward_keys<T>(DP) * DP;
@@ -1322,6 +1335,8 @@ __global__ __launch_bounds__(64 * kJoinWaves) void cache_join(const dconv_cache 
 template <class T, int FORMAT>
 void launch_cache_attend(const dconv_cache &c, const dconv_cache_attend_shape &sh, const Batch &t,
                          const CacheAttendPtrs &p, const CachePlan &plan, char *workspace, hipStream_t s) {
+  // (fp32's products last so long that it does not matter how a tile is found)
+  constexpr bool kScalar = sizeof(T) == 2;
   const AttendTile scale = [&] {
     dconv_attend_shape a = {};
     a.scale = sh.scale;
@@ -1344,16 +1359,16 @@ void launch_cache_attend(const dconv_cache &c, const dconv_cache_attend_shape &s
     const bool together = plan.few > 0 && plan.tiles > 0 && split_waves<T>(DP) == 4;
     if (plan.few > 0 && !together) {
       const dim3 block(64 * split_waves<T>(DP));
-      if (plan.near && c.page_size % 32 == 0)
-        hipLaunchKernelGGL((cache_few<T, DP, FORMAT, true>), dim3(plan.few), block, 0, s, call);
+      if (kScalar && plan.near && c.page_size % 32 == 0)
+        hipLaunchKernelGGL((cache_few<T, DP, FORMAT, kScalar>), dim3(plan.few), block, 0, s, call);
       else
         hipLaunchKernelGGL((cache_few<T, DP, FORMAT, false>), dim3(plan.few), block, 0, s, call);
     }
     if (plan.tiles > 0) {
       CacheCall both = call;
       if (!together) both.few.groups = 0;
-      if (plan.near && c.page_size % forward_keys<T>(DP) == 0)
-        hipLaunchKernelGGL((cache_tiles<T, DP, FORMAT, true>), dim3(plan.tiles), dim3(256), 0, s, both);
+      if (kScalar && plan.near && c.page_size % forward_keys<T>(DP) == 0)
+        hipLaunchKernelGGL((cache_tiles<T, DP, FORMAT, kScalar>), dim3(plan.tiles), dim3(256), 0, s, both);
       else
         hipLaunchKernelGGL((cache_tiles<T, DP, FORMAT, false>), dim3(plan.tiles), dim3(256), 0, s, both);
     }

@@ -109,6 +109,13 @@ def test_sizes_that_are_not_supported():
     assert workspace(cache_struct(Hkv=1), attend_struct(N=1 << 28, Hq=8))[0] == dconv.ERANGE
 
 
+def test_launches_that_do_not_fit_are_refused():
+    """A launch has less than 2^32 threads."""
+    small = cache_struct(Hkv=1, D=8, page_size=1 << 10)
+    for f in (write, read):
+        assert f(small, rows_struct(B=1, N=1 << 30, width=1 << 20)) == dconv.ERANGE
+
+
 def test_calls_without_work_need_no_device():
     for f, s in ((write, rows_struct), (read, rows_struct), (attend, attend_struct)):
         assert f(cache_struct(), s(N=0), ck=None) == 0

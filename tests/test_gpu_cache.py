@@ -302,6 +302,14 @@ def test_attention(kind, case, dt):
     compare(Pool(20, dt, kind, rows, lengths, Hkv, D, page), Hq, **how)
 
 
+@pytest.mark.parametrize("scale", [0.0, -0.3, 2.0])
+@pytest.mark.parametrize("rows", [[1, 3], [90, 40]])
+def test_scales(rows, scale):
+    for kind in KINDS:
+        for dt in TYPES:
+            compare(Pool(19, dt, kind, rows, [900, 130], 2, 64, 16), 4, scale=scale, left=300)
+
+
 @pytest.mark.parametrize("kind", KINDS)
 def test_many_sequences(kind):
     """More sequences than a wave has lanes, single tokens and chunks, some empty."""
