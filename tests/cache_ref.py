@@ -120,5 +120,13 @@ class Attend:
         finally:
             ref.visible = visible
         turn = (lambda x: x[0].transpose(0, 1))
-        return (a.out[0], a.out_tol[0], torch.where(turn(a.empty), 0.0, turn(a.lse)),
+        tol = a.out_tol[0]
+        if q.dtype == torch.float16:
+            # Probabilities below fp16's normal values, as operands, are off by up to half
+            # its smallest step, 2^-25, whatever their size.  They are taken against a base
+            # that is at most the row's largest score, so their sum l is 1 or more, and the
+            # result is off by 2^-25 / l per seen key's value at most.
+            seen = torch.einsum("rn,nhd->rhd", a.see[0].double(), v.abs().nan_to_num(0.0))
+            tol = tol + 2.0 ** -25 * seen.repeat_interleave(Hq // v.shape[1], 1)
+        return (a.out[0], tol, torch.where(turn(a.empty), 0.0, turn(a.lse)),
                 torch.where(turn(a.empty), 0.0, turn(a.lse_tol)), turn(a.empty))
