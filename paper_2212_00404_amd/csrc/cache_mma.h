@@ -394,6 +394,15 @@ struct CacheSoftmax : Softmax<T, DP> {
 
   static __device__ __forceinline__ f32x16 scores(const Reader<T, DP> &rd, const T *ks, int k0, const Frag (&q)[KS]) {
     f32x16 s = {};
+    if constexpr (sizeof(T) == 4) {   // two sums: half as many roundings one after another
+      f32x16 z = {};
+#pragma unroll
+      for (int k = 0; k < KS; k += 2) {
+        s = Mma<T>::mac(rd.row(ks, k0, k), q[k], s);
+        z = Mma<T>::mac(rd.row(ks, k0, k + 1), q[k + 1], z);
+      }
+      return s + z;
+    }
 #pragma unroll
     for (int k = 0; k < KS; ++k) s = Mma<T>::mac(rd.row(ks, k0, k), q[k], s);
     return s;
@@ -1058,8 +1067,18 @@ __device__ __forceinline__ void few_body(T (&kbuf)[LEN], T (&vbuf)[LEN], RangeSc
           kc.read(kl, seen_from, raw);
           in_order();
           f32x16 s = {};
+          if constexpr (sizeof(T) == 4) {   // (as CacheSoftmax::scores)
+            f32x16 z = {};
 #pragma unroll
-          for (int k = 0; k < KS; ++k) s = Mma<T>::mac(kc.frag(raw, k), q[k], s);
+            for (int k = 0; k < KS; k += 2) {
+              s = Mma<T>::mac(kc.frag(raw, k), q[k], s);
+              z = Mma<T>::mac(kc.frag(raw, k + 1), q[k + 1], z);
+            }
+            s += z;
+          } else {
+#pragma unroll
+            for (int k = 0; k < KS; ++k) s = Mma<T>::mac(kc.frag(raw, k), q[k], s);
+          }
           vc.store(vt, vt, lane);
           const uint32_t gone = next;
           landed<0>();   // (read)
