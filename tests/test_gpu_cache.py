@@ -154,6 +154,30 @@ def test_write_and_read(kind, case, dt):
             assert (o[N:] == 7.0).all()
 
 
+@pytest.mark.parametrize("kind", KINDS)
+def test_moves_of_more_sequences_than_lds_holds(kind):
+    """Offsets and lengths looked up in memory: 700 sequences, some without rows."""
+    dt = torch.bfloat16
+    rows = [(b * 5) % 4 for b in range(700)]
+    lengths = [r + (b * 31) % 40 for b, r in enumerate(rows)]
+    pool = Pool(17, dt, kind, rows, lengths, 1, 32, 8)
+    N = sum(rows)
+    g = torch.Generator().manual_seed(18)
+    k, v = (torch.randn(N, 1, 32, generator=g).to(dt) for _ in range(2))
+    dc.cache_write(pool.cache, k.to(DEV), v.to(DEV), *pool.where)
+    got = dc.cache_read(pool.cache, N, *pool.where, dtype=dt)
+    at = cref.places(pool.table, lengths, rows, 8, pool.pages)
+    for x, o, kept, scale in zip((k, v), got, (pool.k, pool.v), (pool.ks, pool.vs)):
+        want = x.double()
+        if kind != "plain":
+            code, s, _ = cref.encode(x, kind)
+            want = cref.decode(cref.stored(code, kind), s.view(cref.SCALE), kind)
+        assert torch.equal(o.cpu().double(), want)
+        dense = cref.decode(kept, scale, kind)
+        assert torch.equal(torch.stack([dense[p, i] for p, i in at]), want)
+    compare(pool, 2)
+
+
 @pytest.mark.parametrize("kind", ["e4m3", "e2m1"])
 def test_finite_values_read_back_finite(kind):
     """Up to the type's largest; each within half a step of its block's scale."""
