@@ -329,8 +329,9 @@ int dconv_probe_latency(const int *chain, int steps, long long *out, void *strea
  * bf16 tensors, compute in fp32 (sums, statistics and angles included) and
  * round each output once.  dconv_attend and its gradient round one thing more
  * for fp16 and bf16: the probabilities and their gradients, which are operands
- * of matrix instructions of the tensors' type (fp32 has no such rounding).  As
- * for the convolutions: device pointers owned by the caller, arguments
+ * of matrix instructions of the tensors' type (fp32 has no such rounding).  In
+ * fp16 dconv_attend's probabilities below 2^-24 of their row's largest are
+ * rounded to steps of 2^-34 of it.  As for the convolutions: device pointers owned by the caller, arguments
  * validated before any HIP call, work enqueued on `stream`, nothing allocated
  * (a workspace is the caller's), bitwise equal results for equal calls on a
  * device.  Strides count elements; the last
@@ -581,6 +582,8 @@ int dconv_cache_read(const dconv_cache *cache, const dconv_cache_rows *rows, con
  * Keys and values that are not seen do not reach a result, whatever they, their
  * scales and the table's entries behind a sequence's last page hold.  Values of
  * 8 and 4 bits are rounded to the type of q (which changes nothing for bf16).
+ * Probabilities are rounded as dconv_attend's are: to the type of q, for fp16 and
+ * bf16, and in fp16 to no finer steps than 2^-34 of their row's largest.
  * 1 <= D <= 256; table_width * page_size and N * Hq below 2^31 - 2^16, B up to
  * 2^20, else DCONV_ERANGE.
  */

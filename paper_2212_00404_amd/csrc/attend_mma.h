@@ -382,18 +382,27 @@ struct Softmax {
       for (int i = 0; i < 16; ++i) s[i] = gone >> acc_row(i, lane >> 5) & 1 ? -INFINITY : s[i];
     }
   }
-  // The base follows the maximum only when it is left behind by more than 2^8:
-  // sums and probabilities stay below 2^8 times their true size, and the
-  // rescaling of the result is rare.  before(): what has to be added first.
+  // The base is set kBelow powers of two under the largest score, and follows it only
+  // when it is left kLag further behind: sums and probabilities stay below
+  // 2^(kBelow + kLag) times their true size, and the rescaling of the result is rare.
+  // bf16 and fp32 have range enough for the base to be the largest itself.  An fp16
+  // operand is rounded to steps of 2^-24 however small it is: with the base at the
+  // largest, a key of 2^-25.5 of its weight would be lost from the result and kept in the
+  // sum, 0.28% of all weight for 131072 such keys beside one.  From 2^10 under it steps are
+  // 2^-34 of the largest's weight (131072 keys: 2^-18 of it lost at most), and
+  // 2^14 leaves two powers of two of fp16's range for the rounding of large scores.
+  // The price is a lag of 2^4 instead of 2^8.
+  static constexpr float kBelow = __is_same(T, f16_t) ? 10.0f : 0.0f, kLag = __is_same(T, f16_t) ? 4.0f : 8.0f;
+  // before(): what has to be added first.
   template <class F>
   __device__ __forceinline__ void follow(const f32x16 &s, float scale2, F before) {
     float top = s[0];
 #pragma unroll
     for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
     top = half_max(top) * scale2;
-    if (__any(top - m > 8.0f)) {
+    if (__any(top - m > kBelow + kLag)) {
       before();
-      const float to = fmaxf(m, top);
+      const float to = fmaxf(m, top - kBelow);
       const float keep = to == -INFINITY ? 1.0f : exp2f(m - to);
 #pragma unroll
       for (int c = 0; c < DT; ++c) o[c] *= keep;
