@@ -151,8 +151,9 @@ class TokenBlock:
     @torch.no_grad()
     def serve_in_pages(self, x, prompt=100, kind=None, page=16):
         """The same over a cache in pages (of ``kind``, else of the block's type): the
-        first tokens in a chunk, then one at a time."""
+        first ``prompt`` tokens (all, if there are fewer) in a chunk, then one at a time."""
         B, T, _ = x.shape
+        prompt = min(max(prompt, 0), T)
         each = -(-T // page)
         cache = dc.Cache.new(B * each, page, self.Hkv, self.head, kind or x.dtype, device=x.device)
         table = torch.arange(B * each, dtype=torch.int32, device=x.device).view(B, each)
