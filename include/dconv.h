@@ -503,7 +503,9 @@ int dconv_attend_backward(const dconv_attend_shape *shape, const void *dout, con
  *     none where they fall), or, with offsets NULL, N / B rows like every
  *     other (N a multiple of B).  They are its last tokens: row t of its n rows
  *     stands at position lengths[b] - n + t.  Rows of no sequence (behind
- *     offsets[B]) are neither read nor written.
+ *     offsets[B], as a rule) are neither read nor written.  Where offsets fall
+ *     and rise again so that two sequences have a row, what is read, written or
+ *     computed for that row is not defined; everything else is.
  *   lengths : int32 [B], the tokens of each sequence, its rows among them;
  *     taken as 0 .. table_width * page_size
  *   table : int32 [B][table_width] with a stride for sequences; an entry that is

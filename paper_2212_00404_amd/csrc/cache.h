@@ -74,8 +74,9 @@ __device__ __forceinline__ Rows rows_of(const Batch &t, const CachePtrs &p, int 
   return r;
 }
 
-// The sequence of a row, -1 for a row of none: the last one that begins at or
-// before it, if it has not ended.
+// The sequence of a row by bisection, -1 if that finds none: where offsets rise, the
+// row is then of no sequence.  Where they fall somewhere, it finds one that has the row
+// for every row in offsets[0] .. offsets[B] - 1, and for others may miss one.
 __device__ __forceinline__ int sequence_of(const Batch &t, const CachePtrs &p, int row) {
   if (!p.offsets) return row / t.each;
   int lo = 0, hi = t.B;   // offsets[lo] <= row < offsets[hi], as far as they rise
