@@ -455,9 +455,9 @@ struct Softmax {
 
   // Adds 32 keys, v0 .., of the tiles ks, vs.
   __device__ __forceinline__ void add(const T *ks, const T *vs, const Frag (&q)[KS], int v0, const RowKeys &see,
-                                      int sinks, float scale2, bool masked, int lane, uint32_t gone = 0) {
+                                      int sinks, float scale2, bool masked, int lane) {
     f32x16 s = scores(ks, 0, q, lane);
-    if (masked) mask(s, v0, see, sinks, lane, gone);
+    if (masked) mask(s, v0, see, sinks, lane);
     follow(s, scale2, [] {});
     Frag w[2];
     probabilities(s, scale2, w);
@@ -467,19 +467,18 @@ struct Softmax {
   // probabilities, and the first half's sum beside the second's probabilities: the
   // matrix and the vector unit work at the same time within a wave.
   __device__ __forceinline__ void add_two(const T *ks, const T *vs, const Frag (&q)[KS], int v0, const RowKeys &see,
-                                          int sinks, float scale2, bool masked, int lane, uint64_t gone = 0) {
-    const uint32_t gone0 = (uint32_t)gone, gone1 = (uint32_t)(gone >> 32);
+                                          int sinks, float scale2, bool masked, int lane) {
     Frag w0[2], w1[2];
     if constexpr (DP > 96) {
       // (operands read ahead would not leave registers for two waves per SIMD, and
       // a register that comes back from memory waits for the copies too)
       f32x16 s0 = scores(ks, 0, q, lane);
-      if (masked) mask(s0, v0, see, sinks, lane, gone0);
+      if (masked) mask(s0, v0, see, sinks, lane);
       follow(s0, scale2, [] {});
       f32x16 s1 = scores(ks, 32, q, lane);
       probabilities(s0, scale2, w0);
       asm volatile("" ::"v"(w0[0]), "v"(w0[1]));   // here, not after the next branch
-      if (masked) mask(s1, v0 + 32, see, sinks, lane, gone1);
+      if (masked) mask(s1, v0 + 32, see, sinks, lane);
       follow(s1, scale2, [&] {
         values(vs, 0, w0, lane);
         w0[0] = w0[1] = Frag{};
@@ -495,14 +494,14 @@ struct Softmax {
     f32x16 s0 = products(kf, q), s1;
     load_keys(kf, ks, 32, lane);
     in_order();
-    if (masked) mask(s0, v0, see, sinks, lane, gone0);
+    if (masked) mask(s0, v0, see, sinks, lane);
     follow(s0, scale2, [] {});
     s1 = products(kf, q);
     load_values(vf[0], vs, 0, lane);
     in_order();
     probabilities(s0, scale2, w0);
     asm volatile("" ::"v"(w0[0]), "v"(w0[1]));
-    if (masked) mask(s1, v0 + 32, see, sinks, lane, gone1);
+    if (masked) mask(s1, v0 + 32, see, sinks, lane);
     follow(s1, scale2, [&] {
       values(vs, 0, w0, lane);
       w0[0] = w0[1] = Frag{};
