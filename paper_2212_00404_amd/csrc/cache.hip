@@ -189,8 +189,8 @@ __device__ __forceinline__ Codes<FORMAT == DCONV_CACHE_E4M3 ? 2 : 1> encode(cons
 
 // A thread's pieces, a batch on their way at a time.
 // (Writing gains nothing by it: a prompt of 61096 tokens, 8 heads of 128, bf16 into
-// e4m3, 379 MB, takes 95 us by one at a time and 108 by four, which leave registers for
-// five waves per SIMD; reading 65536 back takes 107 us by four and 113 by one.)
+// e4m3, 379 MB, takes 94 us by one at a time and 111 by four, which leave registers for
+// five waves per SIMD; reading 65536 back takes 99 us by four and 103 by one.)
 constexpr int kWriteBatch = 1, kReadBatch = 4;
 
 template <class T, int FORMAT>

@@ -713,10 +713,11 @@ constexpr int cache_part() { return R * (DP + 2); }
 // A plain cache's tiles are copied into two LDS buffers in turn, the next while the
 // current one is used; codes come a tile ahead into registers and go into the other
 // buffer after it.  Chunks of 401 to 512 tokens over up to 8192, 32 heads of 128 over
-// 8, bf16: 168 GFLOP of seen scores in 243 us (690 TFLOP/s; matrix cores busy in 0.34 of the
-// cycles, vector instructions issuing in 0.40, waves waiting in 0.43: two waves per
-// SIMD, each a chain of operands, products and exponentials, do not fill it), and 24 us
-// for the join of rows that two or three workgroups have parts of.
+// 8, bf16: 168 GFLOP of seen scores in 247 us (680 TFLOP/s; matrix cores busy in 0.38 of the
+// cycles, vector instructions issuing in 0.42, waves waiting for data in 0.25 of theirs and
+// for a unit in 0.31: two waves per SIMD, each a chain of operands, products and
+// exponentials, do not fill it), and 24 us for the join of rows that two or three
+// workgroups have parts of.
 template <class T, int DP, int FORMAT, bool ONE, int LEN>
 __device__ __forceinline__ void tiles_body(T (&buf0)[LEN], T (&buf1)[LEN], RangeScratch &scratch) {
   constexpr int BN = forward_keys<T>(DP), KS = DP / 16, DT = DP / 32;
@@ -916,9 +917,10 @@ __device__ __forceinline__ void tiles_body(T (&buf0)[LEN], T (&buf1)[LEN], Range
 // No barrier between tiles.  Bound by memory for a plain cache: 32 sequences of 853 to
 // 16384 tokens, 8 key heads of 128, bf16, 1125 MB in 216 us (5.2 TB/s).  A tile of
 // codes takes a wave as long for half or a quarter of the bytes: 64 sequences over 4
-// key heads in e4m3, 568 MB in 140 us (4.1 TB/s); 131072 tokens, 8 heads, five rows
-// each of 4, e2m1, 142 MB in 43 us (3.3 TB/s), the same with all pages in L2.  Reading
-// codes two or three tiles ahead gains nothing (registers: 145 to 245 us for 568 MB).
+// key heads in e4m3, 568 MB in 144 us (3.9 TB/s); 131072 tokens, 8 heads, five rows
+// each of 4, e2m1, 142 MB in 45 us (3.2 TB/s), the same with all pages in L2.  Reading
+// codes two or three tiles ahead gains nothing, for want of registers (568 MB: 162 and 244
+// us a call, join and all, beside 151).
 template <class T, int DP>
 struct FewScratch {
   float ml[split_waves<T>(DP)][64];
