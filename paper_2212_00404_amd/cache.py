@@ -198,9 +198,10 @@ def attend_cache(q: torch.Tensor, cache: Cache, table: torch.Tensor, lengths: to
     ``max_rows``: no sequence has more rows than this (a longer one is left out);
     by it a call of few rows each is one launch less.  Without offsets it is N / B.
 
-    Returns ``out[N, Hq, D]`` (rows behind the last sequence are left as they were,
-    in the ``out`` that was passed); with ``return_lse`` also the logarithms of the
-    softmax sums, fp32 ``[N, Hq]``.
+    Returns ``out[N, Hq, D]``; with ``return_lse`` also the logarithms of the softmax
+    sums, fp32 ``[N, Hq]``.  Rows behind the last sequence, and those of a sequence
+    longer than ``max_rows``, are left as they were in the ``out`` that was passed, and
+    are of no meaning in tensors that the call makes.  ``out`` must not overlap ``q``.
     """
     if not isinstance(q, torch.Tensor):
         raise ValueError("q must be a torch.Tensor")
